@@ -387,6 +387,81 @@ int st_generate_batch(st_batch *small, st_batch *large, const st_host_rule *rule
  * n_layers launches, *step_us the device time of the whole step.  kv_len += 1. */
 int st_decode_step_timed(st_model *m, double *gateup_mean_us, double *step_us);
 
+/* ---- A key/value cache held in 4 bits ----
+ *
+ * For long traces and many sequences: 4.25 bits a number instead of 16, with the operators around it -- norms and rotation with
+ * the write (append), attention (attend), eviction by accumulated attention weight (evict) -- as calls of one layer or several, for
+ * callers that run the rest of a decoder themselves.
+ *
+ * Format (OCP microscaling FP4).  32 neighbouring channels of a head are a group: one byte b, the scale 2^(b - 127), and 4-bit codes, bit 3 the
+ * sign, bits 0-2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  The scale is the least with max |x| <= 7 * scale, its exponent at least -100 and at most 125;
+ * values go to the nearest code, ties to the even one, what lies above 6 to 6.  A group that holds an infinity or a NaN has b = 255 and codes 0
+ * and reads as NaN.  The cache buffer is four planes, each starting at a multiple of 256 bytes: key codes, value codes, key scales, value scales, each
+ * [layer][sequence][kv head][slot][head_dim / 2 or head_dim / 32 bytes]; byte i of a slot's codes is channel 2 i (low four bits) and 2 i + 1.
+ *
+ * The caller says where each sequence stands: a call takes spans, and nothing is remembered from one call to the next, so that a
+ * context is rolled back by passing a smaller len.  A slot is not a position: after an eviction a sequence is at a
+ * later position than it has slots, and its slots are in no particular order. */
+typedef struct st_kv4 st_kv4;
+#define ST_KV4_MAX_SPANS 64
+typedef struct {
+    int32_t n_layers, n_seq, n_q_heads, n_kv_heads, head_dim;
+    int32_t max_seq;  /* slots of a sequence */
+    int32_t max_rows; /* most new rows of one append or attend */
+    int32_t max_pos;  /* positions the rotation table has */
+    float rms_eps;    /* of the norms of queries and keys */
+} st_kv4_config;
+/* Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, at most 16 times as many; max_seq <= 2^24, max_rows <= 2^20. */
+
+/* One sequence's part of a call: it has `len` slots, and `rows` new tokens at positions pos, pos + 1, ... go to (or are in)
+ * slots len, len + 1, ....  The rows of a call are those of its spans one after the other.  The sequences of a call are distinct; rows may be 0. */
+typedef struct {
+    int32_t seq, len, pos, rows;
+} st_kv4_span;
+
+/* What eviction goes by, in device memory of the caller's, both [layer][sequence][kv head][max_seq]: the attention weight each slot has
+ * received and the position of the token in it. */
+typedef struct {
+    float *weights;
+    int32_t *positions;
+} st_kv4_ledger;
+
+/* As st_query_sizes. */
+int st_kv4_query_sizes(const st_kv4_config *cfg, size_t *cache_bytes, size_t *workspace_bytes);
+/* rope: device fp32 [max_pos][head_dim / 2][2], (cos, sin) of every position and rotation pair (i, i + head_dim / 2), 16-byte aligned.  cache and
+ * workspace: device memory, 256-byte aligned; neither needs clearing.  All three are borrowed until st_kv4_destroy.  Every call enqueues on
+ * `stream` and returns without waiting. */
+int st_kv4_create(const st_kv4_config *cfg, const float *rope, void *cache, size_t cache_bytes, void *workspace,
+                  size_t workspace_bytes, void *stream, st_kv4 **out);
+void st_kv4_destroy(st_kv4 *c);
+
+/* Norms, rotation and the write of new rows.  qkv: bf16, a row holds all query heads, then the key heads, then the value heads; rows qkv_stride
+ * elements apart.  With q_norm and k_norm (bf16[head_dim], both or neither) queries and keys are first divided by the root mean square
+ * of their head (rms_eps inside the root) and multiplied by the norm.  Rotated queries go to q_out (bf16, n_q_heads * head_dim a row, rows
+ * q_stride apart), rotated keys and the values to slots [len, len + rows).  Every operation rounds to fp32 by itself and the sum of squares adds
+ * neighbours first, so the codes depend on nothing but the inputs.  With a ledger the new slots' weights become 0 and their positions are noted.
+ * Matrices are 16-byte aligned with strides that are multiples of 8.  ST_ERANGE: a span outside the cache or the table, too many rows. */
+int st_kv4_append(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *qkv, int64_t qkv_stride,
+                  const void *q_norm, const void *k_norm, void *q_out, int64_t q_stride, const st_kv4_ledger *ledger);
+
+/* Causal attention over the cache: row i of a span attends to slots [0, len + i] of its sequence, those of the span's own rows, appended before,
+ * among them; scores are scaled by head_dim^-1/2.  q, out: bf16, n_q_heads * head_dim a row.  With a ledger the weight of every slot
+ * grows by the attention it received, summed over the rows and over the query heads of its kv head, in an order that does not change from run to run. */
+int st_kv4_attend(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *q, int64_t q_stride, void *out,
+                  int64_t out_stride, const st_kv4_ledger *ledger);
+
+/* Eviction: in layers [layer_lo, layer_hi) every kv head of the spans' sequences that has more than `keep` slots (span: len; rows is 0) is brought to
+ * `keep` of them.  Those at positions >= pos - recent stay (pos: the sequence's next position); of the others those of the largest weight,
+ * equal weights by the lower position, a NaN below every weight.  The slots below `keep` that are freed take, in ascending order, the slots at or above it that stay, in
+ * ascending order; nothing else moves.  Pass len = keep from then on.  The ledger's entries move along: in `ledger` itself if `into` is
+ * NULL, else to the slots [0, min(len, keep)) of `into`, and `ledger` stays as it was.  ST_EINVAL: keep <= 0, recent outside [0, keep]. */
+int st_kv4_evict(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, int32_t keep,
+                 int32_t recent, const st_kv4_ledger *ledger, const st_kv4_ledger *into);
+
+/* Slots [len, len + rows) of every span as the bf16 numbers they stand for (every one is a bf16 number): k_out and v_out are
+ * [layer_hi - layer_lo][rows of all spans][n_kv_heads][head_dim], 16-byte aligned. */
+int st_kv4_read(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, void *k_out, void *v_out);
+
 const char *st_last_error(void);
 
 #ifdef __cplusplus

@@ -22,7 +22,8 @@ EXPORTS = ("st_query_sizes", "st_prefill_plan_check", "st_prefill_plan_forms", "
            "st_decode_step_timed", "st_decode_greedy", "st_trigger_scan", "st_trigger_scan_static", "st_handoff",
            "st_generate", "st_generate_policy", "st_batch_query_sizes", "st_batch_create", "st_batch_destroy",
            "st_batch_kv_len", "st_batch_truncate", "st_batch_prefill", "st_batch_prefill_many", "st_batch_decode_step",
-           "st_generate_batch", "st_last_error")
+           "st_generate_batch", "st_kv4_query_sizes", "st_kv4_create", "st_kv4_destroy", "st_kv4_append", "st_kv4_attend",
+           "st_kv4_evict", "st_kv4_read", "st_last_error")
 
 
 class StError(RuntimeError):
@@ -61,6 +62,19 @@ class st_spans(C.Structure):
 class st_gen_stats(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_out", "n_handoffs", "n_large", "n_spans")] + \
                [(n, C.c_double) for n in ("ms_small_decode", "ms_large_decode", "ms_small_prefill", "ms_large_prefill")]
+
+
+class st_kv4_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seq", "n_q_heads", "n_kv_heads", "head_dim", "max_seq", "max_rows",
+                                         "max_pos")] + [("rms_eps", C.c_float)]
+
+
+class st_kv4_span(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "len", "pos", "rows")]
+
+
+class st_kv4_ledger(C.Structure):
+    _fields_ = [("weights", C.c_void_p), ("positions", C.c_void_p)]
 
 
 _lib = None
@@ -121,6 +135,18 @@ def lib():
         L.st_generate_batch.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
                                         C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                         C.POINTER(st_gen_stats)]
+        spans, ledger = C.POINTER(st_kv4_span), C.POINTER(st_kv4_ledger)
+        L.st_kv4_query_sizes.argtypes = [C.POINTER(st_kv4_config), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        L.st_kv4_create.argtypes = [C.POINTER(st_kv4_config), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
+                                    C.c_void_p, C.POINTER(C.c_void_p)]
+        L.st_kv4_destroy.argtypes = [C.c_void_p]
+        L.st_kv4_destroy.restype = None
+        L.st_kv4_append.argtypes = [C.c_void_p, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_int64, ledger]
+        L.st_kv4_attend.argtypes = [C.c_void_p, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                    ledger]
+        L.st_kv4_evict.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_int32, C.c_int32, ledger, ledger]
+        L.st_kv4_read.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -501,3 +527,146 @@ def st_generate_batch(small, large, prompts, n_out, n_seg, vocab, kw=None, delim
                                    None if phase is None else _np_ptr(phase), gather, n,
                                    arr(ps), _np_ptr(lens), n_out, n_seg, arr(seqs), arr(srcs), C.byref(stats)))
     return dict(seqs=seqs, srcs=srcs, stats={k: getattr(stats, k) for k, _ in st_gen_stats._fields_})
+
+
+class Kv4Spans:
+    """The spans of a call, (seq, len, pos, rows) each (see st_kv4_span); made once for all layers of a step."""
+
+    def __init__(self, spans):
+        self.spans = [tuple(int(x) for x in s) for s in spans]
+        self.n, self.rows = len(self.spans), sum(s[3] for s in self.spans)
+        self.c = (st_kv4_span * max(self.n, 1))(*self.spans)
+
+
+class Kv4Ledger:
+    """Accumulated attention weights (float32) and positions (int32), CUDA tensors [layer][sequence][kv head][max_seq]."""
+
+    def __init__(self, weights, positions):
+        if weights.dtype != torch.float32 or positions.dtype != torch.int32:
+            raise StError(ST_EINVAL, f"weights are float32 and positions int32, got {weights.dtype} and {positions.dtype}")
+        if weights.shape != positions.shape or not weights.is_contiguous() or not positions.is_contiguous():
+            raise StError(ST_EINVAL, "weights and positions are contiguous and of one shape")
+        if not weights.is_cuda or not positions.is_cuda:
+            raise StError(ST_EINVAL, "weights and positions must live on the GPU")
+        self.weights, self.positions = weights, positions
+        self.c = st_kv4_ledger(weights.data_ptr(), positions.data_ptr())
+
+
+def rope_table(max_pos, head_dim, theta, device="cuda"):
+    """(cos, sin) of every position and rotation pair, float32 [max_pos][head_dim / 2][2], computed in 64 bits."""
+    i = torch.arange(head_dim // 2, dtype=torch.float64, device=device)
+    a = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * theta ** (-2 * i / head_dim)
+    return torch.stack((a.cos(), a.sin()), -1).float().contiguous()
+
+
+class Kv4Cache:
+    """st_kv4 over torch-owned device buffers: a key/value cache held in 4 bits, with append, attend, evict and read.
+
+    cfg: dict of the fields of st_kv4_config.  Without `stream` the calls enqueue on the stream that was current when the cache was made, and are
+    refused under another one.  With it (a raw handle) ordering other streams' work against the calls is the caller's part."""
+
+    def __init__(self, cfg, rope, cache=None, stream=None):
+        self.cfg = dict(cfg)
+        c = st_kv4_config(*(cfg[n] for n, _ in st_kv4_config._fields_))
+        cb, wb = C.c_size_t(), C.c_size_t()
+        _check(lib().st_kv4_query_sizes(C.byref(c), C.byref(cb), C.byref(wb)))
+        if not rope.is_cuda or rope.dtype != torch.float32 or not rope.is_contiguous() or \
+                tuple(rope.shape) != (cfg["max_pos"], cfg["head_dim"] // 2, 2):
+            raise StError(ST_EINVAL, f"rope is a contiguous float32 CUDA tensor [max_pos][head_dim / 2][2], got {rope.dtype} {tuple(rope.shape)}")
+        dev = rope.device
+        if cache is None:
+            cache = torch.empty(cb.value, dtype=torch.uint8, device=dev)
+        elif cache.device != dev or cache.dtype != torch.uint8 or not cache.is_contiguous():
+            raise StError(ST_EINVAL, "cache is a contiguous uint8 tensor on the device of rope")
+        self.cache, self.rope, self._dev = cache, rope, dev
+        self._ws = torch.empty(wb.value, dtype=torch.uint8, device=dev)
+        self._own_stream = stream is not None
+        self.stream = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
+        h = C.c_void_p()
+        _check(lib().st_kv4_create(C.byref(c), rope.data_ptr(), cache.data_ptr(), cache.numel(), self._ws.data_ptr(),
+                                   wb.value, self.stream, C.byref(h)))
+        self._h = h
+        self._slots = (cfg["n_layers"], cfg["n_seq"], cfg["n_kv_heads"], cfg["max_seq"])
+        self._nq, self._nkv, self._d = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"]
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().st_kv4_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _alloc(self, *shape):
+        if not self._own_stream:
+            return torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+        with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self._dev)):
+            return torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+
+    def _enter(self):
+        if not self._own_stream and torch.cuda.current_stream(self._dev).cuda_stream != self.stream:
+            raise StError(ST_EINVAL, "called under another stream than the cache was made on")
+
+    def _matrix(self, name, x, rows, heads):
+        """(pointer, row stride) of bf16 [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
+        if x.dtype != torch.bfloat16 or x.device != self._dev:
+            raise StError(ST_EINVAL, f"{name} is bfloat16 on {self._dev}, got {x.dtype} on {x.device}")
+        d, shape, stride = self._d, x.shape, x.stride()
+        if not (len(shape) == 2 and shape[1] == heads * d and stride[1] == 1 or
+                len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1)) or \
+                shape[0] != rows:
+            raise StError(ST_EINVAL, f"{name} has shape {tuple(shape)} and strides {stride}, needs {rows} rows of {heads} x {d}")
+        return x.data_ptr(), stride[0] if rows > 1 else max(stride[0], heads * d)
+
+    def _ledger(self, ledger):
+        if ledger is None:
+            return None
+        if tuple(ledger.weights.shape) != self._slots:
+            raise StError(ST_EINVAL, f"the ledger has shape {tuple(ledger.weights.shape)}, needs {self._slots}")
+        if ledger.weights.device != self._dev:
+            raise StError(ST_EINVAL, f"the ledger is on {ledger.weights.device}, the cache on {self._dev}")
+        return C.byref(ledger.c)
+
+    def append(self, layer, spans, qkv, q_norm=None, k_norm=None, ledger=None):
+        """Norms (bf16 [head_dim], or None), rotation and the write of the spans' new rows; qkv: bf16, a row per new token, all query
+        heads, then key heads, then value heads.  Returns the rotated queries, bf16 [rows][n_q_heads][head_dim]."""
+        self._enter()
+        p, stride = self._matrix("qkv", qkv, spans.rows, self._nq + 2 * self._nkv)
+        norms = []
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None and (w.dtype != torch.bfloat16 or tuple(w.shape) != (self._d,) or not w.is_contiguous() or w.device != self._dev):
+                raise StError(ST_EINVAL, f"{name} is bfloat16 [{self._d}] on {self._dev}, got {w.dtype} {tuple(w.shape)}")
+            norms.append(None if w is None else w.data_ptr())
+        out = self._alloc(spans.rows, self._nq, self._d)
+        if spans.rows:
+            _check(lib().st_kv4_append(self._h, layer, spans.c, spans.n, p, stride, *norms, out.data_ptr(), self._nq * self._d,
+                                       self._ledger(ledger)))
+        return out
+
+    def attend(self, layer, spans, q, ledger=None, out=None):
+        """Attention of the spans' rows over their sequences' slots; q: bf16, n_q_heads * head_dim a row.  With a ledger its weights grow by what every
+        slot received.  Returns bf16 [rows][n_q_heads][head_dim] (or `out`)."""
+        self._enter()
+        p, stride = self._matrix("q", q, spans.rows, self._nq)
+        if out is None:
+            out = self._alloc(spans.rows, self._nq, self._d)
+        po, so = self._matrix("out", out, spans.rows, self._nq)
+        if spans.rows:
+            _check(lib().st_kv4_attend(self._h, layer, spans.c, spans.n, p, stride, po, so, self._ledger(ledger)))
+        return out
+
+    def evict(self, layer_lo, layer_hi, spans, keep, recent, ledger, into=None):
+        """Brings the spans' sequences to `keep` slots in layers [layer_lo, layer_hi) (see st_kv4_evict); the ledger's entries move along, in place or to `into`."""
+        self._enter()
+        _check(lib().st_kv4_evict(self._h, layer_lo, layer_hi, spans.c, spans.n, keep, recent, self._ledger(ledger), self._ledger(into)))
+
+    def read(self, layer_lo, layer_hi, spans):
+        """Slots [len, len + rows) of the spans as bf16 (k, v), each [layers][rows][n_kv_heads][head_dim]."""
+        self._enter()
+        k, v = (self._alloc(max(layer_hi - layer_lo, 0), spans.rows, self._nkv, self._d) for _ in range(2))
+        if k.numel():
+            _check(lib().st_kv4_read(self._h, layer_lo, layer_hi, spans.c, spans.n, k.data_ptr(), v.data_ptr()))
+        return k, v

@@ -1,0 +1,74 @@
+// Host-side internals of the 4-bit key/value cache (kv4.hip, kv4_attend.hip, kv4_evict.hip): its record, the span table that the kernels
+// take by value and the launchers the API layer calls.  Nothing here is part of the public ABI.
+#pragma once
+
+#include "st_internal.h"
+
+namespace st {
+
+// One sequence's part of a call, with what the launch gives it.
+struct Kv4Span {
+    int32_t seq, len, pos, rows;  // st_kv4_span
+    int32_t row0;                 // its first row among the call's rows
+    int32_t blk0;                 // its first block in the launch
+    int32_t splits;               // key ranges its blocks are dealt to
+    int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
+};
+// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.
+struct Kv4Table {
+    int32_t n, per;  // spans; key tiles of one range
+    Kv4Span s[ST_KV4_MAX_SPANS];
+};
+static_assert(sizeof(Kv4Table) <= 2200, "kernel arguments are at most 4 KB");
+
+// The planes of one layer and its heads
+struct Kv4View {
+    uint8_t *k, *v, *ks, *vs;  // [sequence][kv head][slot][head_dim / 2 | head_dim / 32]
+    int32_t nq, nkv, max_seq;
+};
+
+struct Kv4 {
+    st_kv4_config c;
+    uint8_t *plane[4];       // K codes, V codes, K scales, V scales, [layer][sequence][kv head][slot][...]
+    size_t per_layer[4];     // bytes of a layer in each
+    const float *rope;       // [max_pos][head_dim / 2][2]
+    float *lse;              // [max_rows][n_q_heads] log2 of each row's softmax sum
+    float *part_ml, *part_o; // partial results of the key ranges: (max, sum) and outputs
+    size_t part_rows;        // rows they hold
+    uint64_t *kept;          // evict: a bit per slot, [layer][span][kv head][kept_words]
+    size_t kept_words;
+    hipStream_t stream;
+    Kv4View view(int layer) const {
+        return Kv4View{plane[0] + layer * per_layer[0], plane[1] + layer * per_layer[1], plane[2] + layer * per_layer[2],
+                       plane[3] + layer * per_layer[3], c.n_q_heads, c.n_kv_heads, c.max_seq};
+    }
+};
+
+// All enqueue only; the arguments have been checked.  `t` holds spans and row0; the launchers fill in the rest.
+void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, const bf16_t *qkv, int64_t qkv_stride,
+                       const bf16_t *q_norm, const bf16_t *k_norm, bf16_t *q_out, int64_t q_stride, float *weights,
+                       int32_t *positions);
+void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out);
+void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf16_t *q, int64_t q_stride, bf16_t *out,
+                       int64_t out_stride, float *weights);
+void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
+                      const int32_t *p_in, float *w_out, int32_t *p_out);
+
+#ifdef __HIPCC__
+// The span whose blocks block `b` belongs to: the last one that starts at or before it (spans without blocks share their
+// start with the next one).  Wave-uniform; all lanes must be active.
+__device__ __forceinline__ int kv4_span_of(const Kv4Table &t, int b) {
+    const int lane = threadIdx.x & 63;
+    const bool at_or_before = lane < t.n && t.s[lane].blk0 <= b;
+    return __builtin_amdgcn_readfirstlane(63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(at_or_before)));
+}
+constexpr int kKv4Nan = 255;  // scale byte of a group that held an infinity or a NaN
+__device__ __forceinline__ float kv4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+// two codes (byte `B` of w: low nibble, high nibble) as two bf16
+template <int B>
+__device__ __forceinline__ uint32_t kv4_pair(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+}
+#endif
+
+}  // namespace st

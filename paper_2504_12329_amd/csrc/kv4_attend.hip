@@ -1,0 +1,739 @@
+// Attention over the 4-bit key/value cache, and the attention weight each of its slots receives.
+//
+// Row i of a span (seq, len, rows) sees slots [0, len + i].  The query heads of a kv head are folded into columns: column i * G + h is row i of
+// head h.  With S^T = K Q^T (slots x columns) a lane holds one column, so the softmax is register arithmetic and P^T is the
+// second product's operand as it stands: O^T = V^T P^T.  Codes become bf16 in registers (v_cvt_scalef32_pk_bf16_fp4, two
+// values an instruction, exact); keys give eight channels of a slot to a lane, which is what the first product
+// wants, values come as channel pairs of one slot and are put together with the neighbouring slot's by a byte permute.
+// Scores, maxima, sums and outputs are fp32; the weights enter the second product as bf16 (rounded just below the running maximum's 1, where
+// that costs least), as the model's own attention does.
+//
+// A value group that held an infinity or NaN reads as NaN, and reaches exactly the rows that see it: in tiles that some row sees only
+// in part such groups are multiplied as zeros and the rows that see them marked.
+#include <utility>
+
+#include "kv4.h"
+#include "st_device.h"
+
+namespace st {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));  // scales: rows of two or four bytes
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ u32x4 keys8(uint32_t w, float unit) {  // eight channels of one slot
+    return u32x4{kv4_pair<0>(w, unit), kv4_pair<1>(w, unit), kv4_pair<2>(w, unit), kv4_pair<3>(w, unit)};
+}
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// Eight slots x D / 16 (or 8) channels of V as a lane loads them: codes of slot j in c[j] (two or four bytes), scale bytes of the slots'
+// group in b[j]
+template <int NB>  // bytes of codes of a slot: 2 or 4
+struct Values8 {
+    uint32_t c[8], b[8];
+    // channels 2 B and 2 B + 1 of the eight slots
+    template <int B>
+    __device__ __forceinline__ void pairs(u32x4 &even, u32x4 &odd) const {
+        uint32_t p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = kv4_pair<B>(c[j], kv4_scale(b[j]));
+        even = u32x4{low_halves(p[0], p[1]), low_halves(p[2], p[3]), low_halves(p[4], p[5]), low_halves(p[6], p[7])};
+        odd = u32x4{high_halves(p[0], p[1]), high_halves(p[2], p[3]), high_halves(p[4], p[5]), high_halves(p[6], p[7])};
+    }
+    __device__ __forceinline__ bool any_nan() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, b[j]);
+        return m == (uint32_t)kKv4Nan;
+    }
+    __device__ __forceinline__ void nan_to_zero() {  // (their codes are zeros)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = b[j] == (uint32_t)kKv4Nan ? 0 : b[j];
+    }
+};
+// Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each, scale byte `group`.  TAIL: slots past `last` are
+// read as `last` (no address past it is formed).
+template <int D, int NB, bool TAIL>
+__device__ __forceinline__ void load_values(Values8<NB> &v, const uint8_t *codes, const uint8_t *scales, int key, int last,
+                                            int at, int group) {
+    constexpr int CB = D / 2, SB = D / 32;
+    auto code = [&](int slot) -> uint32_t {
+        const uint8_t *p = codes + (uint32_t)slot * CB + at;
+        if constexpr (NB == 4) return *reinterpret_cast<const uint32_t *>(p);
+        return *reinterpret_cast<const uint16_t *>(p);
+    };
+    if constexpr (TAIL) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int slot = min(key + j, last);
+            v.c[j] = code(slot);
+            v.b[j] = scales[(uint32_t)slot * SB + group];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v.c[j] = code(key + j);
+        const u32x4_a2 *p = reinterpret_cast<const u32x4_a2 *>(scales + (uint32_t)key * SB);
+        if constexpr (SB == 4) {
+            const u32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.b[j] = a[j] >> (8 * group) & 255, v.b[4 + j] = b[j] >> (8 * group) & 255;
+        } else {
+            const u32x4 a = p[0];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v.b[j] = a[j >> 1] >> (16 * (j & 1) + 8 * group) & 255;
+        }
+    }
+}
+
+// Where a column's query is
+struct Column {
+    int row, head;  // row of the span, query head
+};
+__device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Column{col / G, kvh * G + col % G}; }
+
+// ---------------------------------------------------------------------------------------
+// Few columns (rows x G <= 64 in every span): single tokens and short runs.  Bound by memory: the cache is read once and every
+// value meets at most 64 columns.
+//
+// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end: S^T by 16x16x32 MFMAs whose A rows
+// are slots 8 (m / 4) + 4 t + m % 4, so that lane (column, quarter) ends up with the weights of slots 8 quarter .. + 7 -- the
+// B operand of the second product.  A lane reads 16 bytes (one scale group) of each of its two keys and, of eight value
+// slots, the D / 16 channels that make its row m of D / 16 products.  The next tile's loads are issued before
+// this tile's work.  A block's four waves take every fourth tile of its range and are joined through LDS; ranges are joined by k_kv4_join.
+// ---------------------------------------------------------------------------------------
+constexpr int kFewTile = 32, kFewWaves = 4;
+
+template <int D, int NT>
+__global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+                                                 int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
+                                                 float *__restrict__ part_o, float *__restrict__ part_ml,
+                                                 float *__restrict__ lse) {
+    constexpr int KS = D / 32, DPL = D / 16, NB = D / 32, CB = D / 2, SB = D / 32;
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m16 = lane & 15, qd = lane >> 4;
+    const int nkv = view.nkv, G = view.nq / nkv;
+    const int kvh = (blockIdx.x - sp.blk0) % nkv, z = (blockIdx.x - sp.blk0) / nkv;
+    const int n_keys = sp.len + sp.rows, last = n_keys - 1, n_tiles = (n_keys + kFewTile - 1) / kFewTile;
+    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
+    const uint8_t *kc = view.k + head0 * CB, *vc = view.v + head0 * CB, *ks = view.ks + head0 * SB, *vs = view.vs + head0 * SB;
+    const int cols = sp.rows * G;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+
+    bf16x8 qf[NT][KS];
+    int lim[NT];  // last slot the column sees
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const Column w = column_of(min(16 * c + m16, cols - 1), G, kvh);
+        lim[c] = sp.len + w.row;
+        const bf16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * (D / 4);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[c][s] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 8 * s));
+    }
+    f32x4 o[NT][DPL];
+    float m_i[NT], l_i[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        m_i[c] = -INFINITY, l_i[c] = 0.f;
+#pragma unroll
+        for (int T = 0; T < DPL; ++T) o[c][T] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Tile {
+        uint32_t k[2][KS], kb[2];
+        Values8<NB> v;
+    };
+    auto load = [&](Tile &x, int tile) {
+        const int key0 = tile * kFewTile;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t slot = min(key0 + 8 * (m16 >> 2) + 4 * u + (m16 & 3), last);
+            if constexpr (D == 128) {
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(kc + slot * CB + qd * 16);
+                x.k[u][0] = w.x, x.k[u][1] = w.y, x.k[u][2] = w.z, x.k[u][3] = w.w;
+                x.kb[u] = ks[slot * SB + qd];
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2 *>(kc + slot * CB + qd * 8);
+                x.k[u][0] = w.x, x.k[u][1] = w.y;
+                x.kb[u] = ks[slot * SB + (qd >> 1)];
+            }
+        }
+        const int at = m16 * NB, group = m16 * DPL / 32;
+        if (key0 + kFewTile <= n_keys)
+            load_values<D, NB, false>(x.v, vc, vs, key0 + 8 * qd, last, at, group);
+        else
+            load_values<D, NB, true>(x.v, vc, vs, key0 + 8 * qd, last, at, group);
+    };
+    auto work = [&](Tile &x, int tile) {
+        const int key0 = tile * kFewTile;
+        f32x4 sc[NT][2];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) sc[c][0] = sc[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 kf = as_bf16x8(keys8(x.k[u][s], kv4_scale(x.kb[u])));
+#pragma unroll
+                for (int c = 0; c < NT; ++c) sc[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][s], sc[c][u], 0, 0, 0);
+            }
+        const bool part = key0 + kFewTile - 1 > sp.len;  // some row does not see all of the tile
+        uint32_t poison = 0;                              // columns (bit c) that see a NaN among this lane's output channels
+        if (part) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (key0 + 8 * qd + 4 * u + r > lim[c]) sc[c][u][r] = -INFINITY;
+            if (__builtin_amdgcn_ballot_w64(x.v.any_nan())) {
+                x.v.nan_to_zero();
+                for (int slot = key0; slot < min(key0 + kFewTile, n_keys); ++slot)
+                    if (vs[(uint32_t)slot * SB + qd * SB / 4] == kKv4Nan)
+#pragma unroll
+                        for (int c = 0; c < NT; ++c)
+                            if (slot <= lim[c]) poison |= 1u << c;
+            }
+        }
+        bf16x8 pf[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            float mx = sc[c][0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[c][u][r]);
+            float a, b;
+            with_xor16(mx, a, b);
+            mx = max_xor32(fmaxf(a, b));
+            const float cand = mx * scale;
+            const bool raise = cand > m_i[c];
+            const float m_new = raise ? cand : m_i[c];
+            const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
+            if (__builtin_amdgcn_ballot_w64(raise)) {
+                const float corr = raise ? __builtin_amdgcn_exp2f(m_i[c] - base) : 1.0f;
+                l_i[c] *= corr;
+#pragma unroll
+                for (int T = 0; T < DPL; ++T) o[c][T] *= corr;
+            }
+            m_i[c] = m_new;
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p[j] = __builtin_amdgcn_exp2f(fmaf(sc[c][j >> 2][j & 3], scale, -base));
+                l_i[c] += p[j];
+            }
+            pf[c] = as_bf16x8(u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+        }
+        auto multiply = [&](auto b_c) {
+            constexpr int B = decltype(b_c)::value;
+            u32x4 even, odd;
+            x.v.template pairs<B>(even, odd);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                o[c][2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pf[c], o[c][2 * B], 0, 0, 0);
+                o[c][2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(odd), pf[c], o[c][2 * B + 1], 0, 0, 0);
+            }
+        };
+        multiply(std::integral_constant<int, 0>{});
+        multiply(std::integral_constant<int, 1>{});
+        if constexpr (NB == 4) {
+            multiply(std::integral_constant<int, 2>{});
+            multiply(std::integral_constant<int, 3>{});
+        }
+        if (__builtin_amdgcn_ballot_w64(poison != 0)) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                if (poison >> c & 1)
+#pragma unroll
+                    for (int T = 0; T < DPL; ++T) o[c][T] = f32x4{NAN, NAN, NAN, NAN};
+        }
+    };
+    Tile a, b;
+    int i = t_begin + wave;
+    if (i < t_end) load(a, i);
+    while (i < t_end) {
+        if (i + kFewWaves < t_end) load(b, i + kFewWaves);
+        work(a, i);
+        i += kFewWaves;
+        if (i >= t_end) break;
+        if (i + kFewWaves < t_end) load(a, i + kFewWaves);
+        work(b, i);
+        i += kFewWaves;
+    }
+
+    // the four waves' results, one tile of columns after another
+    constexpr int LD = D + 4;
+    __shared__ __align__(16) float so[kFewWaves][16][LD];
+    __shared__ float sm[kFewWaves][16], sl[kFewWaves][16];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const float l = sum_xor32(sum_xor16(l_i[c]));
+        if (c) __syncthreads();
+        if (qd == 0) sm[wave][m16] = m_i[c], sl[wave][m16] = l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int T = 0; T < DPL; T += 4)
+                *reinterpret_cast<float4 *>(&so[wave][m16][(4 * qd + r) * DPL + T]) =
+                    make_float4(o[c][T][r], o[c][T + 1][r], o[c][T + 2][r], o[c][T + 3][r]);
+        __syncthreads();
+        const int col = 16 * c + (threadIdx.x >> 4), n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DPL;
+        if (col >= cols) continue;
+        float M = sm[0][n], w[kFewWaves], L = 0.f;
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) M = fmaxf(M, sm[v][n]);
+        float x[DPL];
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v) {
+            w[v] = sm[v][n] == -INFINITY && !(sl[v][n] != sl[v][n]) ? 0.f : __builtin_amdgcn_exp2f(sm[v][n] - M);
+            L += w[v] * sl[v][n];
+#pragma unroll
+            for (int e = 0; e < DPL; ++e) x[e] = fmaf(w[v], so[v][n][d0 + e], x[e]);
+        }
+        const Column where = column_of(col, G, kvh);
+        if (sp.splits == 1) {
+            const float inv = 1.0f / L;
+            bf16_t *dst = out + (int64_t)(sp.row0 + where.row) * out_stride + where.head * D + d0;
+            if constexpr (DPL == 8)
+                *reinterpret_cast<u32x4 *>(dst) = u32x4{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
+                                                        pack_bf16x2(x[4] * inv, x[5] * inv), pack_bf16x2(x[6] * inv, x[7] * inv)};
+            else
+                *reinterpret_cast<u32x2 *>(dst) = u32x2{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
+            if (lse && d0 == 0) lse[(size_t)(sp.row0 + where.row) * view.nq + where.head] = M + __builtin_amdgcn_logf(L);
+        } else {
+            const size_t pr = (size_t)sp.part0 + ((size_t)z * sp.rows + where.row) * view.nq + where.head;
+#pragma unroll
+            for (int e = 0; e < DPL; e += 4)
+                *reinterpret_cast<float4 *>(part_o + pr * D + d0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            if (d0 == 0) *reinterpret_cast<float2 *>(part_ml + pr * 2) = make_float2(M, L);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Chunks.  A block is 128 columns of one kv head (four waves of 32) on a range of tiles of 128 slots.  The tile's codes are loaded one
+// tile ahead into registers, turned into bf16 once for all four waves and put into LDS as the MFMA operands that the
+// waves read: 1 KB fragments, 16 bytes a lane, no bank conflicts in writing or reading.  Two blocks share a compute
+// unit, so that one's products run beside the other's softmax.
+//   K: a thread has one scale group (32 channels) of one or two slots;  V: eight slots x eight channels.
+//   S^T rows: fragment row m of 32 slots is slot swap(m) (bits 2 and 3 exchanged): registers 0-7 and 8-15 of a lane are then eight
+//   consecutive slots each, as the second product wants them.
+// ---------------------------------------------------------------------------------------
+constexpr int kTileKeys = 128, kTileCols = 128;
+
+__device__ __forceinline__ int swap23(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+                                                      int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
+                                                      float *__restrict__ part_o, float *__restrict__ part_ml,
+                                                      float *__restrict__ lse) {
+    constexpr int CB = D / 2, SB = D / 32, ST = D / 16, TT = D / 32, NO = D / 8, PT = 32 / NO;  // PT: channels of an octet per tile
+    constexpr int KG = D / 64;  // scale groups of K per thread
+    __shared__ __align__(16) u32x4 kt[4 * ST * 64], vt[TT * 8 * 64];
+    __shared__ uint32_t nan_seen[4];
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+    const int nkv = view.nkv, G = view.nq / nkv, cols = sp.rows * G, n_cb = (cols + kTileCols - 1) / kTileCols;
+    const int local = blockIdx.x - sp.blk0, kvh = local % nkv, z = local / nkv / n_cb;
+    const int cb = n_cb - 1 - local / nkv % n_cb;  // the blocks with the most slots first
+    const int c0 = cb * kTileCols + wave * 32, col = min(c0 + l32, cols - 1);
+    const bool active = c0 < cols;
+    const Column where = column_of(col, G, kvh);
+    const int lim = sp.len + where.row;
+    const int wave_first = sp.len + min(c0, cols - 1) / G, wave_last = sp.len + min(c0 + 31, cols - 1) / G;
+    const int n_keys = sp.len + min(cb * kTileCols + kTileCols - 1, cols - 1) / G + 1, last = n_keys - 1;
+    const int n_tiles = (n_keys + kTileKeys - 1) / kTileKeys;
+    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
+    const uint8_t *kc = view.k + head0 * CB, *vc = view.v + head0 * CB, *ks = view.ks + head0 * SB, *vs = view.vs + head0 * SB;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+
+    bf16x8 qf[ST];
+    {
+        const bf16_t *src = q + (int64_t)(sp.row0 + where.row) * q_stride + where.head * D + 8 * hf;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) qf[s] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 16 * s));
+    }
+    f32x16 o[TT];
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[tt][r] = 0.f;
+    float m_i = -INFINITY, l_i = 0.f;
+
+    // this thread's part of a tile
+    const int k_slot = tid & 127, k_group = tid >> 7;                     // K: groups k_group and k_group + 2
+    const int v_oct = tid % NO, v_kb = tid / NO;                          // V: channels 8 v_oct .. + 7 of slots 8 v_kb .. + 7
+    const bool has_v = v_kb < 16;
+    u32x4 kw[KG];
+    uint32_t kb[KG];
+    Values8<4> vw;
+    auto load = [&](int tile) {
+        const int key0 = tile * kTileKeys;
+        const uint32_t slot = min(key0 + k_slot, last);
+#pragma unroll
+        for (int e = 0; e < KG; ++e) {
+            kw[e] = *reinterpret_cast<const u32x4 *>(kc + slot * CB + (k_group + 2 * e) * 16);
+            kb[e] = ks[slot * SB + k_group + 2 * e];
+        }
+        if (!has_v) return;
+        if (key0 + kTileKeys <= n_keys)
+            load_values<D, 4, false>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct, v_oct >> 2);
+        else
+            load_values<D, 4, true>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct, v_oct >> 2);
+    };
+    auto stage = [&]() {
+        const int u = k_slot >> 5, m = swap23(k_slot & 31);
+#pragma unroll
+        for (int e = 0; e < KG; ++e) {
+            const float unit = kv4_scale(kb[e]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)  // channels 32 group + 8 c
+                kt[(u * ST + 2 * (k_group + 2 * e) + (c >> 1)) * 64 + (c & 1) * 32 + m] = keys8(kw[e][c], unit);
+        }
+        const bool bad = has_v && vw.any_nan();
+        if (bad) vw.nan_to_zero();
+        const uint64_t any = __builtin_amdgcn_ballot_w64(bad);
+        if (lane == 0) nan_seen[wave] = any != 0;
+        if (!has_v) return;
+        u32x4 *dst = &vt[(v_kb >> 1) * 64 + (v_kb & 1) * 32 + v_oct];  // channel 8 v_oct + e: tile e / PT, row v_oct + NO (e % PT)
+        auto put = [&](auto b_c) {
+            constexpr int B = decltype(b_c)::value;
+            u32x4 even, odd;
+            vw.template pairs<B>(even, odd);
+            dst[(2 * B) / PT * 512 + NO * ((2 * B) % PT)] = even;
+            dst[(2 * B + 1) / PT * 512 + NO * ((2 * B + 1) % PT)] = odd;
+        };
+        put(std::integral_constant<int, 0>{});
+        put(std::integral_constant<int, 1>{});
+        put(std::integral_constant<int, 2>{});
+        put(std::integral_constant<int, 3>{});
+    };
+    auto half_tile = [&](int key0, auto h_c) {  // 64 slots
+        constexpr int H = decltype(h_c)::value;
+        f32x16 sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kt[((2 * H + u) * ST + s) * 64 + lane]), qf[s], sc[u], 0, 0, 0);
+        if (key0 + 63 > wave_first) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + 32 * u + 16 * (r >> 3) + 8 * hf + (r & 7) > lim) sc[u][r] = -INFINITY;
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[u][r]);
+        mx = max_xor32(mx);
+        const float cand = mx * scale;
+        const bool raise = cand > m_i;
+        const float m_new = raise ? cand : m_i;
+        const float base = m_new == -INFINITY ? 0.f : m_new;  // a row may see no slot of this range
+        if (__builtin_amdgcn_ballot_w64(raise)) {
+            const float corr = raise ? __builtin_amdgcn_exp2f(m_i - base) : 1.0f;
+            l_i *= corr;
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[tt][r] *= corr;
+        }
+        m_i = m_new;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][r], scale, -base));
+                sc[u][r] = p;
+                l_i += p;
+            }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int u = s >> 1, b = 8 * (s & 1);
+            const bf16x8 pf = as_bf16x8(u32x4{pack_bf16x2(sc[u][b], sc[u][b + 1]), pack_bf16x2(sc[u][b + 2], sc[u][b + 3]),
+                                              pack_bf16x2(sc[u][b + 4], sc[u][b + 5]), pack_bf16x2(sc[u][b + 6], sc[u][b + 7])});
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+                o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vt[(tt * 8 + 4 * H + s) * 64 + lane]), pf, o[tt], 0, 0, 0);
+        }
+    };
+    if (t_begin < t_end) load(t_begin);
+    for (int i = t_begin; i < t_end; ++i) {
+        if (i > t_begin) __syncthreads();  // every wave is done with the tile before
+        stage();
+        __syncthreads();
+        if (i + 1 < t_end) load(i + 1);
+        const int key0 = i * kTileKeys;
+        if (!active || key0 > wave_last) continue;
+        half_tile(key0, std::integral_constant<int, 0>{});
+        if (key0 + 64 <= wave_last) half_tile(key0 + 64, std::integral_constant<int, 1>{});
+        if (nan_seen[0] | nan_seen[1] | nan_seen[2] | nan_seen[3]) {  // rows that see a group without numbers
+            uint32_t groups = 0;
+            for (int slot = key0; slot <= min(key0 + kTileKeys - 1, lim); ++slot)
+#pragma unroll
+                for (int g = 0; g < SB; ++g)
+                    if (vs[(uint32_t)slot * SB + g] == kKv4Nan) groups |= 1u << g;
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int oct = ((r & 3) + 8 * (r >> 2) + 4 * hf) % NO;
+                    if (groups >> (oct >> 2) & 1) o[tt][r] = NAN;
+                }
+        }
+    }
+    l_i = sum_xor32(l_i);
+    if (!active || c0 + l32 >= cols) return;
+    // register r of tile tt is channel 8 oct + tt PT + (m / NO), m = r % 4 + 8 (r / 4) + 4 hf, oct = m % NO: each octet's eight
+    // channels are in this lane
+    auto channel = [&](int oct_r, int e) -> float {  // oct_r: register that holds channel 0 of the octet (in tile 0)
+        const int tt = e / PT, step = (e % PT) * NO;  // row m + step
+        return o[tt][oct_r + step / 2];
+    };
+    if (sp.splits == 1) {
+        const float inv = 1.0f / l_i;
+        bf16_t *dst = out + (int64_t)(sp.row0 + where.row) * out_stride + where.head * D;
+#pragma unroll
+        for (int r = 0; r < NO / 2; ++r) {
+            const int oct = (r & 3) + 8 * (r >> 2) + 4 * hf;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = channel(r, e) * inv;
+            *reinterpret_cast<u32x4 *>(dst + 8 * oct) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+        }
+        if (lse && hf == 0) lse[(size_t)(sp.row0 + where.row) * view.nq + where.head] = m_i + __builtin_amdgcn_logf(l_i);
+    } else {
+        const size_t pr = (size_t)sp.part0 + ((size_t)z * sp.rows + where.row) * view.nq + where.head;
+        float *dst = part_o + pr * D;
+#pragma unroll
+        for (int r = 0; r < NO / 2; ++r) {
+            const int oct = (r & 3) + 8 * (r >> 2) + 4 * hf;
+#pragma unroll
+            for (int e = 0; e < 8; e += 4)
+                *reinterpret_cast<float4 *>(dst + 8 * oct + e) = make_float4(channel(r, e), channel(r, e + 1), channel(r, e + 2), channel(r, e + 3));
+        }
+        if (hf == 0) *reinterpret_cast<float2 *>(part_ml + pr * 2) = make_float2(m_i, l_i);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Joins the key ranges of a row and head: D / 4 threads, four channels each.  A range whose slots the row does not see has sum 0 and an
+// unused output.
+// ---------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void k_kv4_join(const Kv4Table t, int nq, const float *__restrict__ part_o,
+                                                  const float *__restrict__ part_ml, bf16_t *__restrict__ out, int64_t out_stride,
+                                                  float *__restrict__ lse) {
+    constexpr int TPR = D / 4;
+    const Kv4Span sp = t.s[blockIdx.y];
+    const int unit = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, e = threadIdx.x % TPR;
+    if (sp.splits == 1 || unit >= sp.rows * nq) return;
+    const size_t step = (size_t)sp.rows * nq, pr = (size_t)sp.part0 + unit;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + pr;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o) + pr * TPR + e;
+    float M = -INFINITY;
+    for (int z = 0; z < sp.splits; ++z) M = fmaxf(M, ml[z * step].x);
+    float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+    float L = 0.f;
+#pragma unroll 4
+    for (int z = 0; z < sp.splits; ++z) {
+        const float2 r = ml[z * step];
+        const float4 v = po[z * step * TPR];
+        if (r.y == 0.f) continue;
+        const float w = __builtin_amdgcn_exp2f(r.x - M);
+        L = fmaf(w, r.y, L);
+        A.x = fmaf(w, v.x, A.x), A.y = fmaf(w, v.y, A.y), A.z = fmaf(w, v.z, A.z), A.w = fmaf(w, v.w, A.w);
+    }
+    const float inv = 1.0f / L;
+    const int row = sp.row0 + unit / nq, head = unit % nq;
+    *reinterpret_cast<u32x2 *>(out + (int64_t)row * out_stride + head * D + 4 * e) =
+        u32x2{pack_bf16x2(A.x * inv, A.y * inv), pack_bf16x2(A.z * inv, A.w * inv)};
+    if (lse && e == 0) lse[(size_t)row * nq + head] = M + __builtin_amdgcn_logf(L);
+}
+
+// ---------------------------------------------------------------------------------------
+// The weight each slot received: sum over the columns that see it of exp2(score - lse), the scores formed once more (K only).  A block
+// is 64 slots, its keys in registers as bf16; its waves take every fourth tile of 32 columns.  One block owns a slot's
+// sum: no atomics, the same order in every run.
+// ---------------------------------------------------------------------------------------
+constexpr int kWeightKeys = 64;
+
+template <int D>
+__global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+                                                     int64_t q_stride, const float *__restrict__ lse, float *__restrict__ weights) {
+    constexpr int CB = D / 2, SB = D / 32, ST = D / 16;
+    __shared__ float sums[4][kWeightKeys];
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int l32 = lane & 31, hf = lane >> 5, nkv = view.nkv, G = view.nq / nkv, cols = sp.rows * G;
+    const int kvh = (blockIdx.x - sp.blk0) % nkv, key0 = (blockIdx.x - sp.blk0) / nkv * kWeightKeys;
+    const int last = sp.len + sp.rows - 1;
+    const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
+    const uint8_t *kc = view.k + head0 * CB, *ks = view.ks + head0 * SB;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+    bf16x8 kf[2][ST];  // slot key0 + 32 u + l32, channels hf D / 2 + 8 s
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t slot = min(key0 + 32 * u + l32, last);
+#pragma unroll
+        for (int g = 0; g < D / 64; ++g) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(kc + slot * CB + hf * (CB / 2) + 16 * g);
+            const float unit = kv4_scale(ks[slot * SB + hf * (SB / 2) + g]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) kf[u][4 * g + c] = as_bf16x8(keys8(w[c], unit));
+        }
+    }
+    f32x16 acc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[u][r] = 0.f;
+    const int first = max(0, key0 - sp.len) * G / 32;  // the columns before see none of the block
+    for (int ct = first + wave; ct * 32 < cols; ct += waves) {
+        const int col = min(ct * 32 + l32, cols - 1);
+        const Column where = column_of(col, G, kvh);
+        const int lim = ct * 32 + l32 < cols ? sp.len + where.row : -1;
+        const float base = lse[(size_t)(sp.row0 + where.row) * view.nq + where.head];
+        const bf16_t *src = q + (int64_t)(sp.row0 + where.row) * q_stride + where.head * D + hf * (D / 2);
+        f32x16 sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            const bf16x8 qf = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 8 * s));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][s], qf, sc[u], 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = key0 + 32 * u + (r & 3) + 8 * (r >> 2) + 4 * hf;
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][r], scale, -base));
+                acc[u][r] += key <= lim ? p : 0.f;
+            }
+    }
+    // over the 32 columns of a wave
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float v = acc[u][r];
+            v += dpp_move<0xB1, 0xf>(0.f, v);
+            v += dpp_move<0x4E, 0xf>(0.f, v);
+            v += dpp_move<0x141, 0xf>(0.f, v);
+            v += dpp_move<0x140, 0xf>(0.f, v);
+            v = sum_xor16(v);
+            if (l32 == 0) sums[wave][32 * u + (r & 3) + 8 * (r >> 2) + 4 * hf] = v;
+        }
+    __syncthreads();
+    if (threadIdx.x < kWeightKeys && key0 + (int)threadIdx.x <= last) {
+        float v = sums[0][threadIdx.x];
+        for (int w = 1; w < waves; ++w) v += sums[w][threadIdx.x];
+        weights[head0 + key0 + threadIdx.x] += v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// launcher
+// ---------------------------------------------------------------------------------------
+// Cuts the spans' tiles of `tile` slots into ranges of t.per tiles (a multiple of `step`), so that about `want` blocks come out and the partial results
+// fit; returns the blocks.  blocks_of(span): blocks of one range.
+template <class F>
+static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F blocks_of) {
+    const int64_t nq = k.c.n_q_heads;
+    int64_t work = 0;
+    int most = 1;
+    for (int j = 0; j < t.n; ++j) {
+        if (!t.s[j].rows) continue;
+        const int tiles = (t.s[j].len + t.s[j].rows + tile - 1) / tile;
+        work += (int64_t)blocks_of(t.s[j]) * tiles;
+        most = tiles > most ? tiles : most;
+    }
+    int64_t per = (work + want - 1) / want;
+    per = (per + step - 1) / step * step;
+    for (;; per += step) {
+        int64_t blk = 0, part = 0;
+        for (int j = 0; j < t.n; ++j) {
+            Kv4Span &s = t.s[j];
+            const int tiles = s.rows ? (s.len + s.rows + tile - 1) / tile : 0;
+            s.splits = s.rows ? (int)((tiles + per - 1) / per) : 1;
+            s.blk0 = (int)blk, s.part0 = (int)part;
+            if (s.rows) blk += (int64_t)blocks_of(s) * s.splits;
+            if (s.splits > 1) part += (int64_t)s.splits * s.rows * nq;
+        }
+        if (part <= (int64_t)k.part_rows || per >= most) {
+            t.per = (int)per;
+            return (int)blk;
+        }
+    }
+}
+
+void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf16_t *q, int64_t q_stride, bf16_t *out,
+                       int64_t out_stride, float *weights) {
+    const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv, D = k.c.head_dim;
+    const Kv4View view = k.view(layer);
+    float *lse = weights ? k.lse : nullptr;
+    int most = 0;
+    for (int j = 0; j < t.n; ++j) most = t.s[j].rows > most ? t.s[j].rows : most;
+    const int64_t cols = (int64_t)most * G;
+    if (cols <= 64) {
+        const int blocks = cut_ranges(k, t, kFewTile, kFewWaves, 1024, [&](const Kv4Span &) { return nkv; });
+#define ST_FEW(DV, NTV)                                                                                                    \
+    hipLaunchKernelGGL((k_kv4_few<DV, NTV>), dim3(blocks), dim3(256), 0, k.stream, t, view, q, q_stride, out, out_stride, \
+                       k.part_o, k.part_ml, lse)
+        if (D == 128) {
+            if (cols <= 16) ST_FEW(128, 1);
+            else if (cols <= 32) ST_FEW(128, 2);
+            else ST_FEW(128, 4);
+        } else {
+            if (cols <= 16) ST_FEW(64, 1);
+            else if (cols <= 32) ST_FEW(64, 2);
+            else ST_FEW(64, 4);
+        }
+#undef ST_FEW
+    } else {
+        const int blocks = cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return nkv * ((s.rows * G + kTileCols - 1) / kTileCols); });
+        auto *kern = D == 128 ? k_kv4_chunk<128> : k_kv4_chunk<64>;
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, k.stream, t, view, q, q_stride, out, out_stride, k.part_o, k.part_ml, lse);
+    }
+    int join = 0;  // rows of the longest span in several ranges
+    for (int j = 0; j < t.n; ++j)
+        if (t.s[j].splits > 1 && t.s[j].rows > join) join = t.s[j].rows;
+    if (join) {
+        const int per_block = 256 / (D / 4);
+        auto *kern = D == 128 ? k_kv4_join<128> : k_kv4_join<64>;
+        hipLaunchKernelGGL(kern, dim3((join * k.c.n_q_heads + per_block - 1) / per_block, t.n), dim3(256), 0, k.stream, t,
+                           k.c.n_q_heads, k.part_o, k.part_ml, out, out_stride, lse);
+    }
+    if (weights) {
+        int blk = 0;
+        for (int j = 0; j < t.n; ++j) {
+            t.s[j].blk0 = blk;
+            if (t.s[j].rows) blk += nkv * ((t.s[j].len + t.s[j].rows + kWeightKeys - 1) / kWeightKeys);
+        }
+        auto *kern = D == 128 ? k_kv4_weights<128> : k_kv4_weights<64>;
+        hipLaunchKernelGGL(kern, dim3(blk), dim3(cols <= 32 ? 64 : 256), 0, k.stream, t, view, q, q_stride, lse, weights);
+    }
+}
+
+}  // namespace st
