@@ -573,7 +573,7 @@ class Kv4Cache:
         if not rope.is_cuda or rope.dtype != torch.float32 or not rope.is_contiguous() or \
                 tuple(rope.shape) != (cfg["max_pos"], cfg["head_dim"] // 2, 2):
             raise StError(ST_EINVAL, f"rope is a contiguous float32 CUDA tensor [max_pos][head_dim / 2][2], got {rope.dtype} {tuple(rope.shape)}")
-        dev = rope.device
+        dev = rope.device           # (with its index)
         if cache is None:
             cache = torch.empty(cb.value, dtype=torch.uint8, device=dev)
         elif cache.device != dev or cache.dtype != torch.uint8 or not cache.is_contiguous():
@@ -588,6 +588,9 @@ class Kv4Cache:
         self._h = h
         self._slots = (cfg["n_layers"], cfg["n_seq"], cfg["n_kv_heads"], cfg["max_seq"])
         self._nq, self._nkv, self._d = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"]
+        self._proto = torch.empty(0, dtype=torch.bfloat16, device=dev)
+        L = lib()
+        self._append, self._attend, self._evict, self._read = L.st_kv4_append, L.st_kv4_attend, L.st_kv4_evict, L.st_kv4_read
 
     def close(self):
         if getattr(self, "_h", None):
@@ -600,31 +603,34 @@ class Kv4Cache:
         except Exception:
             pass
 
+    # A decode step makes these calls for every layer, so the checks below stay at a few attribute reads.
     def _alloc(self, *shape):
         if not self._own_stream:
-            return torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+            return self._proto.new_empty(shape)
         with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self._dev)):
-            return torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+            return self._proto.new_empty(shape)
 
     def _enter(self):
-        if not self._own_stream and torch.cuda.current_stream(self._dev).cuda_stream != self.stream:
+        if not self._own_stream and torch._C._cuda_getCurrentRawStream(self._dev.index) != self.stream:
             raise StError(ST_EINVAL, "called under another stream than the cache was made on")
 
     def _matrix(self, name, x, rows, heads):
         """(pointer, row stride) of bf16 [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
-        if x.dtype != torch.bfloat16 or x.device != self._dev:
+        d, shape = self._d, x.shape
+        if x.dtype is not torch.bfloat16 or x.device != self._dev:
             raise StError(ST_EINVAL, f"{name} is bfloat16 on {self._dev}, got {x.dtype} on {x.device}")
-        d, shape, stride = self._d, x.shape, x.stride()
-        if not (len(shape) == 2 and shape[1] == heads * d and stride[1] == 1 or
-                len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1)) or \
-                shape[0] != rows:
+        if x.is_contiguous() and (shape == (rows, heads, d) or shape == (rows, heads * d)):
+            return x.data_ptr(), heads * d
+        stride = x.stride()
+        if not (shape == (rows, heads * d) and stride[1] == 1 or
+                shape == (rows, heads, d) and stride[2] == 1 and (stride[1] == d or heads == 1)):
             raise StError(ST_EINVAL, f"{name} has shape {tuple(shape)} and strides {stride}, needs {rows} rows of {heads} x {d}")
         return x.data_ptr(), stride[0] if rows > 1 else max(stride[0], heads * d)
 
     def _ledger(self, ledger):
         if ledger is None:
             return None
-        if tuple(ledger.weights.shape) != self._slots:
+        if ledger.weights.shape != self._slots:
             raise StError(ST_EINVAL, f"the ledger has shape {tuple(ledger.weights.shape)}, needs {self._slots}")
         if ledger.weights.device != self._dev:
             raise StError(ST_EINVAL, f"the ledger is on {ledger.weights.device}, the cache on {self._dev}")
@@ -635,16 +641,22 @@ class Kv4Cache:
         heads, then key heads, then value heads.  Returns the rotated queries, bf16 [rows][n_q_heads][head_dim]."""
         self._enter()
         p, stride = self._matrix("qkv", qkv, spans.rows, self._nq + 2 * self._nkv)
-        norms = []
-        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-            if w is not None and (w.dtype != torch.bfloat16 or tuple(w.shape) != (self._d,) or not w.is_contiguous() or w.device != self._dev):
-                raise StError(ST_EINVAL, f"{name} is bfloat16 [{self._d}] on {self._dev}, got {w.dtype} {tuple(w.shape)}")
-            norms.append(None if w is None else w.data_ptr())
+        qn = kn = None
+        if q_norm is not None or k_norm is not None:
+            qn, kn = self._norm("q_norm", q_norm), self._norm("k_norm", k_norm)
         out = self._alloc(spans.rows, self._nq, self._d)
         if spans.rows:
-            _check(lib().st_kv4_append(self._h, layer, spans.c, spans.n, p, stride, *norms, out.data_ptr(), self._nq * self._d,
-                                       self._ledger(ledger)))
+            rc = self._append(self._h, layer, spans.c, spans.n, p, stride, qn, kn, out.data_ptr(), self._nq * self._d, self._ledger(ledger))
+            if rc:
+                _check(rc)
         return out
+
+    def _norm(self, name, w):
+        if w is None:
+            return None
+        if w.dtype is not torch.bfloat16 or w.shape != (self._d,) or not w.is_contiguous() or w.device != self._dev:
+            raise StError(ST_EINVAL, f"{name} is bfloat16 [{self._d}] on {self._dev}, got {w.dtype} {tuple(w.shape)}")
+        return w.data_ptr()
 
     def attend(self, layer, spans, q, ledger=None, out=None):
         """Attention of the spans' rows over their sequences' slots; q: bf16, n_q_heads * head_dim a row.  With a ledger its weights grow by what every
@@ -653,20 +665,26 @@ class Kv4Cache:
         p, stride = self._matrix("q", q, spans.rows, self._nq)
         if out is None:
             out = self._alloc(spans.rows, self._nq, self._d)
-        po, so = self._matrix("out", out, spans.rows, self._nq)
+            po, so = out.data_ptr(), self._nq * self._d
+        else:
+            po, so = self._matrix("out", out, spans.rows, self._nq)
         if spans.rows:
-            _check(lib().st_kv4_attend(self._h, layer, spans.c, spans.n, p, stride, po, so, self._ledger(ledger)))
+            rc = self._attend(self._h, layer, spans.c, spans.n, p, stride, po, so, self._ledger(ledger))
+            if rc:
+                _check(rc)
         return out
 
     def evict(self, layer_lo, layer_hi, spans, keep, recent, ledger, into=None):
         """Brings the spans' sequences to `keep` slots in layers [layer_lo, layer_hi) (see st_kv4_evict); the ledger's entries move along, in place or to `into`."""
         self._enter()
-        _check(lib().st_kv4_evict(self._h, layer_lo, layer_hi, spans.c, spans.n, keep, recent, self._ledger(ledger), self._ledger(into)))
+        _check(self._evict(self._h, layer_lo, layer_hi, spans.c, spans.n, keep, recent, self._ledger(ledger), self._ledger(into)))
 
     def read(self, layer_lo, layer_hi, spans):
         """Slots [len, len + rows) of the spans as bf16 (k, v), each [layers][rows][n_kv_heads][head_dim]."""
         self._enter()
-        k, v = (self._alloc(max(layer_hi - layer_lo, 0), spans.rows, self._nkv, self._d) for _ in range(2))
-        if k.numel():
-            _check(lib().st_kv4_read(self._h, layer_lo, layer_hi, spans.c, spans.n, k.data_ptr(), v.data_ptr()))
+        layers = max(layer_hi - layer_lo, 0)
+        k = self._alloc(layers, spans.rows, self._nkv, self._d)
+        v = self._alloc(layers, spans.rows, self._nkv, self._d)
+        if layers and spans.rows:
+            _check(self._read(self._h, layer_lo, layer_hi, spans.c, spans.n, k.data_ptr(), v.data_ptr()))
         return k, v

@@ -14,12 +14,28 @@ struct Kv4Span {
     int32_t splits;               // key ranges its blocks are dealt to
     int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
 };
-// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.
-struct Kv4Table {
+// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Two sizes, as a launch with 2 KB of
+// arguments costs the host more (LAUNCHCOST).
+template <int CAP>
+struct Kv4Spans {
     int32_t n, per;  // spans; key tiles of one range
-    Kv4Span s[ST_KV4_MAX_SPANS];
+    Kv4Span s[CAP];
 };
+constexpr int kKv4Few = 4;
+typedef Kv4Spans<ST_KV4_MAX_SPANS> Kv4Table;
 static_assert(sizeof(Kv4Table) <= 2200, "kernel arguments are at most 4 KB");
+// f(the table in the smallest size that holds it)
+template <class F>
+inline void with_table(const Kv4Table &t, F f) {
+    if (t.n <= kKv4Few) {
+        Kv4Spans<kKv4Few> small;
+        small.n = t.n, small.per = t.per;
+        for (int j = 0; j < kKv4Few; ++j) small.s[j] = j < t.n ? t.s[j] : Kv4Span{};
+        f(small);
+    } else {
+        f(t);
+    }
+}
 
 // The planes of one layer and its heads
 struct Kv4View {
@@ -57,7 +73,14 @@ void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &
 #ifdef __HIPCC__
 // The span whose blocks block `b` belongs to: the last one that starts at or before it (spans without blocks share their
 // start with the next one).  Wave-uniform; all lanes must be active.
-__device__ __forceinline__ int kv4_span_of(const Kv4Table &t, int b) {
+template <int CAP>
+__device__ __forceinline__ int kv4_span_of(const Kv4Spans<CAP> &t, int b) {
+    if constexpr (CAP == kKv4Few) {
+        int j = 0;
+#pragma unroll
+        for (int i = 1; i < CAP; ++i) j = i < t.n && t.s[i].blk0 <= b ? i : j;
+        return j;
+    }
     const int lane = threadIdx.x & 63;
     const bool at_or_before = lane < t.n && t.s[lane].blk0 <= b;
     return __builtin_amdgcn_readfirstlane(63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(at_or_before)));

@@ -44,8 +44,8 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     return (uint32_t)(min(max(s, -100), 125) + 127);
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void k_kv4_append(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ qkv,
+template <int D, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_append(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ qkv,
                                                     int64_t qkv_stride, const bf16_t *__restrict__ q_norm,
                                                     const bf16_t *__restrict__ k_norm, float eps,
                                                     const float *__restrict__ rope, bf16_t *__restrict__ q_out,
@@ -124,8 +124,8 @@ __global__ __launch_bounds__(256) void k_kv4_append(const Kv4Table t, const Kv4V
 // Read: slots [len, len + rows) of every span as the bf16 numbers they stand for (each is one exactly).  A thread turns four bytes of codes into
 // 16 of output.
 // ---------------------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256) void k_kv4_read(const Kv4Table t, Kv4View view, size_t k_layer, size_t s_layer, int rows,
+template <int D, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_read(const Kv4Spans<CAP> t, Kv4View view, size_t k_layer, size_t s_layer, int rows,
                                                   bf16_t *__restrict__ k_out, bf16_t *__restrict__ v_out) {
     constexpr int TPH = D / 8;
     const int row = blockIdx.x, layer = blockIdx.y;
@@ -144,10 +144,9 @@ __global__ __launch_bounds__(256) void k_kv4_read(const Kv4Table t, Kv4View view
     }
 }
 
-static Kv4Table by_rows(const Kv4Table &t) {  // block = row
-    Kv4Table r = t;
-    for (int j = 0; j < r.n; ++j) r.s[j].blk0 = r.s[j].row0;
-    return r;
+template <class T>
+static void by_rows(T &t) {  // block = row
+    for (int j = 0; j < t.n; ++j) t.s[j].blk0 = t.s[j].row0;
 }
 
 void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, const bf16_t *qkv, int64_t qkv_stride,
@@ -155,15 +154,23 @@ void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, con
                        int32_t *positions) {
     const int per_block = 256 / (k.c.head_dim / 8), heads = k.c.n_q_heads + 2 * k.c.n_kv_heads;
     const dim3 grid(rows, (heads + per_block - 1) / per_block);
-    auto *kern = k.c.head_dim == 128 ? k_kv4_append<128> : k_kv4_append<64>;
-    hipLaunchKernelGGL(kern, grid, dim3(256), 0, k.stream, by_rows(t), k.view(layer), qkv, qkv_stride, q_norm, k_norm,
-                       k.c.rms_eps, k.rope, q_out, q_stride, weights, positions);
+    with_table(t, [&](auto tab) {
+        constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
+        auto *kern = k.c.head_dim == 128 ? k_kv4_append<128, CAP> : k_kv4_append<64, CAP>;
+        by_rows(tab);
+        hipLaunchKernelGGL(kern, grid, dim3(256), 0, k.stream, tab, k.view(layer), qkv, qkv_stride, q_norm, k_norm, k.c.rms_eps,
+                           k.rope, q_out, q_stride, weights, positions);
+    });
 }
 
 void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out) {
-    auto *kern = k.c.head_dim == 128 ? k_kv4_read<128> : k_kv4_read<64>;
-    hipLaunchKernelGGL(kern, dim3(rows, layer_hi - layer_lo), dim3(256), 0, k.stream, by_rows(t), k.view(layer_lo), k.per_layer[0],
-                       k.per_layer[2], rows, k_out, v_out);
+    with_table(t, [&](auto tab) {
+        constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
+        auto *kern = k.c.head_dim == 128 ? k_kv4_read<128, CAP> : k_kv4_read<64, CAP>;
+        by_rows(tab);
+        hipLaunchKernelGGL(kern, dim3(rows, layer_hi - layer_lo), dim3(256), 0, k.stream, tab, k.view(layer_lo), k.per_layer[0],
+                           k.per_layer[2], rows, k_out, v_out);
+    });
 }
 
 // ---------------------------------------------------------------------------------------

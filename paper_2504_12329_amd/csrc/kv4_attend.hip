@@ -30,36 +30,21 @@ __device__ __forceinline__ u32x4 keys8(uint32_t w, float unit) {  // eight chann
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// Eight slots x D / 16 (or 8) channels of V as a lane loads them: codes of slot j in c[j] (two or four bytes), scale bytes of the slots'
-// group in b[j]
-template <int NB>  // bytes of codes of a slot: 2 or 4
+// Eight slots of V as a lane loads them: NB bytes of codes (2 NB channels of one scale group) of slot j in c[j], and the scale bytes of
+// all groups, not taken apart until they are used, so that nothing waits for the load where it is issued.
+template <int D, int NB>
 struct Values8 {
-    uint32_t c[8], b[8];
-    // channels 2 B and 2 B + 1 of the eight slots
-    template <int B>
-    __device__ __forceinline__ void pairs(u32x4 &even, u32x4 &odd) const {
-        uint32_t p[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = kv4_pair<B>(c[j], kv4_scale(b[j]));
-        even = u32x4{low_halves(p[0], p[1]), low_halves(p[2], p[3]), low_halves(p[4], p[5]), low_halves(p[6], p[7])};
-        odd = u32x4{high_halves(p[0], p[1]), high_halves(p[2], p[3]), high_halves(p[4], p[5]), high_halves(p[6], p[7])};
-    }
-    __device__ __forceinline__ bool any_nan() const {
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, b[j]);
-        return m == (uint32_t)kKv4Nan;
-    }
-    __device__ __forceinline__ void nan_to_zero() {  // (their codes are zeros)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = b[j] == (uint32_t)kKv4Nan ? 0 : b[j];
+    uint32_t c[8], s[D / 16];
+    // bits of the scale of slot j (byte << 23); shift: 8 * group
+    __device__ __forceinline__ uint32_t unit(int j, int shift) const {
+        const uint32_t w = D == 128 ? s[j] : s[j >> 1] >> 16 * (j & 1);
+        return (w >> shift & 255) << 23;
     }
 };
-// Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each, scale byte `group`.  TAIL: slots past `last` are
-// read as `last` (no address past it is formed).
+// Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each.  TAIL: slots past `last` are read as `last` (no address
+// past it is formed).
 template <int D, int NB, bool TAIL>
-__device__ __forceinline__ void load_values(Values8<NB> &v, const uint8_t *codes, const uint8_t *scales, int key, int last,
-                                            int at, int group) {
+__device__ __forceinline__ void load_values(Values8<D, NB> &v, const uint8_t *codes, const uint8_t *scales, int key, int last, int at) {
     constexpr int CB = D / 2, SB = D / 32;
     auto code = [&](int slot) -> uint32_t {
         const uint8_t *p = codes + (uint32_t)slot * CB + at;
@@ -71,22 +56,52 @@ __device__ __forceinline__ void load_values(Values8<NB> &v, const uint8_t *codes
         for (int j = 0; j < 8; ++j) {
             const int slot = min(key + j, last);
             v.c[j] = code(slot);
-            v.b[j] = scales[(uint32_t)slot * SB + group];
+            if constexpr (SB == 4) {
+                v.s[j] = *reinterpret_cast<const uint32_t *>(scales + (uint32_t)slot * SB);
+            } else {
+                const uint32_t w = *reinterpret_cast<const uint16_t *>(scales + (uint32_t)slot * SB);
+                v.s[j >> 1] = j & 1 ? v.s[j >> 1] | w << 16 : w;
+            }
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v.c[j] = code(key + j);
         const u32x4_a2 *p = reinterpret_cast<const u32x4_a2 *>(scales + (uint32_t)key * SB);
-        if constexpr (SB == 4) {
-            const u32x4 a = p[0], b = p[1];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v.b[j] = a[j] >> (8 * group) & 255, v.b[4 + j] = b[j] >> (8 * group) & 255;
-        } else {
-            const u32x4 a = p[0];
+        for (int h = 0; h < D / 64; ++h) {
+            const u32x4 a = p[h];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v.b[j] = a[j >> 1] >> (16 * (j & 1) + 8 * group) & 255;
+            for (int j = 0; j < 4; ++j) v.s[4 * h + j] = a[j];
         }
     }
+}
+// The scales of eight slots, ready for use.  A NaN's (255 << 23) is an infinity, and infinity times its zero codes a NaN.
+struct Units8 {
+    uint32_t f[8];
+    template <int D, int NB>
+    __device__ __forceinline__ Units8(const Values8<D, NB> &v, int shift) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = v.unit(j, shift);
+    }
+    __device__ __forceinline__ bool any_nan() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, f[j]);
+        return m == (uint32_t)kKv4Nan << 23;
+    }
+    __device__ __forceinline__ void nan_to_zero() {  // (their codes are zeros)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = f[j] == (uint32_t)kKv4Nan << 23 ? 0 : f[j];
+    }
+};
+// channels 2 B and 2 B + 1 of the eight slots, slots in order
+template <int B, int D, int NB>
+__device__ __forceinline__ void value_pairs(const Values8<D, NB> &v, const Units8 &u, u32x4 &even, u32x4 &odd) {
+    uint32_t p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = kv4_pair<B>(v.c[j], __uint_as_float(u.f[j]));
+    even = u32x4{low_halves(p[0], p[1]), low_halves(p[2], p[3]), low_halves(p[4], p[5]), low_halves(p[6], p[7])};
+    odd = u32x4{high_halves(p[0], p[1]), high_halves(p[2], p[3]), high_halves(p[4], p[5]), high_halves(p[6], p[7])};
 }
 
 // Where a column's query is
@@ -107,8 +122,8 @@ __device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Co
 // ---------------------------------------------------------------------------------------
 constexpr int kFewTile = 32, kFewWaves = 4;
 
-template <int D, int NT>
-__global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+template <int D, int NT, int CAP>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                  int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
                                                  float *__restrict__ part_o, float *__restrict__ part_ml,
                                                  float *__restrict__ lse) {
@@ -145,7 +160,7 @@ __global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View
     }
     struct Tile {
         uint32_t k[2][KS], kb[2];
-        Values8<NB> v;
+        Values8<D, NB> v;
     };
     auto load = [&](Tile &x, int tile) {
         const int key0 = tile * kFewTile;
@@ -162,11 +177,11 @@ __global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View
                 x.kb[u] = ks[slot * SB + (qd >> 1)];
             }
         }
-        const int at = m16 * NB, group = m16 * DPL / 32;
+        const int at = m16 * NB;
         if (key0 + kFewTile <= n_keys)
-            load_values<D, NB, false>(x.v, vc, vs, key0 + 8 * qd, last, at, group);
+            load_values<D, NB, false>(x.v, vc, vs, key0 + 8 * qd, last, at);
         else
-            load_values<D, NB, true>(x.v, vc, vs, key0 + 8 * qd, last, at, group);
+            load_values<D, NB, true>(x.v, vc, vs, key0 + 8 * qd, last, at);
     };
     auto work = [&](Tile &x, int tile) {
         const int key0 = tile * kFewTile;
@@ -181,6 +196,7 @@ __global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View
 #pragma unroll
                 for (int c = 0; c < NT; ++c) sc[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][s], sc[c][u], 0, 0, 0);
             }
+        Units8 unit(x.v, 8 * (m16 * DPL / 32));
         const bool part = key0 + kFewTile - 1 > sp.len;  // some row does not see all of the tile
         uint32_t poison = 0;                              // columns (bit c) that see a NaN among this lane's output channels
         if (part) {
@@ -191,8 +207,8 @@ __global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (key0 + 8 * qd + 4 * u + r > lim[c]) sc[c][u][r] = -INFINITY;
-            if (__builtin_amdgcn_ballot_w64(x.v.any_nan())) {
-                x.v.nan_to_zero();
+            if (__builtin_amdgcn_ballot_w64(unit.any_nan())) {
+                unit.nan_to_zero();
                 for (int slot = key0; slot < min(key0 + kFewTile, n_keys); ++slot)
                     if (vs[(uint32_t)slot * SB + qd * SB / 4] == kKv4Nan)
 #pragma unroll
@@ -233,7 +249,7 @@ __global__ __launch_bounds__(256) void k_kv4_few(const Kv4Table t, const Kv4View
         auto multiply = [&](auto b_c) {
             constexpr int B = decltype(b_c)::value;
             u32x4 even, odd;
-            x.v.template pairs<B>(even, odd);
+            value_pairs<B>(x.v, unit, even, odd);
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 o[c][2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(even), pf[c], o[c][2 * B], 0, 0, 0);
@@ -331,8 +347,8 @@ constexpr int kTileKeys = 128, kTileCols = 128;
 
 __device__ __forceinline__ int swap23(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+template <int D, int CAP>
+__global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                       int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
                                                       float *__restrict__ part_o, float *__restrict__ part_ml,
                                                       float *__restrict__ lse) {
@@ -376,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv
     const bool has_v = v_kb < 16;
     u32x4 kw[KG];
     uint32_t kb[KG];
-    Values8<4> vw;
+    Values8<D, 4> vw;
     auto load = [&](int tile) {
         const int key0 = tile * kTileKeys;
         const uint32_t slot = min(key0 + k_slot, last);
@@ -387,21 +403,22 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv
         }
         if (!has_v) return;
         if (key0 + kTileKeys <= n_keys)
-            load_values<D, 4, false>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct, v_oct >> 2);
+            load_values<D, 4, false>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct);
         else
-            load_values<D, 4, true>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct, v_oct >> 2);
+            load_values<D, 4, true>(vw, vc, vs, key0 + 8 * v_kb, last, 4 * v_oct);
     };
     auto stage = [&]() {
         const int u = k_slot >> 5, m = swap23(k_slot & 31);
 #pragma unroll
         for (int e = 0; e < KG; ++e) {
-            const float unit = kv4_scale(kb[e]);
+            const float k_unit = kv4_scale(kb[e]);
 #pragma unroll
             for (int c = 0; c < 4; ++c)  // channels 32 group + 8 c
-                kt[(u * ST + 2 * (k_group + 2 * e) + (c >> 1)) * 64 + (c & 1) * 32 + m] = keys8(kw[e][c], unit);
+                kt[(u * ST + 2 * (k_group + 2 * e) + (c >> 1)) * 64 + (c & 1) * 32 + m] = keys8(kw[e][c], k_unit);
         }
-        const bool bad = has_v && vw.any_nan();
-        if (bad) vw.nan_to_zero();
+        Units8 unit(vw, 8 * (v_oct >> 2));
+        const bool bad = has_v && unit.any_nan();
+        if (bad) unit.nan_to_zero();
         const uint64_t any = __builtin_amdgcn_ballot_w64(bad);
         if (lane == 0) nan_seen[wave] = any != 0;
         if (!has_v) return;
@@ -409,7 +426,7 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv
         auto put = [&](auto b_c) {
             constexpr int B = decltype(b_c)::value;
             u32x4 even, odd;
-            vw.template pairs<B>(even, odd);
+            value_pairs<B>(vw, unit, even, odd);
             dst[(2 * B) / PT * 512 + NO * ((2 * B) % PT)] = even;
             dst[(2 * B + 1) / PT * 512 + NO * ((2 * B + 1) % PT)] = odd;
         };
@@ -534,33 +551,52 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Table t, const Kv
 }
 
 // ---------------------------------------------------------------------------------------
-// Joins the key ranges of a row and head: D / 4 threads, four channels each.  A range whose slots the row does not see has sum 0 and an
-// unused output.
+// Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them are fetched at
+// once; then D / 4 lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range whose
+// slots the row does not see has sum 0 and an unused output.
 // ---------------------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256) void k_kv4_join(const Kv4Table t, int nq, const float *__restrict__ part_o,
-                                                  const float *__restrict__ part_ml, bf16_t *__restrict__ out, int64_t out_stride,
-                                                  float *__restrict__ lse) {
-    constexpr int TPR = D / 4;
-    const Kv4Span sp = t.s[blockIdx.y];
-    const int unit = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, e = threadIdx.x % TPR;
-    if (sp.splits == 1 || unit >= sp.rows * nq) return;
+constexpr int kMostRanges = 64;
+
+template <int D, int WPU>
+__device__ __forceinline__ void join_unit(const Kv4Span &sp, int unit, bool live, int nq, const float *__restrict__ part_o,
+                                          const float *__restrict__ part_ml, bf16_t *__restrict__ out, int64_t out_stride,
+                                          float *__restrict__ lse, float4 *red) {
+    constexpr int TPR = D / 4, PAR = 64 * WPU / TPR, kBatch = 8;  // PAR ranges at a time
+    const int lane = threadIdx.x & 63, tid = threadIdx.x & (64 * WPU - 1), e = tid % TPR, g = tid / TPR;
     const size_t step = (size_t)sp.rows * nq, pr = (size_t)sp.part0 + unit;
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + pr;
+    const float2 ml = live && lane < sp.splits ? reinterpret_cast<const float2 *>(part_ml)[pr + lane * step] : make_float2(-INFINITY, 0.f);
     const float4 *po = reinterpret_cast<const float4 *>(part_o) + pr * TPR + e;
-    float M = -INFINITY;
-    for (int z = 0; z < sp.splits; ++z) M = fmaxf(M, ml[z * step].x);
+    float4 v[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) v[u] = live && g + u * PAR < sp.splits ? po[(g + u * PAR) * step * TPR] : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float M = wave_max(ml.x);
+    const float w = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float L = wave_sum(w == 0.f && ml.y == ml.y ? 0.f : w * ml.y);
     float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f;
-#pragma unroll 4
-    for (int z = 0; z < sp.splits; ++z) {
-        const float2 r = ml[z * step];
-        const float4 v = po[z * step * TPR];
-        if (r.y == 0.f) continue;
-        const float w = __builtin_amdgcn_exp2f(r.x - M);
-        L = fmaf(w, r.y, L);
-        A.x = fmaf(w, v.x, A.x), A.y = fmaf(w, v.y, A.y), A.z = fmaf(w, v.z, A.z), A.w = fmaf(w, v.w, A.w);
+    for (int z0 = g; z0 - g < sp.splits; z0 += kBatch * PAR) {
+        if (z0 != g)
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) v[u] = live && z0 + u * PAR < sp.splits ? po[(z0 + u * PAR) * step * TPR] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int z = z0 + u * PAR;
+            const float wz = __shfl(w, z & 63, kWave), lz = __shfl(ml.y, z & 63, kWave);
+            if (z < sp.splits && lz != 0.f)
+                A.x = fmaf(wz, v[u].x, A.x), A.y = fmaf(wz, v[u].y, A.y), A.z = fmaf(wz, v[u].z, A.z), A.w = fmaf(wz, v[u].w, A.w);
+        }
     }
+    // the PAR sums, in order
+    if (PAR > 1) {
+        if (g) red[(g - 1) * TPR + e] = A;
+        __syncthreads();
+        if (g == 0)
+#pragma unroll
+            for (int i = 1; i < PAR; ++i) {
+                const float4 x = red[(i - 1) * TPR + e];
+                A.x += x.x, A.y += x.y, A.z += x.z, A.w += x.w;
+            }
+    }
+    if (!live || g) return;
     const float inv = 1.0f / L;
     const int row = sp.row0 + unit / nq, head = unit % nq;
     *reinterpret_cast<u32x2 *>(out + (int64_t)row * out_stride + head * D + 4 * e) =
@@ -568,20 +604,153 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Table t, int nq, cons
     if (lse && e == 0) lse[(size_t)row * nq + head] = M + __builtin_amdgcn_logf(L);
 }
 
+template <int D, int WPU, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_join(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o,
+                                                  const float *__restrict__ part_ml, bf16_t *__restrict__ out, int64_t out_stride,
+                                                  float *__restrict__ lse) {
+    constexpr int UPB = 4 / WPU, RED = (64 * WPU / (D / 4) - 1) * (D / 4);
+    __shared__ float4 red[UPB][RED];
+    const Kv4Span sp = t.s[blockIdx.y];
+    if (sp.splits == 1 || (int)blockIdx.x * UPB >= sp.rows * nq) return;
+    const int unit = blockIdx.x * UPB + threadIdx.x / (64 * WPU);
+    join_unit<D, WPU>(sp, unit, unit < sp.rows * nq, nq, part_o, part_ml, out, out_stride, lse, red[threadIdx.x / (64 * WPU)]);
+}
+
 // ---------------------------------------------------------------------------------------
-// The weight each slot received: sum over the columns that see it of exp2(score - lse), the scores formed once more (K only).  A block
+// Few columns: the weight each slot received, and the ranges' join beside it in the same launch.  Scores are formed once more, from the keys (half of
+// what the first kernel read, and mostly still in the last-level cache), as S = Q K^T: a lane then has one slot and four columns of
+// each tile of 16, and the sum over the columns is three additions and two exchanges.  One lane owns a slot's sum: no atomics.
+// A block works on the range of slots that the same block of k_kv4_few had; blocks past those join one unit each.
+// ---------------------------------------------------------------------------------------
+template <int D, int NT, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
+                                                         int64_t q_stride, const float *__restrict__ part_o,
+                                                         const float *__restrict__ part_ml, const float *__restrict__ lse,
+                                                         int blocks, int join_rows, bf16_t *__restrict__ out, int64_t out_stride,
+                                                         float *__restrict__ weights) {
+    constexpr int KS = D / 32, CB = D / 2, SB = D / 32;
+    __shared__ float4 red[(256 / (D / 4) - 1) * (D / 4)];
+    __shared__ float base_s[NT * 16];
+    if ((int)blockIdx.x >= blocks) {
+        const int x = blockIdx.x - blocks, per_span = join_rows * view.nq;
+        const Kv4Span sp = t.s[x / per_span];
+        const int unit = x % per_span;
+        if (sp.splits == 1 || unit >= sp.rows * view.nq) return;
+        join_unit<D, 4>(sp, unit, true, view.nq, part_o, part_ml, out, out_stride, nullptr, red);
+        return;
+    }
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m16 = lane & 15, qd = lane >> 4, nkv = view.nkv, G = view.nq / nkv;
+    const int kvh = (blockIdx.x - sp.blk0) % nkv, z = (blockIdx.x - sp.blk0) / nkv;
+    const int n_keys = sp.len + sp.rows, last = n_keys - 1, n_tiles = (n_keys + kFewTile - 1) / kFewTile;
+    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
+    const uint8_t *kc = view.k + head0 * CB, *ks = view.ks + head0 * SB;
+    const int cols = sp.rows * G;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+    bf16x8 qf[NT][KS];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const Column w = column_of(min(16 * c + m16, cols - 1), G, kvh);
+        const bf16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * (D / 4);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[c][s] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 8 * s));
+    }
+    // log2 of the columns' softmax sums: wave c makes those of tile c, four lanes a column
+    if (wave < NT) {
+        const int col = min(16 * wave + m16, cols - 1);
+        const Column w = column_of(col, G, kvh);
+        float b;
+        if (sp.splits == 1) {
+            b = lse[(size_t)(sp.row0 + w.row) * view.nq + w.head];
+        } else {
+            const size_t step = (size_t)sp.rows * view.nq;
+            const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)sp.part0 + (size_t)w.row * view.nq + w.head;
+            float2 r[kMostRanges / 4];
+#pragma unroll
+            for (int i = 0; i < kMostRanges / 4; ++i) r[i] = 4 * i + qd < sp.splits ? ml[(4 * i + qd) * step] : make_float2(-INFINITY, 0.f);
+            float M = -INFINITY, L = 0.f, x, y;
+#pragma unroll
+            for (int i = 0; i < kMostRanges / 4; ++i) M = fmaxf(M, r[i].x);
+            with_xor16(M, x, y);
+            M = max_xor32(fmaxf(x, y));
+#pragma unroll
+            for (int i = 0; i < kMostRanges / 4; ++i)
+                if (r[i].y != 0.f) L = fmaf(__builtin_amdgcn_exp2f(r[i].x - M), r[i].y, L);
+            L = sum_xor32(sum_xor16(L));
+            b = M + __builtin_amdgcn_logf(L);
+        }
+        if (qd == 0) base_s[16 * wave + m16] = b;
+    }
+    __syncthreads();
+    float base[NT][4];
+    int lim[NT][4];
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int col = 16 * c + 4 * qd + r;
+            base[c][r] = base_s[col], lim[c][r] = col < cols ? sp.len + col / G : -1;
+        }
+    float *dst = weights + head0;
+    for (int tile = t_begin + wave; tile < t_end; tile += kFewWaves) {
+        const int key0 = tile * kFewTile;
+        const int key = key0 + 16 * (qd & 1) + m16;  // the slot whose sum lanes of quarters 0 and 1 write
+        float was = 0.f;
+        if (qd < 2 && key < n_keys) was = dst[key];
+        float sum[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t slot = min(key0 + 16 * u + m16, last);
+            f32x4 sc[NT];
+#pragma unroll
+            for (int c = 0; c < NT; ++c) sc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            uint32_t w[KS];
+            float unit;
+            if constexpr (D == 128) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(kc + slot * CB + qd * 16);
+                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+                unit = kv4_scale(ks[slot * SB + qd]);
+            } else {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(kc + slot * CB + qd * 8);
+                w[0] = x.x, w[1] = x.y;
+                unit = kv4_scale(ks[slot * SB + (qd >> 1)]);
+            }
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 kf = as_bf16x8(keys8(w[s], unit));
+#pragma unroll
+                for (int c = 0; c < NT; ++c) sc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[c][s], kf, sc[c], 0, 0, 0);
+            }
+            sum[u] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[c][r], scale, -base[c][r]));
+                    sum[u] += key0 + 16 * u + m16 <= lim[c][r] ? p : 0.f;
+                }
+            sum[u] = sum_xor32(sum_xor16(sum[u]));
+        }
+        if (qd < 2 && key < n_keys) dst[key] = was + (qd ? sum[1] : sum[0]);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Chunks: the weight each slot received, sum over the columns that see it of exp2(score - lse), the scores formed once more (K only).  A block
 // is 64 slots, its keys in registers as bf16; its waves take every fourth tile of 32 columns.  One block owns a slot's
 // sum: no atomics, the same order in every run.
 // ---------------------------------------------------------------------------------------
 constexpr int kWeightKeys = 64;
 
-template <int D>
-__global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Table t, const Kv4View view, const bf16_t *__restrict__ q,
+template <int D, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                      int64_t q_stride, const float *__restrict__ lse, float *__restrict__ weights) {
     constexpr int CB = D / 2, SB = D / 32, ST = D / 16;
     __shared__ float sums[4][kWeightKeys];
     const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, hf = lane >> 5, nkv = view.nkv, G = view.nq / nkv, cols = sp.rows * G;
     const int kvh = (blockIdx.x - sp.blk0) % nkv, key0 = (blockIdx.x - sp.blk0) / nkv * kWeightKeys;
     const int last = sp.len + sp.rows - 1;
@@ -606,7 +775,7 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Table t, const Kv4
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[u][r] = 0.f;
     const int first = max(0, key0 - sp.len) * G / 32;  // the columns before see none of the block
-    for (int ct = first + wave; ct * 32 < cols; ct += waves) {
+    for (int ct = first + wave; ct * 32 < cols; ct += 4) {
         const int col = min(ct * 32 + l32, cols - 1);
         const Column where = column_of(col, G, kvh);
         const int lim = ct * 32 + l32 < cols ? sp.len + where.row : -1;
@@ -647,8 +816,7 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Table t, const Kv4
         }
     __syncthreads();
     if (threadIdx.x < kWeightKeys && key0 + (int)threadIdx.x <= last) {
-        float v = sums[0][threadIdx.x];
-        for (int w = 1; w < waves; ++w) v += sums[w][threadIdx.x];
+        const float v = sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x];
         weights[head0 + key0 + threadIdx.x] += v;
     }
 }
@@ -656,8 +824,8 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Table t, const Kv4
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-// Cuts the spans' tiles of `tile` slots into ranges of t.per tiles (a multiple of `step`), so that about `want` blocks come out and the partial results
-// fit; returns the blocks.  blocks_of(span): blocks of one range.
+// Cuts the spans' tiles of `tile` slots into ranges of t.per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kMostRanges
+// ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.
 template <class F>
 static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F blocks_of) {
     const int64_t nq = k.c.n_q_heads;
@@ -669,9 +837,9 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
         work += (int64_t)blocks_of(t.s[j]) * tiles;
         most = tiles > most ? tiles : most;
     }
-    int64_t per = (work + want - 1) / want;
-    per = (per + step - 1) / step * step;
-    for (;; per += step) {
+    const int64_t least = (most + kMostRanges - 1) / kMostRanges, even = work / want;
+    int64_t per = ((even > least ? even : least) + step - 1) / step * step;
+    for (per = per ? per : step;; per += step) {
         int64_t blk = 0, part = 0;
         for (int j = 0; j < t.n; ++j) {
             Kv4Span &s = t.s[j];
@@ -681,7 +849,7 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
             if (s.rows) blk += (int64_t)blocks_of(s) * s.splits;
             if (s.splits > 1) part += (int64_t)s.splits * s.rows * nq;
         }
-        if (part <= (int64_t)k.part_rows || per >= most) {
+        if ((blk <= want && part <= (int64_t)k.part_rows) || per >= most) {
             t.per = (int)per;
             return (int)blk;
         }
@@ -696,44 +864,53 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf1
     int most = 0;
     for (int j = 0; j < t.n; ++j) most = t.s[j].rows > most ? t.s[j].rows : most;
     const int64_t cols = (int64_t)most * G;
-    if (cols <= 64) {
-        const int blocks = cut_ranges(k, t, kFewTile, kFewWaves, 1024, [&](const Kv4Span &) { return nkv; });
-#define ST_FEW(DV, NTV)                                                                                                    \
-    hipLaunchKernelGGL((k_kv4_few<DV, NTV>), dim3(blocks), dim3(256), 0, k.stream, t, view, q, q_stride, out, out_stride, \
-                       k.part_o, k.part_ml, lse)
-        if (D == 128) {
-            if (cols <= 16) ST_FEW(128, 1);
-            else if (cols <= 32) ST_FEW(128, 2);
-            else ST_FEW(128, 4);
-        } else {
-            if (cols <= 16) ST_FEW(64, 1);
-            else if (cols <= 32) ST_FEW(64, 2);
-            else ST_FEW(64, 4);
-        }
-#undef ST_FEW
-    } else {
-        const int blocks = cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return nkv * ((s.rows * G + kTileCols - 1) / kTileCols); });
-        auto *kern = D == 128 ? k_kv4_chunk<128> : k_kv4_chunk<64>;
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, k.stream, t, view, q, q_stride, out, out_stride, k.part_o, k.part_ml, lse);
-    }
+    const bool few = cols <= 64;
+    const int blocks = few ? cut_ranges(k, t, kFewTile, kFewWaves, 768, [&](const Kv4Span &) { return nkv; })
+                           : cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return nkv * ((s.rows * G + kTileCols - 1) / kTileCols); });
     int join = 0;  // rows of the longest span in several ranges
     for (int j = 0; j < t.n; ++j)
         if (t.s[j].splits > 1 && t.s[j].rows > join) join = t.s[j].rows;
-    if (join) {
-        const int per_block = 256 / (D / 4);
-        auto *kern = D == 128 ? k_kv4_join<128> : k_kv4_join<64>;
-        hipLaunchKernelGGL(kern, dim3((join * k.c.n_q_heads + per_block - 1) / per_block, t.n), dim3(256), 0, k.stream, t,
-                           k.c.n_q_heads, k.part_o, k.part_ml, out, out_stride, lse);
-    }
-    if (weights) {
-        int blk = 0;
-        for (int j = 0; j < t.n; ++j) {
-            t.s[j].blk0 = blk;
-            if (t.s[j].rows) blk += nkv * ((t.s[j].len + t.s[j].rows + kWeightKeys - 1) / kWeightKeys);
+    with_table(t, [&](auto tab) {
+        constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
+        const int nq = k.c.n_q_heads, units = join * nq;
+#define ST_FEW(DV, NTV)                                                                                                          \
+    do {                                                                                                                         \
+        hipLaunchKernelGGL((k_kv4_few<DV, NTV, CAP>), dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out,         \
+                           out_stride, k.part_o, k.part_ml, lse);                                                                \
+        if (weights)                                                                                                             \
+            hipLaunchKernelGGL((k_kv4_few_weights<DV, NTV, CAP>), dim3(blocks + units * t.n), dim3(256), 0, k.stream, tab, view, \
+                               q, q_stride, k.part_o, k.part_ml, lse, blocks, join, out, out_stride, weights);                   \
+    } while (0)
+        if (few && D == 128) {
+            if (cols <= 16) ST_FEW(128, 1);
+            else if (cols <= 32) ST_FEW(128, 2);
+            else ST_FEW(128, 4);
+        } else if (few) {
+            if (cols <= 16) ST_FEW(64, 1);
+            else if (cols <= 32) ST_FEW(64, 2);
+            else ST_FEW(64, 4);
+        } else {
+            auto *kern = D == 128 ? k_kv4_chunk<128, CAP> : k_kv4_chunk<64, CAP>;
+            hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out, out_stride, k.part_o, k.part_ml, lse);
         }
-        auto *kern = D == 128 ? k_kv4_weights<128> : k_kv4_weights<64>;
-        hipLaunchKernelGGL(kern, dim3(blk), dim3(cols <= 32 ? 64 : 256), 0, k.stream, t, view, q, q_stride, lse, weights);
-    }
+#undef ST_FEW
+        if (join && !(few && weights)) {
+            // four waves a unit while there are fewer units than would fill the chip with one each
+            const bool wide = units * t.n < 1024;
+            auto *kern = D == 128 ? (wide ? k_kv4_join<128, 4, CAP> : k_kv4_join<128, 1, CAP>) : (wide ? k_kv4_join<64, 4, CAP> : k_kv4_join<64, 1, CAP>);
+            hipLaunchKernelGGL(kern, dim3(wide ? units : (units + 3) / 4, t.n), dim3(256), 0, k.stream, tab, nq, k.part_o, k.part_ml,
+                               out, out_stride, lse);
+        }
+        if (weights && !few) {
+            int blk = 0;
+            for (int j = 0; j < tab.n; ++j) {
+                tab.s[j].blk0 = blk;
+                if (tab.s[j].rows) blk += nkv * ((tab.s[j].len + tab.s[j].rows + kWeightKeys - 1) / kWeightKeys);
+            }
+            auto *kern = D == 128 ? k_kv4_weights<128, CAP> : k_kv4_weights<64, CAP>;
+            hipLaunchKernelGGL(kern, dim3(blk), dim3(256), 0, k.stream, tab, view, q, q_stride, lse, weights);
+        }
+    });
 }
 
 }  // namespace st
