@@ -12,24 +12,25 @@ struct Kv4Span {
     int32_t row0;                 // its first row among the call's rows
     int32_t blk0;                 // its first block in the launch
     int32_t splits;               // key ranges its blocks are dealt to
+    int32_t per;                  // tiles of slots in a range
     int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
 };
 // Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Two sizes, as a launch with 2 KB of
 // arguments costs the host more (LAUNCHCOST).
 template <int CAP>
 struct Kv4Spans {
-    int32_t n, per;  // spans; key tiles of one range
+    int32_t n;
     Kv4Span s[CAP];
 };
 constexpr int kKv4Few = 4;
 typedef Kv4Spans<ST_KV4_MAX_SPANS> Kv4Table;
-static_assert(sizeof(Kv4Table) <= 2200, "kernel arguments are at most 4 KB");
+static_assert(sizeof(Kv4Table) <= 2400, "kernel arguments are at most 4 KB");
 // f(the table in the smallest size that holds it)
 template <class F>
 inline void with_table(const Kv4Table &t, F f) {
     if (t.n <= kKv4Few) {
         Kv4Spans<kKv4Few> small;
-        small.n = t.n, small.per = t.per;
+        small.n = t.n;
         for (int j = 0; j < kKv4Few; ++j) small.s[j] = j < t.n ? t.s[j] : Kv4Span{};
         f(small);
     } else {

@@ -238,11 +238,11 @@ static int take_spans(const Kv4 &k, const st_kv4_span *spans, int32_t n, bool po
             return fail(ST_ERANGE, "span %d: positions from %d, %d rows, table of %d", j, s.pos, s.rows, c.max_pos);
         for (int i = 0; i < j; ++i)
             if (spans[i].seq == s.seq) return fail(ST_EINVAL, "spans %d and %d are both sequence %d", i, j, s.seq);
-        t->s[j] = Kv4Span{s.seq, s.len, s.pos, s.rows, (int32_t)total, 0, 1, 0};
+        t->s[j] = Kv4Span{s.seq, s.len, s.pos, s.rows, (int32_t)total, 0, 1, 0, 0};
         total += s.rows;
         if (total > INT32_MAX / 2) return fail(ST_ERANGE, "too many rows");
     }
-    t->n = n, t->per = 0;
+    t->n = n;
     *rows = (int)total;
     return ST_OK;
 }

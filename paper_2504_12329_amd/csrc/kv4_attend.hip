@@ -49,7 +49,8 @@ __device__ __forceinline__ void load_values(Values8<D, NB> &v, const uint8_t *co
     auto code = [&](int slot) -> uint32_t {
         const uint8_t *p = codes + (uint32_t)slot * CB + at;
         if constexpr (NB == 4) return *reinterpret_cast<const uint32_t *>(p);
-        return *reinterpret_cast<const uint16_t *>(p);
+        if constexpr (NB == 2) return *reinterpret_cast<const uint16_t *>(p);
+        return *p;
     };
     if constexpr (TAIL) {
 #pragma unroll
@@ -89,9 +90,9 @@ struct Units8 {
         for (int j = 0; j < 8; ++j) m = max(m, f[j]);
         return m == (uint32_t)kKv4Nan << 23;
     }
-    __device__ __forceinline__ void nan_to_zero() {  // (their codes are zeros)
+    __device__ __forceinline__ void nan_to_zero() {  // (their codes are zeros: any finite scale does)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = f[j] == (uint32_t)kKv4Nan << 23 ? 0 : f[j];
+        for (int j = 0; j < 8; ++j) f[j] = min(f[j], 0x7f000000u);
     }
 };
 // channels 2 B and 2 B + 1 of the eight slots, slots in order
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(
     const int nkv = view.nkv, G = view.nq / nkv;
     const int kvh = (blockIdx.x - sp.blk0) % nkv, z = (blockIdx.x - sp.blk0) / nkv;
     const int n_keys = sp.len + sp.rows, last = n_keys - 1, n_tiles = (n_keys + kFewTile - 1) / kFewTile;
-    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
     const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
     const uint8_t *kc = view.k + head0 * CB, *vc = view.v + head0 * CB, *ks = view.ks + head0 * SB, *vs = view.vs + head0 * SB;
     const int cols = sp.rows * G;
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Spans<CAP> t, con
     const int wave_first = sp.len + min(c0, cols - 1) / G, wave_last = sp.len + min(c0 + 31, cols - 1) / G;
     const int n_keys = sp.len + min(cb * kTileCols + kTileCols - 1, cols - 1) / G + 1, last = n_keys - 1;
     const int n_tiles = (n_keys + kTileKeys - 1) / kTileKeys;
-    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
     const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
     const uint8_t *kc = view.k + head0 * CB, *vc = view.v + head0 * CB, *ks = view.ks + head0 * SB, *vs = view.vs + head0 * SB;
     const float scale = 1.4426950408889634f / sqrtf((float)D);
@@ -644,7 +645,7 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
     const int m16 = lane & 15, qd = lane >> 4, nkv = view.nkv, G = view.nq / nkv;
     const int kvh = (blockIdx.x - sp.blk0) % nkv, z = (blockIdx.x - sp.blk0) / nkv;
     const int n_keys = sp.len + sp.rows, last = n_keys - 1, n_tiles = (n_keys + kFewTile - 1) / kFewTile;
-    const int t_begin = z * t.per, t_end = min(n_tiles, t_begin + t.per);
+    const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
     const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
     const uint8_t *kc = view.k + head0 * CB, *ks = view.ks + head0 * SB;
     const int cols = sp.rows * G;
@@ -824,7 +825,7 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Spans<CAP> t, cons
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-// Cuts the spans' tiles of `tile` slots into ranges of t.per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kMostRanges
+// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kMostRanges
 // ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.
 template <class F>
 static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F blocks_of) {
@@ -845,14 +846,11 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
             Kv4Span &s = t.s[j];
             const int tiles = s.rows ? (s.len + s.rows + tile - 1) / tile : 0;
             s.splits = s.rows ? (int)((tiles + per - 1) / per) : 1;
-            s.blk0 = (int)blk, s.part0 = (int)part;
+            s.blk0 = (int)blk, s.part0 = (int)part, s.per = (int)per;
             if (s.rows) blk += (int64_t)blocks_of(s) * s.splits;
             if (s.splits > 1) part += (int64_t)s.splits * s.rows * nq;
         }
-        if ((blk <= want && part <= (int64_t)k.part_rows) || per >= most) {
-            t.per = (int)per;
-            return (int)blk;
-        }
+        if ((blk <= want && part <= (int64_t)k.part_rows) || per >= most) return (int)blk;
     }
 }
 
@@ -901,16 +899,19 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf1
             hipLaunchKernelGGL(kern, dim3(wide ? units : (units + 3) / 4, t.n), dim3(256), 0, k.stream, tab, nq, k.part_o, k.part_ml,
                                out, out_stride, lse);
         }
-        if (weights && !few) {
-            int blk = 0;
-            for (int j = 0; j < tab.n; ++j) {
-                tab.s[j].blk0 = blk;
-                if (tab.s[j].rows) blk += nkv * ((tab.s[j].len + tab.s[j].rows + kWeightKeys - 1) / kWeightKeys);
-            }
+    });
+    if (weights && !few) {
+        int blk = 0;
+        for (int j = 0; j < t.n; ++j) {
+            t.s[j].blk0 = blk;
+            if (t.s[j].rows) blk += nkv * ((t.s[j].len + t.s[j].rows + kWeightKeys - 1) / kWeightKeys);
+        }
+        with_table(t, [&](auto tab) {
+            constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
             auto *kern = D == 128 ? k_kv4_weights<128, CAP> : k_kv4_weights<64, CAP>;
             hipLaunchKernelGGL(kern, dim3(blk), dim3(256), 0, k.stream, tab, view, q, q_stride, lse, weights);
-        }
-    });
+        });
+    }
 }
 
 }  // namespace st

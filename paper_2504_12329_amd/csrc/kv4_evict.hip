@@ -5,25 +5,27 @@
 // are freed take, in ascending order, the slots at or above it that stay, in ascending order.  A context brought back
 // from keep + m to keep slots moves at most m of them, in place, and no slot is both read and written.
 //
-//   k_kv4_evict  one block per head: the keep-th largest weight by up to three digits of 11 bits (histograms in LDS), among ties the positions likewise;
-//                a bit per slot, and the moves.  Bound by latency: weights and positions are read once, into registers up to 32768 slots
-//                (beyond, once per digit).
-//   k_kv4_move   where few heads move many slots: the moves, by several blocks per head.
+// A slot's rank is that of 64 bits: its class and weight (32 bits, larger first), then its position (lower first).  k_kv4_evict, one block per
+// head, finds the keep-th by histograms of 11-bit digits in LDS until at most 128 slots share the digits so far, and ranks those
+// against each other; it writes a bit per slot and moves.  Bound by latency: weights and positions are read once, the 32 bits kept in
+// LDS (up to 24576 slots; beyond, they are read again for every digit).  k_kv4_move: where few heads move many slots, the moves by several blocks
+// per head.
+#include <mutex>
+
 #include "kv4.h"
 #include "st_device.h"
 
 namespace st {
 
-constexpr int kSelThreads = 1024, kBins = 2048, kCopies = 4;
-constexpr int kBitWords = 2048;  // bits of 131072 slots fit LDS; those of longer contexts go to the workspace
+constexpr int kBins = 2048, kDirect = 128;
+constexpr int kHeldSlots = 24576, kBitSlots = 131072;  // LDS: 4 bytes a slot, or a bit a slot (those of longer contexts go to the workspace)
 
-// Order-preserving image of a weight: NaN below everything, -0 as 0
-__device__ __forceinline__ uint32_t weight_key(float w) {
+// 32 bits that order slots: those that stay without being asked first (0), then by weight, larger first; -0 is 0, NaN is last
+__device__ __forceinline__ uint32_t order_of(float w, bool fixed) {
     const uint32_t b = __float_as_uint(w + 0.0f);
-    return w != w ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+    return fixed ? 0u : w != w ? 0xffffffffu : (b & 0x80000000u) ? b : ~(b | 0x80000000u);
 }
-constexpr uint32_t kFixedKey = 0xffffffffu;  // of slots that stay without being asked (no weight has it)
-constexpr uint32_t kNoKey = 0xfffffffeu;     // of no slot (nor has any weight this)
+__device__ __forceinline__ uint32_t order_of(int pos) { return (uint32_t)pos ^ 0x80000000u; }
 
 // Inclusive sum over the lanes of a wave
 template <int CTRL, int ROW_MASK>
@@ -39,85 +41,109 @@ __device__ __forceinline__ int wave_running_sum(int v) {
     return dpp_add<0x143, 0xc>(v);  // row_bcast31 into rows 2 and 3
 }
 
-// In the histogram's order (from the top bin down if TOP, else from bin 0 up) the bin that the `rank`-th entry (1-based) lies in, the entries
-// before that bin and those in it.  All kSelThreads threads; res is three ints of LDS.  Ends with a barrier, and leaves the histogram cleared.
+// The bin that the `rank`-th entry (1-based) of the histogram lies in, the entries before that bin and those in it.  All THREADS threads; hist is COPIES
+// histograms, added up; res is three ints of LDS.  Ends with a barrier, and leaves the histograms cleared.
 struct Bin {
     int bin, before, count;
 };
-template <bool TOP>
+template <int THREADS, int COPIES>
 __device__ __forceinline__ Bin find_bin(int *hist, int *wsum, int *res, int rank) {
+    constexpr int BPT = kBins / THREADS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int c[2];
+    int c[BPT], sum = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int b = TOP ? kBins - 1 - (2 * tid + e) : 2 * tid + e;
-        c[e] = 0;
+    for (int e = 0; e < BPT; ++e) c[e] = 0;
 #pragma unroll
-        for (int v = 0; v < kCopies; ++v) c[e] += hist[v * kBins + b], hist[v * kBins + b] = 0;
-    }
-    const int run = wave_running_sum(c[0] + c[1]);
+    for (int v = 0; v < COPIES; ++v)
+#pragma unroll
+        for (int e = 0; e < BPT; ++e) c[e] += hist[v * kBins + BPT * tid + e];
+#pragma unroll
+    for (int v = 0; v < COPIES; ++v)
+#pragma unroll
+        for (int e = 0; e < BPT; ++e) hist[v * kBins + BPT * tid + e] = 0;
+#pragma unroll
+    for (int e = 0; e < BPT; ++e) sum += c[e];
+    const int run = wave_running_sum(sum);
     if (lane == 63) wsum[wave] = run;
     __syncthreads();
-    int base = run - c[0] - c[1];
+    int base = run - sum;
 #pragma unroll
-    for (int v = 0; v < kSelThreads / 64; ++v) base += v < wave ? wsum[v] : 0;
+    for (int v = 0; v < THREADS / 64; ++v) base += v < wave ? wsum[v] : 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (base < rank && rank <= base + c[e]) res[0] = TOP ? kBins - 1 - (2 * tid + e) : 2 * tid + e, res[1] = base, res[2] = c[e];
+    for (int e = 0; e < BPT; ++e) {
+        if (base < rank && rank <= base + c[e]) res[0] = BPT * tid + e, res[1] = base, res[2] = c[e];
         base += c[e];
     }
     __syncthreads();
     return Bin{res[0], res[1], res[2]};
 }
 
-// Entries r0 .. r0 + SIZE - 1 of the set bits of words [from, to) of word(i), in order, into list; returns how many set bits there are.  All THREADS
-// threads; cnt: THREADS / 64 ints, pre: THREADS ints, xs: THREADS words of LDS.  Ends with a barrier.
-template <int THREADS, int SIZE, class W>
-__device__ __forceinline__ int list_bits(W word, int from, int to, int r0, int *list, int *cnt, int *pre, uint64_t *xs) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int total = 0;
-    for (int i0 = from; i0 < to; i0 += THREADS) {
-        const uint64_t x = i0 + tid < to ? word(i0 + tid) : 0;
-        const int c = __popcll(x), run = wave_running_sum(c);
-        if (lane == 63) cnt[wave] = run;
-        __syncthreads();
-        int first = total + run - c;
-#pragma unroll
-        for (int v = 0; v < THREADS / 64; ++v) {
-            first += v < wave ? cnt[v] : 0;
-            total += cnt[v];
-        }
-        pre[tid] = first - r0, xs[tid] = x;
-        __syncthreads();
-        const int n = min(THREADS, to - i0);
-        // a wave a word, a lane a bit, four words at a time
-        for (int j0 = wave; j0 < n; j0 += THREADS / 16) {
-            uint64_t y[4];
-            int at[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = min(j0 + e * (THREADS / 64), THREADS - 1);  // (words past n are zeros)
-                y[e] = xs[j], at[e] = pre[j];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = at[e] + __popcll(y[e] & ((1ull << lane) - 1));
-                if ((y[e] >> lane & 1) && j0 + e * (THREADS / 64) < n && r >= 0 && r < SIZE) list[r] = (i0 + j0 + e * (THREADS / 64)) * 64 + lane;
-            }
-        }
-        __syncthreads();
-    }
-    return total;
-}
-
 // The bits of word i that count: freed slots below keep, or late ones from keep on (of n)
 __device__ __forceinline__ uint64_t freed_word(uint64_t bits, int i, int keep) {
-    return ~bits & (keep - i * 64 >= 64 ? ~0ull : (1ull << (keep - i * 64)) - 1);
+    return i * 64 >= keep ? 0 : ~bits & (keep - i * 64 >= 64 ? ~0ull : (1ull << (keep - i * 64)) - 1);
 }
 __device__ __forceinline__ uint64_t late_word(uint64_t bits, int i, int n, int keep) {
     const int s0 = i * 64;
     const uint64_t held = n - s0 >= 64 ? ~0ull : (1ull << (n - s0)) - 1;
-    return bits & held & (s0 >= keep ? ~0ull : ~((1ull << (keep - s0)) - 1));  // (word keep / 64 on)
+    return s0 + 64 <= keep ? 0 : bits & held & (s0 >= keep ? ~0ull : ~((1ull << (keep - s0)) - 1));
+}
+
+// LDS of list_moves
+template <int THREADS>
+struct MoveLists {
+    int pre[2][THREADS], cnt[2][THREADS / 64];
+    uint64_t xs[2][THREADS];
+};
+// Entries r0 .. r0 + SIZE - 1 of the freed slots and of the late ones, in order, into list[0] and list[1]; returns how many there are of each.  A
+// thread counts a word's bits, then a wave takes a word and a lane a bit, four words at a time.  All THREADS threads; ends with a barrier.
+template <int THREADS, int SIZE>
+__device__ __forceinline__ int list_moves(const uint64_t *bits, int n, int keep, int r0, int *freed, int *late, MoveLists<THREADS> &m) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), words = (n + 63) / 64;
+    int total[2] = {0, 0};
+    for (int i0 = 0; i0 < words; i0 += THREADS) {
+        const uint64_t b = i0 + tid < words ? bits[i0 + tid] : 0;
+        const uint64_t x[2] = {i0 + tid < words ? freed_word(b, i0 + tid, keep) : 0, i0 + tid < words ? late_word(b, i0 + tid, n, keep) : 0};
+        int run[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            run[h] = wave_running_sum(__popcll(x[h]));
+            if (lane == 63) m.cnt[h][wave] = run[h];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int first = total[h] + run[h] - __popcll(x[h]);
+#pragma unroll
+            for (int v = 0; v < THREADS / 64; ++v) {
+                first += v < wave ? m.cnt[h][v] : 0;
+                total[h] += m.cnt[h][v];
+            }
+            m.pre[h][tid] = first - r0, m.xs[h][tid] = x[h];
+        }
+        __syncthreads();
+        const int have = min(THREADS, words - i0);
+        for (int h = 0; h < 2; ++h) {
+            // (freed slots are in the words up to keep's, late ones in those from it on)
+            const int from = h ? max(keep / 64 - i0, 0) : 0, to = h ? have : min((keep + 63) / 64 - i0, have);
+            int *list = h ? late : freed;
+            for (int j0 = from + wave; j0 < to; j0 += THREADS / 16) {
+                uint64_t y[4];
+                int at[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = min(j0 + e * (THREADS / 64), THREADS - 1);
+                    y[e] = m.xs[h][j], at[e] = m.pre[h][j];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + e * (THREADS / 64), r = at[e] + __popcll(y[e] & ((1ull << lane) - 1));
+                    if (j < to && (y[e] >> lane & 1) && r >= 0 && r < SIZE) list[r] = (i0 + j) * 64 + lane;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    return total[1];
 }
 
 struct Planes {  // of one layer, sequence and head
@@ -130,7 +156,7 @@ struct Planes {  // of one layer, sequence and head
 // Slots late[i] to freed[i], i < m: D / 16 threads a slot, 16 bytes of codes each, a few slots' loads in flight
 template <int D, int THREADS>
 __device__ __forceinline__ void move_slots(const Planes &p, const int *late, const int *freed, int m) {
-    constexpr int CB = D / 2, SB = D / 32, TPM = CB / 16 * 2, U = 4;
+    constexpr int CB = D / 2, SB = D / 32, TPM = CB / 16 * 2, U = 8;
     for (int u0 = threadIdx.x; u0 < m * TPM; u0 += U * THREADS) {
         u32x4 x[U];
         uint32_t y[U];
@@ -182,194 +208,205 @@ __device__ __forceinline__ Planes planes_of(const EvictArgs &a, const Kv4Span &s
     return Planes{a.view.k + k, a.view.v + k, a.view.ks + s, a.view.vs + s, a.w_in + at, a.p_in + at, a.w_out + at, a.p_out + at};
 }
 
-// SINGLE: all slots are in registers (at most 1024 PER), else they are read anew for every digit
-template <int D, int PER, bool SINGLE, int CAP>
-__global__ __launch_bounds__(kSelThreads) void k_kv4_evict(const Kv4Spans<CAP> t, const EvictArgs a) {
-    constexpr int kChunk = kSelThreads * PER, kList = 1024;
-    __shared__ __align__(16) int hist[kCopies * kBins];
-    __shared__ int wsum[kSelThreads / 64], res[3];
-    __shared__ uint64_t bits_s[kBitWords];
+// HELD: the slots' 32 bits are kept in LDS
+template <int D, int THREADS, bool HELD, int CAP>
+__global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, const EvictArgs a) {
+    constexpr int COPIES = THREADS / 256, WAVES = THREADS / 64;
+    extern __shared__ __align__(16) uint64_t dyn[];  // the bits, then the slots' 32 bits
+    __shared__ __align__(16) int hist[COPIES * kBins + 2048];  // (and later the lists of moves)
+    __shared__ __align__(16) int wsum[WAVES], res[3], n_near;
+    __shared__ __align__(16) uint32_t near_o[kDirect], near_p[kDirect];
+    __shared__ __align__(16) int near_s[kDirect], near_rank[kDirect];
     const Kv4Span sp = t.s[blockIdx.y];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = sp.len, keep = a.keep;
     const Planes pl = planes_of<D>(a, sp, blockIdx.x, blockIdx.z);
     const bool copy = a.w_out != a.w_in;
     if (n <= keep) {
         if (copy)
-            for (int i = tid; i < n; i += kSelThreads) pl.w_out[i] = pl.w_in[i], pl.p_out[i] = pl.p_in[i];
+            for (int i = tid; i < n; i += THREADS) pl.w_out[i] = pl.w_in[i], pl.p_out[i] = pl.p_in[i];
         return;
     }
-    const int fixed_from = sp.pos - a.recent;  // positions from here on stay
-    uint32_t key[PER];  // (positions are read again where they decide between equal weights)
-    auto load = [&](int i0) {
-        constexpr int U = PER < 16 ? PER : 16;  // at a time
-#pragma unroll
-        for (int e0 = 0; e0 < PER; e0 += U) {
-            if (i0 + e0 * kSelThreads >= n) break;
-            int pos[U];
+    const int fixed_from = sp.pos - a.recent, words = (n + 63) / 64;  // positions from fixed_from on stay
+    uint64_t *bits = dyn;
+    if (n > kBitSlots || a.parts) bits = a.kept + (((size_t)blockIdx.z * t.n + blockIdx.y) * a.view.nkv + blockIdx.x) * a.kept_words;
+    uint32_t *held = reinterpret_cast<uint32_t *>(dyn + words);
+    for (int i = tid; i < COPIES * kBins; i += THREADS) hist[i] = 0;
+    if (tid == 0) n_near = 0;
+    if (tid < kDirect) near_rank[tid] = 0;
+    __syncthreads();
+    int *mine = hist + (wave % COPIES) * kBins;
+    // f(slot, its 32 bits) for all slots; whole waves, `in` says which lanes have one
+    auto each = [&](auto f) {
+        constexpr int U = 4;
+        for (int i0 = 0; i0 < n; i0 += U * THREADS) {
+            uint32_t o[U];
 #pragma unroll
             for (int e = 0; e < U; ++e) {
-                const int i = i0 + (e0 + e) * kSelThreads + tid;
-                pos[e] = i < n ? pl.p_in[i] : 0;
-                key[e0 + e] = i < n ? __float_as_uint(pl.w_in[i]) : 0;
+                const int i = min(i0 + e * THREADS + tid, n - 1);
+                o[e] = HELD ? held[i] : order_of(pl.w_in[i], pl.p_in[i] >= fixed_from);
+            }
+#pragma unroll
+            for (int e = 0; e < U; ++e) f(i0 + e * THREADS + tid, o[e], i0 + e * THREADS + tid < n);
+        }
+    };
+    // a histogram entry; those that stay anyway are many, share a bin, and are counted by wave
+    auto count = [&](int bin, bool in, bool same) {
+        const uint64_t b = __builtin_amdgcn_ballot_w64(in && same);
+        if (in && !same) atomicAdd(&mine[bin], 1);
+        if (b && lane == 0) atomicAdd(&mine[0], __popcll(b));
+    };
+    if constexpr (HELD) {
+        constexpr int U = 8;
+        for (int i0 = 0; i0 < n; i0 += U * THREADS) {
+            int p[U];
+            float w[U];
+#pragma unroll
+            for (int e = 0; e < U; ++e) {
+                const int i = min(i0 + e * THREADS + tid, n - 1);
+                p[e] = pl.p_in[i], w[e] = pl.w_in[i];
             }
 #pragma unroll
             for (int e = 0; e < U; ++e) {
-                key[e0 + e] = pos[e] >= fixed_from ? kFixedKey : weight_key(__uint_as_float(key[e0 + e]));
-                if (i0 + (e0 + e) * kSelThreads + tid >= n) key[e0 + e] = kNoKey;
+                const int i = i0 + e * THREADS + tid;
+                const uint32_t o = order_of(w[e], p[e] >= fixed_from);
+                if (i < n) held[i] = o;
+                if (i0 + e * THREADS < n) count(o >> 21, i < n, o >> 21 == 0);
             }
         }
-    };
-    auto each = [&](auto f) {  // f(slot, key) over all slots (and some past the last, without a key)
-        for (int i0 = 0; i0 < n; i0 += kChunk) {
-            if (!SINGLE) load(i0);
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                if (i0 + e * kSelThreads >= n) break;
-                f(i0 + e * kSelThreads + tid, key[e]);
-            }
-        }
-    };
-    if (SINGLE) load(0);
-    for (int i = tid; i < kCopies * kBins; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    int *mine = hist + (wave % kCopies) * kBins;
-
-    // Threshold: keys above it stay, and of those equal to it all, or `ties` by position.  The first digit also counts the slots that stay
-    // without being asked.
-    int fixed = 0;
-    each([&](int, uint32_t k) {
-        if (k < kNoKey) atomicAdd(&mine[k >> 21], 1);
-        fixed += k == kFixedKey;
-    });
-    fixed = __builtin_amdgcn_readlane(wave_running_sum(fixed), 63);
-    if (lane == 0) wsum[wave] = fixed;
-    __syncthreads();
-    fixed = 0;
-#pragma unroll
-    for (int v = 0; v < kSelThreads / 64; ++v) fixed += wsum[v];
-    __syncthreads();
-    uint32_t threshold = kFixedKey;
-    bool all_equal = false;  // those equal to the threshold, or above it up to the digit's end, all stay
-    int need = keep;
-    if (fixed < keep) {
-        need = keep - fixed;
-        Bin b = find_bin<true>(hist, wsum, res, need);
-        need -= b.before;
-        uint32_t prefix = b.bin;
-        int shift = 21;
-        if (need != b.count) {
-            each([&](int, uint32_t k) {
-                if (k < kNoKey && k >> 21 == prefix) atomicAdd(&mine[k >> 10 & 2047], 1);
-            });
-            __syncthreads();
-            b = find_bin<true>(hist, wsum, res, need);
-            need -= b.before;
-            prefix = prefix << 11 | b.bin, shift = 10;
-            if (need != b.count) {
-                each([&](int, uint32_t k) {
-                    if (k < kNoKey && k >> 10 == prefix) atomicAdd(&mine[k & 1023], 1);
-                });
-                __syncthreads();
-                b = find_bin<true>(hist, wsum, res, need);
-                need -= b.before;
-                prefix = prefix << 10 | b.bin, shift = 0;
-            }
-        }
-        threshold = prefix << shift;
-        all_equal = need == b.count;
     } else {
-        __syncthreads();
-        for (int i = tid; i < kCopies * kBins; i += kSelThreads) hist[i] = 0;  // (the first digit's)
-        __syncthreads();
-        all_equal = need == fixed;
+        each([&](int, uint32_t o, bool in) { count(o >> 21, in, o >> 21 == 0); });
     }
-    // among the ties: the `need` lowest positions (and, should positions repeat, the lowest slots)
-    uint32_t at_most = 0;
-    int ties = need;
-    if (!all_equal) {
-#pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-            each([&](int i, uint32_t k) {
-                if (k != threshold) return;
-                const uint32_t x = (uint32_t)pl.p_in[i] ^ 0x80000000u;
-                if ((pass == 0 || x >> (shift + width & 31) == at_most)) atomicAdd(&mine[x >> shift & ((1 << width) - 1)], 1);
-            });
-            __syncthreads();
-            const Bin b = find_bin<false>(hist, wsum, res, ties);
-            ties -= b.before;
-            at_most = at_most << width | b.bin;
+    __syncthreads();
+    // Digits of the 64 bits until few slots share them: `prefix` of the first `top` bits, of which `need` slots stay
+    Bin b = find_bin<THREADS, COPIES>(hist, wsum, res, keep);
+    int need = keep - b.before, top = 11;
+    uint32_t prefix = b.bin, prefix_p = 0;  // of the 32 bits, and of the position's
+    while (need != b.count && b.count > kDirect && top < 64) {
+        const int width = top == 22 || top == 54 ? 10 : 11;
+        const int from = top < 32 ? 32 - top : 64 - top;  // bits of the word below the prefix
+        each([&](int i, uint32_t o, bool in) {
+            if (top < 32) {
+                if (in && o >> from == prefix) atomicAdd(&mine[o >> (from - width) & ((1 << width) - 1)], 1);
+            } else if (in && o == prefix) {
+                const uint32_t p = order_of(pl.p_in[i]);
+                if (top == 32 || p >> from == prefix_p) atomicAdd(&mine[p >> (from - width) & ((1 << width) - 1)], 1);
+            }
+        });
+        __syncthreads();
+        b = find_bin<THREADS, COPIES>(hist, wsum, res, need);
+        need -= b.before;
+        if (top < 32) prefix = prefix << width | b.bin;
+        else prefix_p = prefix_p << width | b.bin;
+        top += width;
+    }
+    const bool all = need == b.count, ranked = !all && b.count <= kDirect;
+    const int from = top <= 32 ? 32 - top : 64 - top;
+    int done = 0;  // of slots alike in all 64 bits (a ledger of repeated positions), the first stay
+    each([&](int i, uint32_t o, bool in) {
+        bool less, like;
+        uint32_t p = 0;
+        if (top <= 32) {
+            less = o >> from < prefix, like = o >> from == prefix;
+        } else {
+            if (in && o == prefix) p = order_of(pl.p_in[i]);
+            less = o < prefix || (o == prefix && p >> from < prefix_p), like = o == prefix && p >> from == prefix_p;
         }
-    }
-    // the bits
-    uint64_t *bits = bits_s;
-    if (n > kBitWords * 64 || a.parts) bits = a.kept + (((size_t)blockIdx.z * t.n + blockIdx.y) * a.view.nkv + blockIdx.x) * a.kept_words;
-    int done = 0;  // ties with the last position, in the slots before
-    auto mark = [&](int i, uint32_t k) {  // (i may be past n)
-        const uint32_t x = !all_equal && k == threshold ? (uint32_t)pl.p_in[i] ^ 0x80000000u : 0;
-        bool stays = k != kNoKey && (all_equal ? k >= threshold : k > threshold || (k == threshold && x < at_most));
-        if (!all_equal) {
-            const bool tie = k == threshold && x == at_most;
-            const uint64_t tied = __builtin_amdgcn_ballot_w64(tie);
-            if (lane == 0) wsum[wave] = __popcll(tied);
+        less = less && in, like = like && in;
+        bool stays = less || (all && like);
+        if (ranked && like) {
+            const int at = atomicAdd(&n_near, 1);
+            near_o[at] = o, near_p[at] = order_of(pl.p_in[i]), near_s[at] = i;
+        }
+        if (!all && !ranked) {
+            const uint64_t alike = __builtin_amdgcn_ballot_w64(like);
+            if (lane == 0) wsum[wave] = __popcll(alike);
             __syncthreads();
             int before = done;
 #pragma unroll
-            for (int v = 0; v < kSelThreads / 64; ++v) {
+            for (int v = 0; v < WAVES; ++v) {
                 before += v < wave ? wsum[v] : 0;
                 done += wsum[v];
             }
-            if (tie) stays = before + __popcll(tied & ((1ull << lane) - 1)) < ties;
+            if (like) stays = before + __popcll(alike & ((1ull << lane) - 1)) < need;
             __syncthreads();
         }
         const uint64_t word = __builtin_amdgcn_ballot_w64(stays);
-        if (lane == 0 && i < n) bits[i >> 6] = word;
-        if (copy && stays && i < keep) pl.w_out[i] = pl.w_in[i], pl.p_out[i] = pl.p_in[i];
-    };
-    for (int i0 = 0; i0 < n; i0 += kChunk) {
-        if (!SINGLE) load(i0);
-#pragma unroll
-        for (int e = 0; e < PER; ++e)
-            if (i0 + e * kSelThreads < n) mark(i0 + e * kSelThreads + tid, key[e]);
-    }
-    if (a.parts) return;
+        if (lane == 0 && in) bits[i >> 6] = word;
+    });
     __syncthreads();
+    if (ranked) {  // b.count slots, THREADS / kDirect threads each
+        const int c = tid % kDirect;
+        if (c < b.count) {
+            const uint64_t x = (uint64_t)near_o[c] << 32 | near_p[c];
+            const int slot = near_s[c];
+            int rank = 0;
+            for (int j = tid / kDirect; j < b.count; j += THREADS / kDirect) {
+                const uint64_t y = (uint64_t)near_o[j] << 32 | near_p[j];
+                rank += y < x || (y == x && near_s[j] < slot);
+            }
+            atomicAdd(&near_rank[c], rank);
+        }
+        __syncthreads();
+        if (tid < b.count && near_rank[tid] < need)
+            atomicOr(reinterpret_cast<unsigned long long *>(&bits[near_s[tid] >> 6]), 1ull << (near_s[tid] & 63));
+        __syncthreads();
+    }
+    if (copy)
+        for (int i = tid; i < keep; i += THREADS)
+            if (bits[i >> 6] >> (i & 63) & 1) pl.w_out[i] = pl.w_in[i], pl.p_out[i] = pl.p_in[i];
+    if (a.parts) return;
     // the moves; the histogram's memory holds the lists
-    int *freed = hist, *late = hist + kList, *pre = hist + 2 * kList;
-    uint64_t *xs = reinterpret_cast<uint64_t *>(hist + 3 * kList);
-    static_assert(3 * kList + 2 * kSelThreads <= kCopies * kBins && kList == kSelThreads, "lists in the histogram");
+    constexpr int kList = THREADS;
+    static_assert(2 * kList * sizeof(int) + sizeof(MoveLists<THREADS>) <= sizeof(hist), "lists in the histogram");
+    int *freed = hist, *late = hist + kList;
+    MoveLists<THREADS> &lists = *reinterpret_cast<MoveLists<THREADS> *>(hist + 2 * kList);
     for (int r0 = 0;; r0 += kList) {
-        list_bits<kSelThreads, kList>([&](int i) { return freed_word(bits[i], i, keep); }, 0, (keep + 63) / 64, r0, freed, wsum, pre, xs);
-        const int total = list_bits<kSelThreads, kList>([&](int i) { return late_word(bits[i], i, n, keep); }, keep / 64, (n + 63) / 64, r0, late, wsum, pre, xs);
-        move_slots<D, kSelThreads>(pl, late, freed, min(total - r0, kList));
+        const int total = list_moves<THREADS, kList>(bits, n, keep, r0, freed, late, lists);
+        move_slots<D, THREADS>(pl, late, freed, min(total - r0, kList));
         if (r0 + kList >= total) return;
         __syncthreads();
     }
 }
 
-// Moves part * 256 .. + 255, and every parts * 256 further, of a head
-constexpr int kMoveThreads = 256;
+// Moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer further, of a head
+constexpr int kMoveThreads = 1024, kMovesPer = 512;
 template <int D, int CAP>
 __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t, const EvictArgs a) {
-    __shared__ int freed[kMoveThreads], late[kMoveThreads], pre[kMoveThreads], cnt[kMoveThreads / 64];
-    __shared__ uint64_t xs[kMoveThreads];
+    __shared__ int freed[kMovesPer], late[kMovesPer];
+    __shared__ MoveLists<kMoveThreads> lists;
     const Kv4Span sp = t.s[blockIdx.y];
     const int n = sp.len, keep = a.keep, kvh = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     if (n <= keep) return;
     const Planes pl = planes_of<D>(a, sp, kvh, blockIdx.z);
     const uint64_t *bits = a.kept + (((size_t)blockIdx.z * t.n + blockIdx.y) * a.view.nkv + kvh) * a.kept_words;
-    for (int r0 = part * kMoveThreads;; r0 += a.parts * kMoveThreads) {
-        list_bits<kMoveThreads, kMoveThreads>([&](int i) { return freed_word(bits[i], i, keep); }, 0, (keep + 63) / 64, r0, freed, cnt, pre, xs);
-        const int total = list_bits<kMoveThreads, kMoveThreads>([&](int i) { return late_word(bits[i], i, n, keep); }, keep / 64, (n + 63) / 64, r0,
-                                                                late, cnt, pre, xs);
-        move_slots<D, kMoveThreads>(pl, late, freed, min(total - r0, kMoveThreads));
-        if (r0 + a.parts * kMoveThreads >= total) return;
+    for (int r0 = part * kMovesPer;; r0 += a.parts * kMovesPer) {
+        const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, r0, freed, late, lists);
+        move_slots<D, kMoveThreads>(pl, late, freed, min(total - r0, kMovesPer));
+        if (r0 + a.parts * kMovesPer >= total) return;
         __syncthreads();
     }
 }
 
 // Moves by blocks of their own from so many moves of one head, and below so many heads
 constexpr int kMoveMany = 1024, kMoveHeads = 128;
+
+template <int D, int CAP>
+static void evict_in(const Kv4 &k, const Kv4Spans<CAP> &t, const EvictArgs &a, int longest, dim3 grid) {
+    const size_t bit_bytes = (size_t)((longest + 63) / 64) * 8;
+    auto raised = [](auto *kern) {  // once per kernel: up to 115 KB of LDS asked for at the launch
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 4 + kHeldSlots / 8);
+    };
+    if (longest <= 2048) {  // a block of 256 threads: cheaper barriers and scans
+        hipLaunchKernelGGL((k_kv4_evict<D, 256, true, CAP>), grid, dim3(256), bit_bytes + 4 * (size_t)longest, k.stream, t, a);
+    } else if (longest <= kHeldSlots) {
+        static std::once_flag once;
+        std::call_once(once, [&] { raised(k_kv4_evict<D, 1024, true, CAP>); });
+        hipLaunchKernelGGL((k_kv4_evict<D, 1024, true, CAP>), grid, dim3(1024), bit_bytes + 4 * (size_t)longest, k.stream, t, a);
+    } else {
+        hipLaunchKernelGGL((k_kv4_evict<D, 1024, false, CAP>), grid, dim3(1024), longest <= kBitSlots ? bit_bytes : kBitSlots / 8, k.stream, t, a);
+    }
+    if (a.parts) hipLaunchKernelGGL((k_kv4_move<D, CAP>), dim3(grid.x * a.parts, grid.y, grid.z), dim3(kMoveThreads), 0, k.stream, t, a);
+}
 
 void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
                       const int32_t *p_in, float *w_out, int32_t *p_out) {
@@ -378,21 +415,12 @@ void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &
     int longest = 0;
     for (int j = 0; j < t.n; ++j) longest = t.s[j].len > longest ? t.s[j].len : longest;
     const int over = longest - keep > 0 ? longest - keep : 0, moves = over < keep ? over : keep;  // at most, of one head
-    const int parts = moves > kMoveMany && nkv * t.n * layers < kMoveHeads ? (moves + kMoveThreads - 1) / kMoveThreads : 0;
+    const int parts = moves > kMoveMany && nkv * t.n * layers < kMoveHeads ? (moves + kMovesPer - 1) / kMovesPer : 0;
     const EvictArgs a = {k.view(layer_lo), k.per_layer[0], k.per_layer[2], slots, keep, recent, parts, w_in + off, p_in + off, w_out + off,
                          p_out + off, k.kept, k.kept_words};
     with_table(t, [&](auto tab) {
-        constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
-#define ST_EVICT(DV)                                                                                         \
-    (longest <= 4096    ? k_kv4_evict<DV, 4, true, CAP>                                                      \
-     : longest <= 32768 ? k_kv4_evict<DV, 32, true, CAP>                                                     \
-                        : k_kv4_evict<DV, 32, false, CAP>)
-        auto *kern = k.c.head_dim == 128 ? ST_EVICT(128) : ST_EVICT(64);
-#undef ST_EVICT
-        hipLaunchKernelGGL(kern, dim3(nkv, t.n, layers), dim3(kSelThreads), 0, k.stream, tab, a);
-        if (!parts) return;
-        auto *move = k.c.head_dim == 128 ? k_kv4_move<128, CAP> : k_kv4_move<64, CAP>;
-        hipLaunchKernelGGL(move, dim3(nkv * parts, t.n, layers), dim3(kMoveThreads), 0, k.stream, tab, a);
+        if (k.c.head_dim == 128) evict_in<128>(k, tab, a, longest, dim3(nkv, t.n, layers));
+        else evict_in<64>(k, tab, a, longest, dim3(nkv, t.n, layers));
     });
 }
 
