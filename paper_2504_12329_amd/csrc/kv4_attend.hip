@@ -112,10 +112,11 @@ struct Column {
 __device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Column{col / G, kvh * G + col % G}; }
 
 // ---------------------------------------------------------------------------------------
-// Few columns (rows x G <= 64 in every span): single tokens and short runs.  Bound by memory: the cache is read once and every
-// value meets at most 64 columns.
+// Few columns: single tokens and short runs.  With one group of columns bound by memory (the cache is read once), with more by the vector
+// pipe.
 //
-// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end: S^T by 16x16x32 MFMAs whose A rows
+// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end (four tiles no longer fit the
+// registers without moves: 36 us for 86 rows of 40 / 8 heads on 4096 slots, against 28 with two): S^T by 16x16x32 MFMAs whose A rows
 // are slots 8 (m / 4) + 4 t + m % 4, so that lane (column, quarter) ends up with the weights of slots 8 quarter .. + 7 -- the
 // B operand of the second product.  A lane reads 16 bytes (one scale group) of each of its two keys and, of eight value
 // slots, the D / 16 channels that make its row m of D / 16 products.  The next tile's loads are issued before
@@ -124,7 +125,7 @@ __device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Co
 constexpr int kFewTile = 32, kFewWaves = 4;
 
 template <int D, int NT, int CAP>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                  int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
                                                  float *__restrict__ part_o, float *__restrict__ part_ml,
                                                  float *__restrict__ lse) {
@@ -133,19 +134,20 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m16 = lane & 15, qd = lane >> 4;
     const int nkv = view.nkv, G = view.nq / nkv;
-    const int kvh = (blockIdx.x - sp.blk0) % nkv, z = (blockIdx.x - sp.blk0) / nkv;
+    const int cols = sp.rows * G, n_cb = (cols + 16 * NT - 1) / (16 * NT), local = blockIdx.x - sp.blk0;
+    const int kvh = local % nkv, z = local / nkv / n_cb, c0 = local / nkv % n_cb * (16 * NT);  // c0: the block's first column
     const int n_keys = sp.len + sp.rows, last = n_keys - 1, n_tiles = (n_keys + kFewTile - 1) / kFewTile;
     const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
     const size_t head0 = ((size_t)sp.seq * nkv + kvh) * view.max_seq;
     const uint8_t *kc = view.k + head0 * CB, *vc = view.v + head0 * CB, *ks = view.ks + head0 * SB, *vs = view.vs + head0 * SB;
-    const int cols = sp.rows * G;
+    const int sees_all = sp.len + c0 / G;  // last slot that all of its columns see
     const float scale = 1.4426950408889634f / sqrtf((float)D);
 
     bf16x8 qf[NT][KS];
     int lim[NT];  // last slot the column sees
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
-        const Column w = column_of(min(16 * c + m16, cols - 1), G, kvh);
+        const Column w = column_of(min(c0 + 16 * c + m16, cols - 1), G, kvh);
         lim[c] = sp.len + w.row;
         const bf16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * (D / 4);
 #pragma unroll
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(
                 for (int c = 0; c < NT; ++c) sc[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][s], sc[c][u], 0, 0, 0);
             }
         Units8 unit(x.v, 8 * (m16 * DPL / 32));
-        const bool part = key0 + kFewTile - 1 > sp.len;  // some row does not see all of the tile
+        const bool part = key0 + kFewTile - 1 > sees_all;  // some row does not see all of the tile
         uint32_t poison = 0;                              // columns (bit c) that see a NaN among this lane's output channels
         if (part) {
 #pragma unroll
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_kv4_few(
                 *reinterpret_cast<float4 *>(&so[wave][m16][(4 * qd + r) * DPL + T]) =
                     make_float4(o[c][T][r], o[c][T + 1][r], o[c][T + 2][r], o[c][T + 3][r]);
         __syncthreads();
-        const int col = 16 * c + (threadIdx.x >> 4), n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DPL;
+        const int col = c0 + 16 * c + (threadIdx.x >> 4), n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DPL;
         if (col >= cols) continue;
         float M = sm[0][n], w[kFewWaves], L = 0.f;
 #pragma unroll
@@ -859,40 +861,62 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf1
     const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv, D = k.c.head_dim;
     const Kv4View view = k.view(layer);
     float *lse = weights ? k.lse : nullptr;
-    int most = 0;
-    for (int j = 0; j < t.n; ++j) most = t.s[j].rows > most ? t.s[j].rows : most;
-    const int64_t cols = (int64_t)most * G;
-    const bool few = cols <= 64;
-    const int blocks = few ? cut_ranges(k, t, kFewTile, kFewWaves, 768, [&](const Kv4Span &) { return nkv; })
-                           : cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return nkv * ((s.rows * G + kTileCols - 1) / kTileCols); });
+    int64_t most = 0, few_tiles = 0, chunk_tiles = 0;
+    for (int j = 0; j < t.n; ++j) {
+        if (!t.s[j].rows) continue;
+        const int64_t cols = (int64_t)t.s[j].rows * G, held = t.s[j].len + t.s[j].rows;
+        most = cols > most ? cols : most;
+        few_tiles += (cols + 31) / 32 * nkv * ((held + kFewTile - 1) / kFewTile);
+        chunk_tiles += (cols + kTileCols - 1) / kTileCols * nkv * ((held + kTileKeys - 1) / kTileKeys);
+    }
+    // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk, which takes some 14 us more to
+    // get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
+    const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10, fused = weights && few && most <= 64;
+    const int cols_few = most <= 16 ? 16 : 32;  // columns of a block
+    auto groups = [&](const Kv4Span &s, int cols) { return nkv * ((s.rows * G + cols - 1) / cols); };
+    const int blocks = few ? cut_ranges(k, t, kFewTile, kFewWaves, most <= 16 ? 512 : 256, [&](const Kv4Span &s) { return groups(s, cols_few); })
+                           : cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return groups(s, kTileCols); });
     int join = 0;  // rows of the longest span in several ranges
     for (int j = 0; j < t.n; ++j)
         if (t.s[j].splits > 1 && t.s[j].rows > join) join = t.s[j].rows;
     with_table(t, [&](auto tab) {
         constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
         const int nq = k.c.n_q_heads, units = join * nq;
-#define ST_FEW(DV, NTV)                                                                                                          \
-    do {                                                                                                                         \
-        hipLaunchKernelGGL((k_kv4_few<DV, NTV, CAP>), dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out,         \
-                           out_stride, k.part_o, k.part_ml, lse);                                                                \
-        if (weights)                                                                                                             \
-            hipLaunchKernelGGL((k_kv4_few_weights<DV, NTV, CAP>), dim3(blocks + units * t.n), dim3(256), 0, k.stream, tab, view, \
-                               q, q_stride, k.part_o, k.part_ml, lse, blocks, join, out, out_stride, weights);                   \
-    } while (0)
-        if (few && D == 128) {
-            if (cols <= 16) ST_FEW(128, 1);
-            else if (cols <= 32) ST_FEW(128, 2);
-            else ST_FEW(128, 4);
+#define ST_FEW(DV, NTV)                                                                                                                  \
+    hipLaunchKernelGGL((k_kv4_few<DV, NTV, CAP>), dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out, out_stride, k.part_o, \
+                       k.part_ml, lse)
+        if (few && most <= 16) {
+            if (D == 128) ST_FEW(128, 1);
+            else ST_FEW(64, 1);
         } else if (few) {
-            if (cols <= 16) ST_FEW(64, 1);
-            else if (cols <= 32) ST_FEW(64, 2);
-            else ST_FEW(64, 4);
+            if (D == 128) ST_FEW(128, 2);
+            else ST_FEW(64, 2);
         } else {
             auto *kern = D == 128 ? k_kv4_chunk<128, CAP> : k_kv4_chunk<64, CAP>;
             hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out, out_stride, k.part_o, k.part_ml, lse);
         }
 #undef ST_FEW
-        if (join && !(few && weights)) {
+        if (fused) {
+            int blk = 0;  // one block for all columns of a range
+            for (int j = 0; j < tab.n; ++j) {
+                tab.s[j].blk0 = blk;
+                if (tab.s[j].rows) blk += nkv * tab.s[j].splits;
+            }
+#define ST_FEW_WEIGHTS(DV, NTV)                                                                                                           \
+    hipLaunchKernelGGL((k_kv4_few_weights<DV, NTV, CAP>), dim3(blk + units * tab.n), dim3(256), 0, k.stream, tab, view, q, q_stride, k.part_o, \
+                       k.part_ml, lse, blk, join, out, out_stride, weights)
+            if (D == 128) {
+                if (most <= 16) ST_FEW_WEIGHTS(128, 1);
+                else if (most <= 32) ST_FEW_WEIGHTS(128, 2);
+                else ST_FEW_WEIGHTS(128, 4);
+            } else {
+                if (most <= 16) ST_FEW_WEIGHTS(64, 1);
+                else if (most <= 32) ST_FEW_WEIGHTS(64, 2);
+                else ST_FEW_WEIGHTS(64, 4);
+            }
+#undef ST_FEW_WEIGHTS
+        }
+        if (join && !fused) {
             // four waves a unit while there are fewer units than would fill the chip with one each
             const bool wide = units * t.n < 1024;
             auto *kern = D == 128 ? (wide ? k_kv4_join<128, 4, CAP> : k_kv4_join<128, 1, CAP>) : (wide ? k_kv4_join<64, 4, CAP> : k_kv4_join<64, 1, CAP>);
@@ -900,7 +924,7 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf1
                                out, out_stride, lse);
         }
     });
-    if (weights && !few) {
+    if (weights && !fused) {
         int blk = 0;
         for (int j = 0; j < t.n; ++j) {
             t.s[j].blk0 = blk;
