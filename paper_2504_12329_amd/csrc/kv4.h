@@ -15,27 +15,29 @@ struct Kv4Span {
     int32_t per;                  // tiles of slots in a range
     int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
 };
-// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Two sizes, as a launch with 2 KB of
-// arguments costs the host more (LAUNCHCOST).
+// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Three sizes, as a launch with the
+// largest costs the host 3.4 us and one with the smallest 2.4.
 template <int CAP>
 struct Kv4Spans {
     int32_t n;
     Kv4Span s[CAP];
 };
-constexpr int kKv4Few = 4;
+constexpr int kKv4Few = 4, kKv4Some = 16;
 typedef Kv4Spans<ST_KV4_MAX_SPANS> Kv4Table;
 static_assert(sizeof(Kv4Table) <= 2400, "kernel arguments are at most 4 KB");
 // f(the table in the smallest size that holds it)
+template <int CAP, class F>
+inline void with_table_of(const Kv4Table &t, F f) {
+    Kv4Spans<CAP> small;
+    small.n = t.n;
+    for (int j = 0; j < CAP; ++j) small.s[j] = j < t.n ? t.s[j] : Kv4Span{};
+    f(small);
+}
 template <class F>
 inline void with_table(const Kv4Table &t, F f) {
-    if (t.n <= kKv4Few) {
-        Kv4Spans<kKv4Few> small;
-        small.n = t.n;
-        for (int j = 0; j < kKv4Few; ++j) small.s[j] = j < t.n ? t.s[j] : Kv4Span{};
-        f(small);
-    } else {
-        f(t);
-    }
+    if (t.n <= kKv4Few) with_table_of<kKv4Few>(t, f);
+    else if (t.n <= kKv4Some) with_table_of<kKv4Some>(t, f);
+    else f(t);
 }
 
 // The planes of one layer and its heads

@@ -37,8 +37,7 @@ struct Values8 {
     uint32_t c[8], s[D / 16];
     // bits of the scale of slot j (byte << 23); shift: 8 * group
     __device__ __forceinline__ uint32_t unit(int j, int shift) const {
-        const uint32_t w = D == 128 ? s[j] : s[j >> 1] >> 16 * (j & 1);
-        return (w >> shift & 255) << 23;
+        return __builtin_amdgcn_ubfe(D == 128 ? s[j] : s[j >> 1], shift + (D == 128 ? 0 : 16 * (j & 1)), 8) << 23;
     }
 };
 // Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each.  TAIL: slots past `last` are read as `last` (no address

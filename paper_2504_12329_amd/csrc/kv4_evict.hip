@@ -136,8 +136,10 @@ __device__ __forceinline__ int list_moves(const uint64_t *bits, int n, int keep,
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + e * (THREADS / 64), r = at[e] + __popcll(y[e] & ((1ull << lane) - 1));
-                    if (j < to && (y[e] >> lane & 1) && r >= 0 && r < SIZE) list[r] = (i0 + j) * 64 + lane;
+                    const int j = j0 + e * (THREADS / 64), first = __builtin_amdgcn_readfirstlane(at[e]);
+                    if (j >= to || first >= SIZE || first <= -64) continue;  // nothing of these entries
+                    const int r = first + __popcll(y[e] & ((1ull << lane) - 1));
+                    if ((y[e] >> lane & 1) && r >= 0 && r < SIZE) list[r] = (i0 + j) * 64 + lane;
                 }
             }
         }
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
         if (b && lane == 0) atomicAdd(&mine[0], __popcll(b));
     };
     if constexpr (HELD) {
-        constexpr int U = 8;
+        constexpr int U = THREADS == 1024 ? 16 : 8;
         for (int i0 = 0; i0 < n; i0 += U * THREADS) {
             int p[U];
             float w[U];
@@ -300,39 +302,49 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
         top += width;
     }
     const bool all = need == b.count, ranked = !all && b.count <= kDirect;
-    const int from = top <= 32 ? 32 - top : 64 - top;
-    int done = 0;  // of slots alike in all 64 bits (a ledger of repeated positions), the first stay
-    each([&](int i, uint32_t o, bool in) {
-        bool less, like;
-        uint32_t p = 0;
-        if (top <= 32) {
-            less = o >> from < prefix, like = o >> from == prefix;
-        } else {
-            if (in && o == prefix) p = order_of(pl.p_in[i]);
-            less = o < prefix || (o == prefix && p >> from < prefix_p), like = o == prefix && p >> from == prefix_p;
-        }
-        less = less && in, like = like && in;
-        bool stays = less || (all && like);
-        if (ranked && like) {
-            const int at = atomicAdd(&n_near, 1);
-            near_o[at] = o, near_p[at] = order_of(pl.p_in[i]), near_s[at] = i;
-        }
-        if (!all && !ranked) {
-            const uint64_t alike = __builtin_amdgcn_ballot_w64(like);
-            if (lane == 0) wsum[wave] = __popcll(alike);
-            __syncthreads();
-            int before = done;
-#pragma unroll
-            for (int v = 0; v < WAVES; ++v) {
-                before += v < wave ? wsum[v] : 0;
-                done += wsum[v];
+    if (top <= 32) {
+        // slots below `low` stay, of those from it to `high` all or the ones that rank below `need`
+        const uint32_t low = prefix << (32 - top), high = low + ((1u << (32 - top)) - 1);
+        each([&](int i, uint32_t o, bool in) {
+            const uint64_t word = all ? __builtin_amdgcn_ballot_w64(in && o <= high) : __builtin_amdgcn_ballot_w64(in && o < low);
+            if (lane == 0 && in) bits[i >> 6] = word;
+            const bool like = in && o >= low && o <= high;
+            if (ranked && __builtin_amdgcn_ballot_w64(like)) {
+                if (like) {
+                    const int at = atomicAdd(&n_near, 1);
+                    near_o[at] = o, near_p[at] = order_of(pl.p_in[i]), near_s[at] = i;
+                }
             }
-            if (like) stays = before + __popcll(alike & ((1ull << lane) - 1)) < need;
-            __syncthreads();
-        }
-        const uint64_t word = __builtin_amdgcn_ballot_w64(stays);
-        if (lane == 0 && in) bits[i >> 6] = word;
-    });
+        });
+    } else {
+        const int from = 64 - top;
+        int done = 0;  // of slots alike in all 64 bits (a ledger of repeated positions), the first stay
+        each([&](int i, uint32_t o, bool in) {
+            uint32_t p = 0;
+            if (in && o == prefix) p = order_of(pl.p_in[i]);
+            const bool less = in && (o < prefix || (o == prefix && p >> from < prefix_p)), like = in && o == prefix && p >> from == prefix_p;
+            bool stays = less || (all && like);
+            if (ranked && like) {
+                const int at = atomicAdd(&n_near, 1);
+                near_o[at] = o, near_p[at] = p, near_s[at] = i;
+            }
+            if (!all && !ranked) {
+                const uint64_t alike = __builtin_amdgcn_ballot_w64(like);
+                if (lane == 0) wsum[wave] = __popcll(alike);
+                __syncthreads();
+                int before = done;
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) {
+                    before += v < wave ? wsum[v] : 0;
+                    done += wsum[v];
+                }
+                if (like) stays = before + __popcll(alike & ((1ull << lane) - 1)) < need;
+                __syncthreads();
+            }
+            const uint64_t word = __builtin_amdgcn_ballot_w64(stays);
+            if (lane == 0 && in) bits[i >> 6] = word;
+        });
+    }
     __syncthreads();
     if (ranked) {  // b.count slots, THREADS / kDirect threads each
         const int c = tid % kDirect;
