@@ -23,7 +23,7 @@ EXPORTS = ("st_query_sizes", "st_prefill_plan_check", "st_prefill_plan_forms", "
            "st_generate", "st_generate_policy", "st_batch_query_sizes", "st_batch_create", "st_batch_destroy",
            "st_batch_kv_len", "st_batch_truncate", "st_batch_prefill", "st_batch_prefill_many", "st_batch_decode_step",
            "st_generate_batch", "st_kv4_query_sizes", "st_kv4_create", "st_kv4_destroy", "st_kv4_append", "st_kv4_attend",
-           "st_kv4_evict", "st_kv4_read", "st_last_error")
+           "st_kv4_attend_plan", "st_kv4_evict", "st_kv4_read", "st_last_error")
 
 
 class StError(RuntimeError):
@@ -145,6 +145,7 @@ def lib():
                                     C.c_void_p, C.c_int64, ledger]
         L.st_kv4_attend.argtypes = [C.c_void_p, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                     ledger]
+        L.st_kv4_attend_plan.argtypes = [C.POINTER(st_kv4_config), spans, C.c_int32] + [C.POINTER(C.c_int32)] * 3
         L.st_kv4_evict.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_int32, C.c_int32, ledger, ledger]
         L.st_kv4_read.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_void_p]
         _lib = L
@@ -673,6 +674,13 @@ class Kv4Cache:
             if rc:
                 _check(rc)
         return out
+
+    def attend_plan(self, spans):
+        """(columns of a block, blocks, key ranges of every span) of attend(..., spans, ...) (see st_kv4_attend_plan)."""
+        c = st_kv4_config(*(self.cfg[n] for n, _ in st_kv4_config._fields_))
+        columns, blocks, ranges = C.c_int32(), C.c_int32(), (C.c_int32 * max(spans.n, 1))()
+        _check(lib().st_kv4_attend_plan(C.byref(c), spans.c, spans.n, C.byref(columns), C.byref(blocks), ranges))
+        return columns.value, blocks.value, list(ranges)[:spans.n]
 
     def evict(self, layer_lo, layer_hi, spans, keep, recent, ledger, into=None):
         """Brings the spans' sequences to `keep` slots in layers [layer_lo, layer_hi) (see st_kv4_evict); the ledger's entries move along, in place or to `into`."""

@@ -40,6 +40,9 @@ inline void with_table(const Kv4Table &t, F f) {
     else f(t);
 }
 
+// Attention: most columns (rows x query heads of a kv head) of a block, most key ranges, most blocks where key ranges are cut
+constexpr int kKv4Columns = 128, kKv4Ranges = 64, kKv4Blocks = 512;
+
 // The planes of one layer and its heads
 struct Kv4View {
     uint8_t *k, *v, *ks, *vs;  // [sequence][kv head][slot][head_dim / 2 | head_dim / 32]
@@ -63,13 +66,22 @@ struct Kv4 {
     }
 };
 
+// How attention deals out a call.  Fills in blk0, splits, per and part0 of the spans.
+struct Kv4AttendPlan {
+    int cols;      // columns of a block: 16 or 32 (k_kv4_few), 128 (k_kv4_chunk)
+    int blocks;
+    int join;      // rows of the longest span in several ranges, 0 without one
+    int64_t most;  // columns of a kv head in the span with most rows
+};
+Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t);
+
 // All enqueue only; the arguments have been checked.  `t` holds spans and row0; the launchers fill in the rest.
 void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, const bf16_t *qkv, int64_t qkv_stride,
                        const bf16_t *q_norm, const bf16_t *k_norm, bf16_t *q_out, int64_t q_stride, float *weights,
                        int32_t *positions);
 void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out);
-void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf16_t *q, int64_t q_stride, bf16_t *out,
-                       int64_t out_stride, float *weights);
+void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
+                       float *weights);
 void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
                       const int32_t *p_in, float *w_out, int32_t *p_out);
 

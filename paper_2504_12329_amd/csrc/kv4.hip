@@ -212,8 +212,9 @@ static void carve(const st_kv4_config &c, char *cache, char *ws, Kv4 *k, size_t 
         off += up256(bytes);
         return p;
     };
-    // Key ranges pay while rows are few: up to 64 of them for one row, 4096 rows x ranges in all.
-    k->part_rows = (c.max_rows < 64 ? (size_t)c.max_rows * 64 : 4096) * (size_t)c.n_q_heads;
+    // A launch that cuts ranges has at most 512 blocks, of at most 128 columns each, and at most 64 ranges of a row.
+    const size_t columns = (size_t)c.max_rows * c.n_q_heads * kKv4Ranges, blocks = (size_t)kKv4Blocks * kKv4Columns;
+    k->part_rows = columns < blocks ? columns : blocks;
     k->lse = reinterpret_cast<float *>(take(sizeof(float) * c.max_rows * (size_t)c.n_q_heads));
     k->part_ml = reinterpret_cast<float *>(take(sizeof(float) * 2 * k->part_rows));
     k->part_o = reinterpret_cast<float *>(take(sizeof(float) * c.head_dim * k->part_rows));
@@ -240,7 +241,7 @@ static int take_spans(const Kv4 &k, const st_kv4_span *spans, int32_t n, bool po
             if (spans[i].seq == s.seq) return fail(ST_EINVAL, "spans %d and %d are both sequence %d", i, j, s.seq);
         t->s[j] = Kv4Span{s.seq, s.len, s.pos, s.rows, (int32_t)total, 0, 1, 0, 0};
         total += s.rows;
-        if (total > INT32_MAX / 2) return fail(ST_ERANGE, "too many rows");
+        if (total >= 1 << 24) return fail(ST_ERANGE, "2^24 rows or more");  // a launch has at most 2^32 - 1 threads a direction
     }
     t->n = n;
     *rows = (int)total;
@@ -251,6 +252,9 @@ static int check_rows(const Kv4 &k, int rows) {
 }
 static int check_layers(const Kv4 &k, int lo, int hi) {
     return lo < 0 || hi > k.c.n_layers || lo > hi ? fail(ST_ERANGE, "layers [%d, %d) outside [0, %d)", lo, hi, k.c.n_layers) : ST_OK;
+}
+static int check_layer(const Kv4 &k, int layer) {
+    return layer < 0 || layer >= k.c.n_layers ? fail(ST_ERANGE, "layer %d outside [0, %d)", layer, k.c.n_layers) : ST_OK;
 }
 // rows of `width` 16-bit numbers, moved 16 bytes at a time
 static int check_matrix(const char *name, const void *p, int64_t stride, int64_t width) {
@@ -316,7 +320,7 @@ int st_kv4_append(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     const int64_t d = k->c.head_dim;
     Kv4Table t;
     int rows;
-    if (int rc = check_layers(*k, layer, layer + 1)) return rc;
+    if (int rc = check_layer(*k, layer)) return rc;
     if (int rc = take_spans(*k, spans, n, true, &t, &rows)) return rc;
     if (int rc = check_rows(*k, rows)) return rc;
     if (int rc = check_matrix("qkv", qkv, qkv_stride, (k->c.n_q_heads + 2 * k->c.n_kv_heads) * d)) return rc;
@@ -340,7 +344,7 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     const int64_t width = (int64_t)k->c.n_q_heads * k->c.head_dim;
     Kv4Table t;
     int rows;
-    if (int rc = check_layers(*k, layer, layer + 1)) return rc;
+    if (int rc = check_layer(*k, layer)) return rc;
     if (int rc = take_spans(*k, spans, n, false, &t, &rows)) return rc;
     if (int rc = check_rows(*k, rows)) return rc;
     if (int rc = check_matrix("q", q, q_stride, width)) return rc;
@@ -349,9 +353,26 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
         if (int rc = check_ledger(ledger, "ledger")) return rc;
     if (!rows) return ST_OK;
     const size_t base = (size_t)layer * k->c.n_seq * k->c.n_kv_heads * k->c.max_seq;
-    launch_kv4_attend(*k, layer, t, rows, (const bf16_t *)q, q_stride, (bf16_t *)out, out_stride,
+    launch_kv4_attend(*k, layer, t, (const bf16_t *)q, q_stride, (bf16_t *)out, out_stride,
                       ledger ? ledger->weights + base : nullptr);
     return launched("st_kv4_attend");
+}
+
+int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t *columns, int32_t *blocks, int32_t *ranges) {
+    if (int rc = check_config(cfg)) return rc;
+    Kv4 k{};
+    size_t cb, wb;
+    Kv4Table t;
+    int rows;
+    k.c = *cfg;
+    carve(*cfg, nullptr, nullptr, &k, &cb, &wb);
+    if (int rc = take_spans(k, spans, n, false, &t, &rows)) return rc;
+    if (int rc = check_rows(k, rows)) return rc;
+    const Kv4AttendPlan p = plan_kv4_attend(k, t);
+    if (columns) *columns = rows ? p.cols : 0;
+    if (blocks) *blocks = rows ? p.blocks : 0;
+    for (int j = 0; ranges && j < n; ++j) ranges[j] = t.s[j].rows ? t.s[j].splits : 0;
+    return ST_OK;
 }
 
 int st_kv4_evict(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, int32_t keep,

@@ -345,7 +345,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans
 //   S^T rows: fragment row m of 32 slots is slot swap(m) (bits 2 and 3 exchanged): registers 0-7 and 8-15 of a lane are then eight
 //   consecutive slots each, as the second product wants them.
 // ---------------------------------------------------------------------------------------
-constexpr int kTileKeys = 128, kTileCols = 128;
+constexpr int kTileKeys = 128, kTileCols = kKv4Columns;
 
 __device__ __forceinline__ int swap23(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
@@ -557,8 +557,6 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Spans<CAP> t, con
 // once; then D / 4 lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range whose
 // slots the row does not see has sum 0 and an unused output.
 // ---------------------------------------------------------------------------------------
-constexpr int kMostRanges = 64;
-
 template <int D, int WPU>
 __device__ __forceinline__ void join_unit(const Kv4Span &sp, int unit, bool live, int nq, const float *__restrict__ part_o,
                                           const float *__restrict__ part_ml, bf16_t *__restrict__ out, int64_t out_stride,
@@ -669,16 +667,16 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
         } else {
             const size_t step = (size_t)sp.rows * view.nq;
             const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)sp.part0 + (size_t)w.row * view.nq + w.head;
-            float2 r[kMostRanges / 4];
+            float2 r[kKv4Ranges / 4];
 #pragma unroll
-            for (int i = 0; i < kMostRanges / 4; ++i) r[i] = 4 * i + qd < sp.splits ? ml[(4 * i + qd) * step] : make_float2(-INFINITY, 0.f);
+            for (int i = 0; i < kKv4Ranges / 4; ++i) r[i] = 4 * i + qd < sp.splits ? ml[(4 * i + qd) * step] : make_float2(-INFINITY, 0.f);
             float M = -INFINITY, L = 0.f, x, y;
 #pragma unroll
-            for (int i = 0; i < kMostRanges / 4; ++i) M = fmaxf(M, r[i].x);
+            for (int i = 0; i < kKv4Ranges / 4; ++i) M = fmaxf(M, r[i].x);
             with_xor16(M, x, y);
             M = max_xor32(fmaxf(x, y));
 #pragma unroll
-            for (int i = 0; i < kMostRanges / 4; ++i)
+            for (int i = 0; i < kKv4Ranges / 4; ++i)
                 if (r[i].y != 0.f) L = fmaf(__builtin_amdgcn_exp2f(r[i].x - M), r[i].y, L);
             L = sum_xor32(sum_xor16(L));
             b = M + __builtin_amdgcn_logf(L);
@@ -826,8 +824,9 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Spans<CAP> t, cons
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kMostRanges
-// ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.
+// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kKv4Ranges
+// ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.  (Steps grow with the range: a long
+// context with few rows tries some dozen lengths, not thousands.)
 template <class F>
 static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F blocks_of) {
     const int64_t nq = k.c.n_q_heads;
@@ -839,9 +838,9 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
         work += (int64_t)blocks_of(t.s[j]) * tiles;
         most = tiles > most ? tiles : most;
     }
-    const int64_t least = (most + kMostRanges - 1) / kMostRanges, even = work / want;
+    const int64_t least = (most + kKv4Ranges - 1) / kKv4Ranges, even = work / want;
     int64_t per = ((even > least ? even : least) + step - 1) / step * step;
-    for (per = per ? per : step;; per += step) {
+    for (per = per ? per : step;; per += (per / 16 + step) / step * step) {
         int64_t blk = 0, part = 0;
         for (int j = 0; j < t.n; ++j) {
             Kv4Span &s = t.s[j];
@@ -855,11 +854,8 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
     }
 }
 
-void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf16_t *q, int64_t q_stride, bf16_t *out,
-                       int64_t out_stride, float *weights) {
-    const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv, D = k.c.head_dim;
-    const Kv4View view = k.view(layer);
-    float *lse = weights ? k.lse : nullptr;
+Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t) {
+    const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv;
     int64_t most = 0, few_tiles = 0, chunk_tiles = 0;
     for (int j = 0; j < t.n; ++j) {
         if (!t.s[j].rows) continue;
@@ -870,14 +866,24 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, int rows, const bf1
     }
     // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk, which takes some 14 us more to
     // get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
-    const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10, fused = weights && few && most <= 64;
-    const int cols_few = most <= 16 ? 16 : 32;  // columns of a block
-    auto groups = [&](const Kv4Span &s, int cols) { return nkv * ((s.rows * G + cols - 1) / cols); };
-    const int blocks = few ? cut_ranges(k, t, kFewTile, kFewWaves, most <= 16 ? 512 : 256, [&](const Kv4Span &s) { return groups(s, cols_few); })
-                           : cut_ranges(k, t, kTileKeys, 1, 512, [&](const Kv4Span &s) { return groups(s, kTileCols); });
-    int join = 0;  // rows of the longest span in several ranges
+    const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
+    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most};
+    auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
+    p.blocks = cut_ranges(k, t, few ? kFewTile : kTileKeys, few ? kFewWaves : 1, p.cols == 32 ? 256 : kKv4Blocks, groups);
     for (int j = 0; j < t.n; ++j)
-        if (t.s[j].splits > 1 && t.s[j].rows > join) join = t.s[j].rows;
+        if (t.s[j].splits > 1 && t.s[j].rows > p.join) p.join = t.s[j].rows;
+    return p;
+}
+
+void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
+                       float *weights) {
+    const int nkv = k.c.n_kv_heads, D = k.c.head_dim;
+    const Kv4View view = k.view(layer);
+    float *lse = weights ? k.lse : nullptr;
+    const Kv4AttendPlan plan = plan_kv4_attend(k, t);
+    const bool few = plan.cols < kTileCols, fused = weights && few && plan.most <= 64;
+    const int blocks = plan.blocks, join = plan.join;
+    const int64_t most = plan.most;
     with_table(t, [&](auto tab) {
         constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
         const int nq = k.c.n_q_heads, units = join * nq;

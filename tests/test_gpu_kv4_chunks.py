@@ -1,0 +1,137 @@
+"""Long chunks over the 4-bit cache: the form of attention whose blocks hold 128 columns, and the weights beside it, against 64 bits.  The tolerances are
+those of test_gpu_kv4; the reference goes by query heads, in float64 matrix products."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_12329_amd import binding as B
+
+from . import kv4_ref as R
+from .test_gpu_kv4 import WEIGHT_TOL, bf16, f64, ledger_for, make, out_tol, planes, put
+
+pytestmark = pytest.mark.gpu
+
+
+def attention(q, k, v, length):
+    """kv4_ref.attention, a query head at a time (float64 arrays; computed on the GPU)."""
+    rows, nq, d = q.shape
+    nkv, slots = k.shape[0], length + rows
+    q, k, v = (torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (q, k, v))
+    hidden = torch.arange(slots, device="cuda")[None] > length + torch.arange(rows, device="cuda")[:, None]
+    out, size = torch.empty_like(q), torch.empty_like(q)
+    got = torch.zeros(nkv, slots, dtype=torch.float64, device="cuda")
+    for h in range(nq):
+        kv = h // (nq // nkv)
+        p = (q[:, h].contiguous() @ k[kv].t().contiguous() / math.sqrt(d)).masked_fill_(hidden, -math.inf).softmax(1)
+        # (0 x NaN is NaN: slots that a row does not see are taken out of its sums)
+        odd = v[kv].isnan().any(1).nonzero().flatten()
+        clean = torch.where(v[kv].isnan(), 0.0, v[kv])
+        out[:, h], size[:, h] = p @ clean, p @ clean.abs()
+        for slot in odd.tolist():
+            out[max(slot - length, 0):, h, v[kv, slot].isnan()] = math.nan
+        got[kv] += p.masked_fill(hidden, 0.0).sum(0)
+    return out.cpu().numpy(), size.cpu().numpy(), got.cpu().numpy()
+
+
+def check(got, want, tol):
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    err = np.where(np.isnan(want), 0, np.abs(got - want) / np.maximum(tol, 1e-300))
+    err[~np.isnan(want) & (tol == 0) & (got == want)] = 0
+    assert err.max() <= 1, (err.max(), np.unravel_index(err.argmax(), err.shape))
+
+
+def run(kv, spans, rng, q_pad=0, scale=0.3, with_ledger=True, spoil=None):
+    c = kv.cfg
+    nq, d, rows = c["n_q_heads"], c["head_dim"], sum(s[3] for s in spans)
+    kvs = {seq: put(kv, 0, seq, n + r, rng) for seq, n, _, r in spans}
+    if spoil:
+        spoil(planes(kv), kvs)
+    wide = bf16(rng.standard_normal((rows, nq * d + q_pad)) * scale)
+    led = ledger_for(kv, rng) if with_ledger else None
+    before = f64(led.weights) if led else None
+    out = torch.full((rows, nq * d + q_pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    kv.attend(0, B.Kv4Spans(spans), wide[:, :nq * d], led, out=out[:, :nq * d])
+    assert (out[:, nq * d:] == 7).all()
+    got, q, at = f64(out[:, :nq * d]).reshape(rows, nq, d), f64(wide[:, :nq * d]).reshape(rows, nq, d), 0
+    for seq, n, _, r in spans:
+        if r:
+            want, size, w = attention(q[at:at + r], *kvs[seq], n)
+            check(got[at:at + r], want, out_tol(want, size))
+            if led:
+                before[0, seq, :, :n + r] += w
+        at += r
+    if led:
+        check(f64(led.weights), before, WEIGHT_TOL * np.abs(before))
+
+
+def test_the_reference_is_the_plain_one():
+    rng = np.random.default_rng(0)
+    q, k, v = (rng.standard_normal(s) for s in ((5, 4, 64), (2, 12, 64), (2, 12, 64)))
+    v[1, 9, 32:] = math.nan
+    k[0, 11] = math.nan
+    for a, b in zip(attention(q, k, v, 7), R.attention(q, k, v, 7)):
+        fine = ~np.isnan(b)
+        if a.shape == b.shape and a.ndim == 3 and np.isnan(b).any():
+            assert np.allclose(a[fine], b[fine], rtol=1e-12, atol=1e-14)
+        else:
+            assert np.allclose(a[fine], b[fine], rtol=1e-12, atol=1e-14) and np.array_equal(np.isnan(a), np.isnan(b))
+
+
+SHAPES = [                                               # and whether the slots are cut into ranges
+    (40, 8, 128, [(1, 1490, 0, 523)], True),
+    (14, 2, 64, [(0, 0, 0, 1100), (2, 777, 0, 901), (1, 5, 0, 0), (3, 3000, 0, 300)], True),
+    (5, 5, 128, [(0, 9000, 0, 768)], True),
+    (16, 1, 64, [(0, 8003, 0, 300)], True),
+    (16, 1, 128, [(1, 3, 0, 1500), (0, 1, 0, 1501)], False),    # little but the diagonal
+    (40, 8, 64, [(0, 0, 0, 1300)], False),
+    (1, 1, 128, [(0, 5000, 0, 6500)], True),
+]
+
+
+@pytest.mark.parametrize("nq,nkv,d,spans,cut", SHAPES)
+def test_chunks(nq, nkv, d, spans, cut):
+    print("chunks", nq, nkv, d, spans, flush=True)
+    rng = np.random.default_rng(nq)
+    slots = max(n + r for _, n, _, r in spans) + 3
+    kv = make(nq, nkv, d, n_seq=4, max_seq=slots, max_rows=sum(s[3] for s in spans), max_pos=64, fill=0xff)
+    columns, _, ranges = kv.attend_plan(B.Kv4Spans(spans))
+    assert columns == 128 and (max(ranges) > 1) == cut, (columns, ranges)
+    run(kv, spans, rng, q_pad=24)
+    run(kv, spans, rng, with_ledger=False, scale=2.0)
+
+
+@pytest.mark.parametrize("nq,nkv,d,n,rows", [(40, 8, 128, 1490, 523), (14, 2, 64, 1500, 1600), (5, 5, 128, 9000, 768)])
+@pytest.mark.parametrize("side", [0, 1])
+def test_chunks_with_groups_without_numbers(nq, nkv, d, n, rows, side):
+    """In a slot that every row sees, in one on the diagonal and in the last one, each in another kv head."""
+    print("chunks, NaN in", "KV"[side], nq, nkv, d, flush=True)
+    rng = np.random.default_rng(d + side)
+    kv = make(nq, nkv, d, n_seq=2, max_seq=n + rows + 1, max_rows=rows, max_pos=64, fill=0xff)
+    spans = [(1, n, 0, rows)]
+    assert kv.attend_plan(B.Kv4Spans(spans))[0] == 128
+
+    def spoil(pl, kvs):
+        for i, (slot, group) in enumerate(((70, 1), (n + rows // 2 + 1, 0), (n + rows - 1, d // 32 - 1))):
+            h = i % nkv
+            pl[side][0, 1, h, slot, 16 * group:16 * group + 16] = 0
+            pl[2 + side][0, 1, h, slot, group] = 255
+            kvs[1][side][h, slot, 32 * group:32 * group + 32] = math.nan
+
+    # A key without numbers leaves the rows that see it without: all of head 0, so its weights say nothing about the others'.
+    run(kv, spans, rng, spoil=spoil)
+
+
+def test_forms_of_neighbouring_sizes_agree():
+    """Rows on both sides of the switch between the forms, one context: what a row gets does not depend on its company but for rounding."""
+    print("both forms", flush=True)
+    rng = np.random.default_rng(3)
+    kv = make(40, 8, 128, n_seq=1, max_seq=4700, max_rows=600, max_pos=64)
+    put(kv, 0, 0, 4700, rng)
+    q = bf16(rng.standard_normal((600, 40 * 128)) * 0.3)
+    spans = [B.Kv4Spans([(0, 4100, 0, r)]) for r in (100, 600)]
+    assert [kv.attend_plan(s)[0] for s in spans] == [32, 128]
+    a, b = (f64(kv.attend(0, s, q[:s.rows])) for s in spans)
+    # each lies within 2^-8 (sum p |v| + |out|) of the exact value, and |v| <= 6
+    assert np.abs(a - b[:100]).max() <= 2 * (2.0 ** -8 + 2.0 ** -15) * 6 + 2.0 ** -7 * np.abs(a).max()

@@ -151,3 +151,43 @@ def test_calls_with_nothing_to_do(L, kv):
     assert L.st_kv4_read(kv, 0, 3, none, n, PTR, PTR) == B.ST_OK
     assert L.st_kv4_evict(kv, 1, 1, none, n, 5, 0, C.byref(led), None) == B.ST_OK
     assert L.st_kv4_evict(kv, 0, 3, None, 0, 5, 0, C.byref(led), None) == B.ST_OK
+
+
+def plan(L, c, s, n):
+    columns, blocks, ranges = C.c_int32(-1), C.c_int32(-1), (C.c_int32 * 64)(*[-1] * 64)
+    rc = L.st_kv4_attend_plan(C.byref(c), s, n, C.byref(columns), C.byref(blocks), ranges)
+    return rc, columns.value, blocks.value, list(ranges)[:max(n, 0)]
+
+
+def test_attend_plan(L):
+    c = config(n_q_heads=40, n_kv_heads=8, n_seq=64, max_seq=1 << 20, max_rows=1 << 16)
+    assert plan(L, c, None, 0) == (B.ST_OK, 0, 0, [])
+    assert plan(L, c, *spans((3, 9, 0, 0))) == (B.ST_OK, 0, 0, [0])
+    rc, columns, blocks, ranges = plan(L, c, *spans((0, 1 << 19, 0, 1)))
+    assert rc == B.ST_OK and columns == 16 and ranges == [64] and blocks == 8 * 64
+    assert plan(L, c, *spans((0, 0, 0, 1)))[1:] == (16, 8, [1])
+    assert plan(L, c, *spans((0, 100, 0, 20), (1, 0, 0, 0)))[1] == 32
+    assert plan(L, c, *spans((0, 0, 0, 1 << 16)))[1:] == (128, 8 * (1 << 16) * 5 // 128, [1])
+    assert L.st_kv4_attend_plan(C.byref(c), *spans((0, 5, 0, 1)), None, None, None) == B.ST_OK
+    assert plan(L, config(head_dim=96), *spans((0, 0, 0, 1)))[0] == B.ST_EINVAL
+    assert L.st_kv4_attend_plan(None, None, 0, None, None, None) == B.ST_EINVAL
+    for bad, code in BAD_SPANS:
+        assert plan(L, config(), *spans(*bad))[0] == code
+
+
+def test_ranges_stay_within_what_the_workspace_holds(L):
+    """Wherever slots are cut into ranges: at most 512 blocks, 64 ranges of a span, and partial results for every row and head."""
+    for nq, nkv in ((1, 1), (12, 2), (40, 8), (16, 1), (4096, 256)):
+        for max_rows in (1, 7, 64, 5000):
+            c = config(n_layers=1, n_q_heads=nq, n_kv_heads=nkv, n_seq=64, max_seq=1 << 22, max_rows=max_rows)
+            held = min(max_rows * nq * 64, 512 * 128)
+            for n in (1, 3, 64):
+                for rows in (1, 2, max_rows // n):
+                    for length in (0, 31, 4097, 1 << 21):
+                        if rows < 1 or rows * n > max_rows:
+                            continue
+                        rc, columns, blocks, ranges = plan(L, c, *spans(*((j, length if j % 2 == 0 else length // 3, 0, rows) for j in range(n))))
+                        cut = [r for r in ranges if r > 1]
+                        assert rc == B.ST_OK and min(ranges) >= 1 and max(ranges) <= 64
+                        assert blocks == sum(r * nkv * -(-rows * (nq // nkv) // columns) for r in ranges)
+                        assert not cut or (blocks <= 512 and sum(cut) * rows * nq <= held), (nq, nkv, max_rows, n, rows, length)
