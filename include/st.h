@@ -450,9 +450,10 @@ int st_kv4_append(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n,
 int st_kv4_attend(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *q, int64_t q_stride, void *out,
                   int64_t out_stride, const st_kv4_ledger *ledger);
 
-/* Host only: how such a call of st_kv4_attend is dealt out.  columns: rows x query heads of one kv head that a block works on (16, 32 or 128, each a kernel
+/* Host only: how such a call of st_kv4_attend, with or without a ledger, is dealt out.  columns: rows x query heads of one kv head that a block works on (16, 32 or 128, each a kernel
  * of its own); blocks: of the first launch; ranges[n]: the parts each span's slots are cut into.  Each may be NULL; a call without rows has 0 of each. */
-int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t *columns, int32_t *blocks, int32_t *ranges);
+int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t with_ledger, int32_t *columns, int32_t *blocks,
+                       int32_t *ranges);
 
 /* Eviction: in layers [layer_lo, layer_hi) every kv head of the spans' sequences that has more than `keep` slots (span: len; rows is 0) is brought to
  * `keep` of them.  Those at positions >= pos - recent stay (pos: the sequence's next position); of the others those of the largest weight,

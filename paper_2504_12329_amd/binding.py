@@ -145,7 +145,7 @@ def lib():
                                     C.c_void_p, C.c_int64, ledger]
         L.st_kv4_attend.argtypes = [C.c_void_p, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                     ledger]
-        L.st_kv4_attend_plan.argtypes = [C.POINTER(st_kv4_config), spans, C.c_int32] + [C.POINTER(C.c_int32)] * 3
+        L.st_kv4_attend_plan.argtypes = [C.POINTER(st_kv4_config), spans, C.c_int32, C.c_int32] + [C.POINTER(C.c_int32)] * 3
         L.st_kv4_evict.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_int32, C.c_int32, ledger, ledger]
         L.st_kv4_read.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_void_p]
         _lib = L
@@ -675,11 +675,11 @@ class Kv4Cache:
                 _check(rc)
         return out
 
-    def attend_plan(self, spans):
-        """(columns of a block, blocks, key ranges of every span) of attend(..., spans, ...) (see st_kv4_attend_plan)."""
+    def attend_plan(self, spans, with_ledger=False):
+        """(columns of a block, blocks, key ranges of every span) of such an attend (see st_kv4_attend_plan)."""
         c = st_kv4_config(*(self.cfg[n] for n, _ in st_kv4_config._fields_))
         columns, blocks, ranges = C.c_int32(), C.c_int32(), (C.c_int32 * max(spans.n, 1))()
-        _check(lib().st_kv4_attend_plan(C.byref(c), spans.c, spans.n, C.byref(columns), C.byref(blocks), ranges))
+        _check(lib().st_kv4_attend_plan(C.byref(c), spans.c, spans.n, int(with_ledger), C.byref(columns), C.byref(blocks), ranges))
         return columns.value, blocks.value, list(ranges)[:spans.n]
 
     def evict(self, layer_lo, layer_hi, spans, keep, recent, ledger, into=None):

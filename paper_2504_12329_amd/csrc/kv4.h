@@ -72,8 +72,9 @@ struct Kv4AttendPlan {
     int blocks;
     int join;      // rows of the longest span in several ranges, 0 without one
     int64_t most;  // columns of a kv head in the span with most rows
+    bool fused;    // the ranges are joined by the kernel that sums up the weights
 };
-Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t);
+Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights);
 
 // All enqueue only; the arguments have been checked.  `t` holds spans and row0; the launchers fill in the rest.
 void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, const bf16_t *qkv, int64_t qkv_stride,

@@ -358,7 +358,8 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     return launched("st_kv4_attend");
 }
 
-int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t *columns, int32_t *blocks, int32_t *ranges) {
+int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t with_ledger, int32_t *columns, int32_t *blocks,
+                       int32_t *ranges) {
     if (int rc = check_config(cfg)) return rc;
     Kv4 k{};
     size_t cb, wb;
@@ -368,7 +369,7 @@ int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32
     carve(*cfg, nullptr, nullptr, &k, &cb, &wb);
     if (int rc = take_spans(k, spans, n, false, &t, &rows)) return rc;
     if (int rc = check_rows(k, rows)) return rc;
-    const Kv4AttendPlan p = plan_kv4_attend(k, t);
+    const Kv4AttendPlan p = plan_kv4_attend(k, t, with_ledger != 0);
     if (columns) *columns = rows ? p.cols : 0;
     if (blocks) *blocks = rows ? p.blocks : 0;
     for (int j = 0; ranges && j < n; ++j) ranges[j] = t.s[j].rows ? t.s[j].splits : 0;

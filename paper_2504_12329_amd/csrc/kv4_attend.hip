@@ -824,11 +824,11 @@ __global__ __launch_bounds__(256) void k_kv4_weights(const Kv4Spans<CAP> t, cons
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`), as short as leaves at most `want` blocks, kKv4Ranges
+// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`, at least `whole` of them if no span has more), as short as leaves at most `want` blocks, kKv4Ranges
 // ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.  (Steps grow with the range: a long
 // context with few rows tries some dozen lengths, not thousands.)
 template <class F>
-static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F blocks_of) {
+static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int whole, int want, F blocks_of) {
     const int64_t nq = k.c.n_q_heads;
     int64_t work = 0;
     int most = 1;
@@ -840,6 +840,7 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
     }
     const int64_t least = (most + kKv4Ranges - 1) / kKv4Ranges, even = work / want;
     int64_t per = ((even > least ? even : least) + step - 1) / step * step;
+    if (most <= whole && per < whole) per = whole;
     for (per = per ? per : step;; per += (per / 16 + step) / step * step) {
         int64_t blk = 0, part = 0;
         for (int j = 0; j < t.n; ++j) {
@@ -854,7 +855,7 @@ static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int want, F
     }
 }
 
-Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t) {
+Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
     const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv;
     int64_t most = 0, few_tiles = 0, chunk_tiles = 0;
     for (int j = 0; j < t.n; ++j) {
@@ -867,9 +868,12 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t) {
     // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk, which takes some 14 us more to
     // get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
     const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
-    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most};
+    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, few && weights && most <= 64};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
-    p.blocks = cut_ranges(k, t, few ? kFewTile : kTileKeys, few ? kFewWaves : 1, p.cols == 32 ? 256 : kKv4Blocks, groups);
+    // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us against 6.5, on 512 6.2
+    // against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7 against 6.7.)
+    const int whole = few && !p.fused ? 512 / kFewTile : 0;
+    p.blocks = cut_ranges(k, t, few ? kFewTile : kTileKeys, few ? kFewWaves : 1, whole, p.cols == 32 ? 256 : kKv4Blocks, groups);
     for (int j = 0; j < t.n; ++j)
         if (t.s[j].splits > 1 && t.s[j].rows > p.join) p.join = t.s[j].rows;
     return p;
@@ -880,8 +884,8 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
     const int nkv = k.c.n_kv_heads, D = k.c.head_dim;
     const Kv4View view = k.view(layer);
     float *lse = weights ? k.lse : nullptr;
-    const Kv4AttendPlan plan = plan_kv4_attend(k, t);
-    const bool few = plan.cols < kTileCols, fused = weights && few && plan.most <= 64;
+    const Kv4AttendPlan plan = plan_kv4_attend(k, t, weights);
+    const bool few = plan.cols < kTileCols, fused = plan.fused;
     const int blocks = plan.blocks, join = plan.join;
     const int64_t most = plan.most;
     with_table(t, [&](auto tab) {

@@ -51,7 +51,7 @@ int main() {
                     for (int j = 0; j < n; ++j)
                         s[j] = {n - 1 - j, (int32_t)(j % 3 == 2 ? len / 2 : len), 0, (int32_t)(j % 4 == 3 ? 0 : rows)};
                     int32_t columns = -1, blocks = -1;
-                    const int rc = st_kv4_attend_plan(&c, s.data(), n, &columns, &blocks, ranges.data());
+                    const int rc = st_kv4_attend_plan(&c, s.data(), n, len % 2, &columns, &blocks, ranges.data());
                     CHECK(rc == ST_OK || (rc == ST_ERANGE && rows * n > c.max_rows * 3 / 4));
                     CHECK(rc != ST_OK || (blocks >= 0 && (columns == 0) == (blocks == 0)));
                 }
@@ -69,7 +69,7 @@ int main() {
                             CHECK(st_kv4_attend(h, 0, &s, 1, p, 1 << 20, p, 1 << 20, &led) == ST_ERANGE);
                             CHECK(st_kv4_read(h, 0, 1, &s, 1, p, p) == ST_ERANGE);
                             CHECK(st_kv4_evict(h, 0, 1, &s, 1, 1, 0, &led, nullptr) == ST_ERANGE);
-                            CHECK(st_kv4_attend_plan(&c, &s, 1, nullptr, nullptr, nullptr) == ST_ERANGE);
+                            CHECK(st_kv4_attend_plan(&c, &s, 1, 0, nullptr, nullptr, nullptr) == ST_ERANGE);
                         } else if (rows) {
                             CHECK(st_kv4_evict(h, 0, 1, &s, 1, 1, 0, &led, nullptr) == (rows < 1 << 24 ? ST_EINVAL : ST_ERANGE));
                         }

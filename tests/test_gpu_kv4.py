@@ -277,6 +277,20 @@ def test_attend_long_and_peaked(d):
         check_attend(kv, 0, [(1, 2111, 0, 41), (0, 77, 0, 3)], rng, scale=scale)
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(12, 2, 128), (4, 2, 64), (5, 5, 128)])
+@pytest.mark.parametrize("rows", [1, 9])
+def test_attend_where_ranges_begin(nq, nkv, d, rows):
+    """Contexts that stay in one range without a ledger, and the first that do not; with a ledger they are cut, and joined beside the weights."""
+    print("attend: one range or several", nq, nkv, d, rows, flush=True)
+    rng = np.random.default_rng(nq + rows)
+    kv = make(nq, nkv, d, n_seq=2, max_seq=640, fill=0xff)
+    for held, ranges in ((rows, 1), (128, 1), (129, 1), (511, 1), (512, 1), (513, 5), (620, 5)):
+        spans = [(1, held - rows, 0, rows), (0, 2, 0, rows)]
+        assert kv.attend_plan(B.Kv4Spans(spans))[2][0] == ranges
+        for with_ledger in (False, True):
+            check_attend(kv, 0, spans, rng, with_ledger)
+
+
 def test_attend_many_spans():
     print("attend: 64 spans", flush=True)
     rng = np.random.default_rng(9)

@@ -153,9 +153,9 @@ def test_calls_with_nothing_to_do(L, kv):
     assert L.st_kv4_evict(kv, 0, 3, None, 0, 5, 0, C.byref(led), None) == B.ST_OK
 
 
-def plan(L, c, s, n):
+def plan(L, c, s, n, ledger=0):
     columns, blocks, ranges = C.c_int32(-1), C.c_int32(-1), (C.c_int32 * 64)(*[-1] * 64)
-    rc = L.st_kv4_attend_plan(C.byref(c), s, n, C.byref(columns), C.byref(blocks), ranges)
+    rc = L.st_kv4_attend_plan(C.byref(c), s, n, ledger, C.byref(columns), C.byref(blocks), ranges)
     return rc, columns.value, blocks.value, list(ranges)[:max(n, 0)]
 
 
@@ -167,10 +167,12 @@ def test_attend_plan(L):
     assert rc == B.ST_OK and columns == 16 and ranges == [64] and blocks == 8 * 64
     assert plan(L, c, *spans((0, 0, 0, 1)))[1:] == (16, 8, [1])
     assert plan(L, c, *spans((0, 100, 0, 20), (1, 0, 0, 0)))[1] == 32
+    assert plan(L, c, *spans((0, 511, 0, 1), (1, 0, 0, 1)))[3] == [1, 1] and plan(L, c, *spans((0, 512, 0, 1), (1, 0, 0, 1)))[3] == [5, 1]
+    assert plan(L, c, *spans((0, 511, 0, 1), (1, 0, 0, 1)), ledger=1)[3] == [4, 1]     # joined beside the weights
     assert plan(L, c, *spans((0, 0, 0, 1 << 16)))[1:] == (128, 8 * (1 << 16) * 5 // 128, [1])
-    assert L.st_kv4_attend_plan(C.byref(c), *spans((0, 5, 0, 1)), None, None, None) == B.ST_OK
+    assert L.st_kv4_attend_plan(C.byref(c), *spans((0, 5, 0, 1)), 0, None, None, None) == B.ST_OK
     assert plan(L, config(head_dim=96), *spans((0, 0, 0, 1)))[0] == B.ST_EINVAL
-    assert L.st_kv4_attend_plan(None, None, 0, None, None, None) == B.ST_EINVAL
+    assert L.st_kv4_attend_plan(None, None, 0, 0, None, None, None) == B.ST_EINVAL
     for bad, code in BAD_SPANS:
         assert plan(L, config(), *spans(*bad))[0] == code
 
@@ -186,7 +188,8 @@ def test_ranges_stay_within_what_the_workspace_holds(L):
                     for length in (0, 31, 4097, 1 << 21):
                         if rows < 1 or rows * n > max_rows:
                             continue
-                        rc, columns, blocks, ranges = plan(L, c, *spans(*((j, length if j % 2 == 0 else length // 3, 0, rows) for j in range(n))))
+                        s = spans(*((j, length if j % 2 == 0 else length // 3, 0, rows) for j in range(n)))
+                        rc, columns, blocks, ranges = plan(L, c, *s, ledger=rows % 2)
                         cut = [r for r in ranges if r > 1]
                         assert rc == B.ST_OK and min(ranges) >= 1 and max(ranges) <= 64
                         assert blocks == sum(r * nkv * -(-rows * (nq // nkv) // columns) for r in ranges)
