@@ -122,25 +122,42 @@ __global__ __launch_bounds__(256) void k_kv4_append(const Kv4Spans<CAP> t, const
 
 // ---------------------------------------------------------------------------------------
 // Read: slots [len, len + rows) of every span as the bf16 numbers they stand for (each is one exactly).  A thread turns four bytes of codes into
-// 16 of output.
+// 16 of output; 1 << shift waves have RPW rows, so that heads too few for a block share it with other rows.  Bound by memory.
 // ---------------------------------------------------------------------------------------
-template <int D, int CAP>
-__global__ __launch_bounds__(256) void k_kv4_read(const Kv4Spans<CAP> t, Kv4View view, size_t k_layer, size_t s_layer, int rows,
+template <int D, int RPW, int CAP>
+__global__ __launch_bounds__(256) void k_kv4_read(const Kv4Spans<CAP> t, Kv4View view, size_t k_layer, size_t s_layer, int rows, int shift,
                                                   bf16_t *__restrict__ k_out, bf16_t *__restrict__ v_out) {
     constexpr int TPH = D / 8;
-    const int row = blockIdx.x, layer = blockIdx.y;
-    const Kv4Span sp = t.s[kv4_span_of(t, row)];
-    const size_t slot = (size_t)sp.len + (row - sp.row0), out0 = ((size_t)layer * rows + row) * view.nkv * D;
-    for (int u = threadIdx.x; u < 2 * view.nkv * TPH; u += 256) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), layer = blockIdx.y;
+    const int first = (((blockIdx.x << 2) + wave) >> shift) * RPW;
+    size_t slot[RPW];
+#pragma unroll
+    for (int r = 0; r < RPW; ++r) {
+        const int row = min(first + r, rows - 1);
+        const Kv4Span sp = t.s[kv4_span_of(t, row)];
+        slot[r] = (size_t)sp.seq * view.nkv * view.max_seq + sp.len + (row - sp.row0);
+    }
+    for (int u = (wave & ((1 << shift) - 1)) * 64 + (threadIdx.x & 63); u < 2 * view.nkv * TPH; u += 64 << shift) {
         const bool is_k = u < view.nkv * TPH;
         const int x = is_k ? u : u - view.nkv * TPH, head = x / TPH, l = x % TPH;
-        const size_t at = ((size_t)sp.seq * view.nkv + head) * view.max_seq + slot;
-        const uint32_t w = *reinterpret_cast<const uint32_t *>((is_k ? view.k : view.v) + layer * k_layer + at * (D / 2) + 4 * l);
-        const uint32_t byte = ((is_k ? view.ks : view.vs) + layer * s_layer)[at * (D / 32) + (l >> 2)];
-        const float unit = kv4_scale(byte);
-        u32x4 o = {kv4_pair<0>(w, unit), kv4_pair<1>(w, unit), kv4_pair<2>(w, unit), kv4_pair<3>(w, unit)};
-        if (byte == kKv4Nan) o = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-        *reinterpret_cast<u32x4 *>((is_k ? k_out : v_out) + out0 + head * D + 8 * l) = o;
+        const uint8_t *codes = (is_k ? view.k : view.v) + layer * k_layer + 4 * l;
+        const uint8_t *scales = (is_k ? view.ks : view.vs) + layer * s_layer + (l >> 2);
+        bf16_t *out = (is_k ? k_out : v_out) + ((size_t)layer * rows + first) * view.nkv * D + head * D + 8 * l;
+        uint32_t w[RPW], byte[RPW];
+#pragma unroll
+        for (int r = 0; r < RPW; ++r) {
+            const size_t at = slot[r] + (size_t)head * view.max_seq;
+            w[r] = *reinterpret_cast<const uint32_t *>(codes + at * (D / 2));
+            byte[r] = scales[at * (D / 32)];
+        }
+#pragma unroll
+        for (int r = 0; r < RPW; ++r) {
+            if (first + r >= rows) break;
+            const float unit = kv4_scale(byte[r]);
+            u32x4 o = {kv4_pair<0>(w[r], unit), kv4_pair<1>(w[r], unit), kv4_pair<2>(w[r], unit), kv4_pair<3>(w[r], unit)};
+            if (byte[r] == kKv4Nan) o = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+            *reinterpret_cast<u32x4 *>(out + (size_t)r * view.nkv * D) = o;
+        }
     }
 }
 
@@ -164,12 +181,17 @@ void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, con
 }
 
 void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out) {
+    const int units = 2 * k.c.n_kv_heads * (k.c.head_dim / 8), shift = units > 128 ? 2 : units > 64 ? 1 : 0, layers = layer_hi - layer_lo;
+    // Two rows a wave once that leaves the chip full: 16 x 1024 rows of 8 heads 16.8 us against 19.8 (5.1 TB/s), 28 x 512 of 2 heads 5.8 against 6.2; 12 x 35 of 4
+    // heads 2.8 against 2.5.
+    const bool many = (int64_t)rows * layers << shift >= 12288;
+    const int groups = many ? (rows + 1) / 2 : rows;
     with_table(t, [&](auto tab) {
         constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
-        auto *kern = k.c.head_dim == 128 ? k_kv4_read<128, CAP> : k_kv4_read<64, CAP>;
+        auto *kern = k.c.head_dim == 128 ? (many ? k_kv4_read<128, 2, CAP> : k_kv4_read<128, 1, CAP>) : (many ? k_kv4_read<64, 2, CAP> : k_kv4_read<64, 1, CAP>);
         by_rows(tab);
-        hipLaunchKernelGGL(kern, dim3(rows, layer_hi - layer_lo), dim3(256), 0, k.stream, tab, k.view(layer_lo), k.per_layer[0],
-                           k.per_layer[2], rows, k_out, v_out);
+        hipLaunchKernelGGL(kern, dim3((((int64_t)groups << shift) + 3) / 4, layers), dim3(256), 0, k.stream, tab, k.view(layer_lo), k.per_layer[0],
+                           k.per_layer[2], rows, shift, k_out, v_out);
     });
 }
 

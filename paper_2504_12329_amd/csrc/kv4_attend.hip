@@ -741,7 +741,7 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
 // Chunks: the weight each slot received, sum over the columns that see it of exp2(score - lse), the scores formed once more (K only).  A block
 // is 64 slots, its keys in registers as bf16; its W waves take every W-th tile of 32 columns, S = Q K^T, so that a lane has one slot and
 // the sum over the columns stays in the lane.  One block owns a slot's sum: no atomics, the same order in every run.  Bound by the matrix and the
-// vector pipe in turn (an exponential and two more operations a score): 2048 rows of 40 / 8 heads on 4096 slots 212 us, 0.62 PFLOP/s; 86 rows 13.5 us.
+// vector pipe in turn (an exponential and two more operations a score): 2048 rows of 40 / 8 heads on 4096 slots 212 us, 0.51 PFLOP/s; 86 rows 13.5 us.
 // ---------------------------------------------------------------------------------------
 constexpr int kWeightKeys = 64;
 

@@ -239,6 +239,21 @@ def test_the_codes_do_not_depend_on_how_rows_are_dealt():
         assert torch.equal(a[0, 0, :, :33], b[0, 0, :, :33])
 
 
+@pytest.mark.parametrize("nkv,d,rows", [(1, 64, 4100), (1, 128, 77), (2, 128, 2050), (3, 128, 1501), (8, 128, 1025), (5, 64, 33)])
+def test_read(nkv, d, rows):
+    """Rows that fill the chip (two a wave) and rows that do not, an odd number of them, in spans that do not start with the sequence."""
+    print("read", nkv, d, rows, flush=True)
+    rng = np.random.default_rng(rows)
+    kv = make(nkv, nkv, d, n_seq=5, max_seq=rows + 9, n_layers=4)
+    held = {(layer, seq): put(kv, layer, seq, rows + 9, rng) for layer in (1, 2, 3) for seq in (0, 3, 4)}
+    spans = [(3, 9, 0, rows), (1, 5, 0, 0), (0, 0, 0, 1), (4, 7, 0, rows - rows % 2)]
+    got = kv.read(1, 4, B.Kv4Spans(spans))
+    for layer in (1, 2, 3):
+        for side in (0, 1):
+            want = np.concatenate([held[layer, seq][side][:, n:n + r] for seq, n, _, r in spans if r], 1).transpose(1, 0, 2)
+            assert np.array_equal(f64(got[side][layer - 1]), want)
+
+
 # ---- attend ----
 
 @pytest.mark.parametrize("nq,nkv,d", [(1, 1, 128), (4, 2, 64), (10, 2, 128), (7, 1, 128), (16, 1, 64), (32, 2, 128)])
