@@ -440,12 +440,12 @@ void st_kv4_destroy(st_kv4 *c);
  * of their head (rms_eps inside the root) and multiplied by the norm.  Rotated queries go to q_out (bf16, n_q_heads * head_dim a row, rows
  * q_stride apart), rotated keys and the values to slots [len, len + rows).  Every operation rounds to fp32 by itself and the sum of squares adds
  * neighbours first, so the codes depend on nothing but the inputs.  With a ledger the new slots' weights become 0 and their positions are noted.
- * Matrices are 16-byte aligned with strides that are multiples of 8.  ST_ERANGE: a span outside the cache or the table, too many rows. */
+ * Matrices are 16-byte aligned with strides that are multiples of 8, and share no memory.  ST_ERANGE: a span outside the cache or the table, too many rows. */
 int st_kv4_append(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *qkv, int64_t qkv_stride,
                   const void *q_norm, const void *k_norm, void *q_out, int64_t q_stride, const st_kv4_ledger *ledger);
 
 /* Causal attention over the cache: row i of a span attends to slots [0, len + i] of its sequence, those of the span's own rows, appended before,
- * among them; scores are scaled by head_dim^-1/2.  q, out: bf16, n_q_heads * head_dim a row.  With a ledger the weight of every slot
+ * among them; scores are scaled by head_dim^-1/2.  q, out: bf16, n_q_heads * head_dim a row; they share no memory.  With a ledger the weight of every slot
  * grows by the attention it received, summed over the rows and over the query heads of its kv head, in an order that does not change from run to run. */
 int st_kv4_attend(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *q, int64_t q_stride, void *out,
                   int64_t out_stride, const st_kv4_ledger *ledger);
@@ -459,7 +459,8 @@ int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32
  * `keep` of them.  Those at positions >= pos - recent stay (pos: the sequence's next position); of the others those of the largest weight,
  * equal weights by the lower position, a NaN below every weight.  The slots below `keep` that are freed take, in ascending order, the slots at or above it that stay, in
  * ascending order; nothing else moves.  Pass len = keep from then on.  The ledger's entries move along: in `ledger` itself if `into` is
- * NULL, else to the slots [0, min(len, keep)) of `into`, and `ledger` stays as it was.  ST_EINVAL: keep <= 0, recent outside [0, keep]. */
+ * NULL, else to the slots [0, min(len, keep)) of `into`, and `ledger` stays as it was.  ST_EINVAL: keep <= 0, recent outside [0, keep],
+ * `into` and `ledger` overlap in part. */
 int st_kv4_evict(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, int32_t keep,
                  int32_t recent, const st_kv4_ledger *ledger, const st_kv4_ledger *into);
 

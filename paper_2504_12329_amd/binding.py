@@ -575,14 +575,17 @@ class Kv4Cache:
                 tuple(rope.shape) != (cfg["max_pos"], cfg["head_dim"] // 2, 2):
             raise StError(ST_EINVAL, f"rope is a contiguous float32 CUDA tensor [max_pos][head_dim / 2][2], got {rope.dtype} {tuple(rope.shape)}")
         dev = rope.device           # (with its index)
-        if cache is None:
-            cache = torch.empty(cb.value, dtype=torch.uint8, device=dev)
-        elif cache.device != dev or cache.dtype != torch.uint8 or not cache.is_contiguous():
-            raise StError(ST_EINVAL, "cache is a contiguous uint8 tensor on the device of rope")
-        self.cache, self.rope, self._dev = cache, rope, dev
-        self._ws = torch.empty(wb.value, dtype=torch.uint8, device=dev)
         self._own_stream = stream is not None
         self.stream = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
+        # what is allocated here belongs to the stream that uses it: freed, it does not go to another one while calls are still running
+        on = torch.cuda.ExternalStream(self.stream, device=dev) if self._own_stream else torch.cuda.current_stream(dev)
+        with torch.cuda.stream(on):
+            self._ws = torch.empty(wb.value, dtype=torch.uint8, device=dev)
+            if cache is None:
+                cache = torch.empty(cb.value, dtype=torch.uint8, device=dev)
+        if cache.device != dev or cache.dtype != torch.uint8 or not cache.is_contiguous():
+            raise StError(ST_EINVAL, "cache is a contiguous uint8 tensor on the device of rope")
+        self.cache, self.rope, self._dev = cache, rope, dev
         h = C.c_void_p()
         _check(lib().st_kv4_create(C.byref(c), rope.data_ptr(), cache.data_ptr(), cache.numel(), self._ws.data_ptr(),
                                    wb.value, self.stream, C.byref(h)))

@@ -285,6 +285,19 @@ static int check_matrix(const char *name, const void *p, int64_t stride, int64_t
     if (stride < width || stride % 8) return fail(ST_EINVAL, "%s: row stride %lld, needs a multiple of 8 from %lld on", name, (long long)stride, (long long)width);
     return ST_OK;
 }
+// Matrices of `rows` rows, read and written by one call, must not share memory; with one stride they may be columns side by side.
+static int check_apart(const char *in_name, const void *in, int64_t in_stride, int64_t in_width, const char *out_name, const void *out,
+                       int64_t out_stride, int64_t out_width, int rows) {
+    if (!rows) return ST_OK;
+    const uintptr_t i0 = (uintptr_t)in, o0 = (uintptr_t)out;
+    const uintptr_t i1 = i0 + 2 * (((uintptr_t)rows - 1) * in_stride + in_width), o1 = o0 + 2 * (((uintptr_t)rows - 1) * out_stride + out_width);
+    if (i1 <= o0 || o1 <= i0) return ST_OK;
+    if (in_stride == out_stride) {
+        const int64_t d = ((int64_t)o0 - (int64_t)i0) / 2 % in_stride, at = d < 0 ? d + in_stride : d;  // column of in's rows that out starts at
+        if (at >= in_width && at + out_width <= in_stride) return ST_OK;
+    }
+    return fail(ST_EINVAL, "%s and %s share memory", in_name, out_name);
+}
 static int check_ledger(const st_kv4_ledger *l, const char *name) {
     if (!l->weights || !l->positions) return fail(ST_EINVAL, "%s: weights or positions is NULL", name);
     if (((uintptr_t)l->weights | (uintptr_t)l->positions) & 3) return fail(ST_EINVAL, "%s is not aligned to 4 bytes", name);
@@ -347,6 +360,7 @@ int st_kv4_append(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     if (int rc = check_rows(*k, rows)) return rc;
     if (int rc = check_matrix("qkv", qkv, qkv_stride, (k->c.n_q_heads + 2 * k->c.n_kv_heads) * d)) return rc;
     if (int rc = check_matrix("q_out", q_out, q_stride, k->c.n_q_heads * d)) return rc;
+    if (int rc = check_apart("qkv", qkv, qkv_stride, (k->c.n_q_heads + 2 * k->c.n_kv_heads) * d, "q_out", q_out, q_stride, k->c.n_q_heads * d, rows)) return rc;
     if (!q_norm != !k_norm) return fail(ST_EINVAL, "q_norm and k_norm are given together or not at all");
     if (((uintptr_t)q_norm | (uintptr_t)k_norm) & 7) return fail(ST_EINVAL, "the norms are not aligned to 8 bytes");
     if (ledger)
@@ -371,6 +385,7 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     if (int rc = check_rows(*k, rows)) return rc;
     if (int rc = check_matrix("q", q, q_stride, width)) return rc;
     if (int rc = check_matrix("out", out, out_stride, width)) return rc;
+    if (int rc = check_apart("q", q, q_stride, width, "out", out, out_stride, width, rows)) return rc;
     if (ledger)
         if (int rc = check_ledger(ledger, "ledger")) return rc;
     if (!rows) return ST_OK;
@@ -415,6 +430,13 @@ int st_kv4_evict(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_spa
     if (int rc = check_ledger(into, "into")) return rc;
     if ((into->weights == ledger->weights) != (into->positions == ledger->positions))
         return fail(ST_EINVAL, "into shares one array with ledger and not the other");
+    const size_t bytes = 4 * (size_t)k->c.n_layers * k->c.n_seq * k->c.n_kv_heads * k->c.max_seq;
+    auto partly = [&](const void *a, const void *b) {
+        const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+        return x != y && (x < y ? y - x : x - y) < bytes;
+    };
+    if (partly(into->weights, ledger->weights) || partly(into->positions, ledger->positions))
+        return fail(ST_EINVAL, "into and ledger overlap");
     if (!n || layer_lo == layer_hi) return ST_OK;
     launch_kv4_evict(*k, layer_lo, layer_hi, t, keep, recent, ledger->weights, ledger->positions, into->weights, into->positions);
     return launched("st_kv4_evict");

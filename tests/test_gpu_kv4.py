@@ -521,6 +521,21 @@ def test_streams():
     assert torch.equal(got, want)
 
 
+def test_what_a_cache_allocates_stays_with_its_stream():
+    """Freed while its calls may still run, the memory of a cache on a named stream is not handed to another stream."""
+    print("memory and streams", flush=True)
+    side = torch.cuda.Stream()
+    probe = make(4, 2, 64, max_seq=5000)
+    kv = B.Kv4Cache(probe.cfg, probe.rope, stream=side.cuda_stream)
+    was = {kv.cache.data_ptr(), kv._ws.data_ptr()}
+    sizes = kv.cache.numel(), kv._ws.numel()
+    del kv
+    assert not was & {torch.empty(n, dtype=torch.uint8, device="cuda").data_ptr() for n in sizes}
+    with torch.cuda.stream(side):
+        again = B.Kv4Cache(probe.cfg, probe.rope)
+    assert again.cache.data_ptr() in was
+
+
 def test_a_captured_step_replays():
     """Append, attend with weights and eviction in a HIP graph, replayed with new inputs between eager work."""
     print("graph", flush=True)
@@ -564,6 +579,27 @@ def test_a_captured_step_replays():
             torch.cuda.synchronize()
             assert torch.equal(out, want)
             assert all(torch.equal(a, b) for a, b in zip((kv.cache, led.weights, led.positions), state))
+
+
+def test_matrices_side_by_side():
+    """Queries and outputs as columns of one matrix, and appended rows beside the queries they become."""
+    print("one matrix", flush=True)
+    rng = np.random.default_rng(12)
+    nq, nkv, d = 4, 2, 64
+    kv = make(nq, nkv, d, fill=0xff)
+    w = (nq + 2 * nkv) * d
+    both = torch.zeros(5, w + 2 * nq * d, dtype=torch.bfloat16, device="cuda")
+    both[:, :w] = bf16(rng.standard_normal((5, w)))
+    spans = B.Kv4Spans([(0, 0, 0, 2), (2, 0, 5, 3)])
+    q = kv.append(0, spans, both[:, :w])
+    both[:, w:w + nq * d] = q.flatten(1)
+    out = both[:, w + nq * d:]
+    kv.attend(0, spans, both[:, w:w + nq * d], out=out)
+    assert torch.equal(out, kv.attend(0, spans, q).flatten(1))
+    for bad in (both[:, w:w + nq * d], both[:, w + 8:w + 8 + nq * d]):
+        with pytest.raises(B.StError) as e:
+            kv.attend(0, spans, both[:, w:w + nq * d], out=bad)
+        assert e.value.code == B.ST_EINVAL
 
 
 def test_refusals_of_the_binding():

@@ -117,6 +117,17 @@ def test_attend_refusals(L, kv):
         assert L.st_kv4_attend(kv, 0, s, n, q, qs, o, os_, None) == B.ST_EINVAL
 
 
+def test_matrices_that_share_memory(L, kv):
+    s, n = spans((0, 3, 0, 2), (1, 0, 0, 3))
+    attend = lambda q, qs, o, os_: L.st_kv4_attend(kv, 0, s, n, q, qs, o, os_, None)
+    for q, qs, o, os_ in ((PTR, 1536, PTR, 1536), (PTR, 1536, PTR + 2 * 1528, 1536), (PTR + 16, 1536, PTR, 1536), (PTR, 4096, PTR + 2 * 4096, 4096),
+                          (PTR, 4096, PTR + 2 * 1528, 4096), (PTR, 4096, PTR + 2 * 2568, 4096), (PTR + 2 * 2568, 4096, PTR, 4096),
+                          (PTR, 3096, PTR + 2 * 1536, 3088), (PTR + 2 * (4 * 1536 + 1528), 1536, PTR, 1536)):
+        assert attend(q, qs, o, os_) == B.ST_EINVAL and b"share" in L.st_last_error()
+    assert L.st_kv4_append(kv, 0, s, n, PTR, 2048, None, None, PTR, 2048, None) == B.ST_EINVAL and b"share" in L.st_last_error()
+    assert L.st_kv4_append(kv, 0, s, n, PTR, 2048, None, None, PTR + 2 * 2048, 1536, None) == B.ST_EINVAL and b"share" in L.st_last_error()
+
+
 def test_evict_refusals(L, kv):
     led = B.st_kv4_ledger(PTR, PTR)
     s, n = spans((0, 300, 500, 0))
@@ -132,6 +143,11 @@ def test_evict_refusals(L, kv):
     assert call(s=twice, n=m) == B.ST_EINVAL
     assert call(into=C.byref(B.st_kv4_ledger(PTR, PTR + 4096))) == B.ST_EINVAL     # one array shared
     assert call(into=C.byref(B.st_kv4_ledger(None, PTR))) == B.ST_EINVAL
+    size, base = 4 * 3 * 5 * 2 * 1000, 0x10000000
+    far = C.byref(B.st_kv4_ledger(base, base + 64 * size))
+    for off in (4, size - 4, -4, 4 - size):
+        assert call(led=far, into=C.byref(B.st_kv4_ledger(base + off, base + 16 * size))) == B.ST_EINVAL
+        assert call(led=far, into=C.byref(B.st_kv4_ledger(base + 16 * size, base + 64 * size + off))) == B.ST_EINVAL
     assert L.st_kv4_evict(None, 0, 1, s, n, 1, 0, C.byref(led), None) == B.ST_EINVAL
 
 
