@@ -55,8 +55,9 @@ struct Kv4 {
     size_t per_layer[4];     // bytes of a layer in each
     const float *rope;       // [max_pos][head_dim / 2][2]
     float *lse;              // [max_rows][n_q_heads] log2 of each row's softmax sum
-    float *part_ml, *part_o; // partial results of the key ranges: (max, sum) and outputs
+    float *part_ml, *part_o; // partial results of the key ranges: (max, sum) and outputs (and behind those, scores)
     size_t part_rows;        // rows they hold
+    size_t part_floats;      // in part_o
     uint64_t *kept;          // evict: a bit per slot, [layer][span][kv head][kept_words]
     size_t kept_words;
     hipStream_t stream;
@@ -73,6 +74,7 @@ struct Kv4AttendPlan {
     int join;      // rows of the longest span in several ranges, 0 without one
     int64_t most;  // columns of a kv head in the span with most rows
     bool fused;    // the ranges are joined by the kernel that sums up the weights
+    int64_t score_at, score_stride;  // where in part_o the scores are kept, [row][query head][stride]; stride 0: they are not
 };
 Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights);
 

@@ -5,6 +5,7 @@
 // of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  s is the least with max |x| <= 7 * 2^s: the largest value is then clipped by less than the
 // rounding of its neighbours costs (mean error on normal data 19.0 dB below the data, against 18.75 with max |x| <= 6 * 2^s).  A slot is head_dim / 2
 // bytes of codes and head_dim / 32 of scales, in planes of their own, so that a wave reads whole lines of codes.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -239,7 +240,11 @@ static void carve(const st_kv4_config &c, char *cache, char *ws, Kv4 *k, size_t 
     k->part_rows = columns < blocks ? columns : blocks;
     k->lse = reinterpret_cast<float *>(take(sizeof(float) * c.max_rows * (size_t)c.n_q_heads));
     k->part_ml = reinterpret_cast<float *>(take(sizeof(float) * 2 * k->part_rows));
-    k->part_o = reinterpret_cast<float *>(take(sizeof(float) * c.head_dim * k->part_rows));
+    // (and scores: of single rows over all slots, as far as the largest partial results' room goes)
+    const size_t score_rows = (size_t)(c.max_rows < ST_KV4_MAX_SPANS ? c.max_rows : ST_KV4_MAX_SPANS) * c.n_q_heads;
+    const size_t wanted = k->part_rows * c.head_dim + score_rows * (((size_t)c.max_seq + 31) & ~(size_t)31), most = blocks * 128;
+    k->part_floats = std::max(k->part_rows * c.head_dim, std::min(wanted, most));
+    k->part_o = reinterpret_cast<float *>(take(sizeof(float) * k->part_floats));
     k->kept_words = ((size_t)c.max_seq + 63) / 64;
     const size_t spans = c.n_seq < ST_KV4_MAX_SPANS ? c.n_seq : ST_KV4_MAX_SPANS;
     k->kept = reinterpret_cast<uint64_t *>(take(sizeof(uint64_t) * c.n_layers * spans * c.n_kv_heads * k->kept_words));

@@ -127,7 +127,7 @@ template <int D, int NT, int CAP>
 __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                  int64_t q_stride, bf16_t *__restrict__ out, int64_t out_stride,
                                                  float *__restrict__ part_o, float *__restrict__ part_ml,
-                                                 float *__restrict__ lse) {
+                                                 float *__restrict__ lse, float *__restrict__ scores, int64_t score_stride) {
     constexpr int KS = D / 32, DPL = D / 16, NB = D / 32, CB = D / 2, SB = D / 32;
     const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -218,6 +218,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans
                             if (slot <= lim[c]) poison |= 1u << c;
             }
         }
+        if constexpr (NT == 1)
+            if (scores && c0 + m16 < cols) {
+                const Column w = column_of(c0 + m16, G, kvh);
+                float4 *dst = reinterpret_cast<float4 *>(scores + ((int64_t)(sp.row0 + w.row) * view.nq + w.head) * score_stride + key0 + 8 * qd);
+                dst[0] = make_float4(sc[0][0][0], sc[0][0][1], sc[0][0][2], sc[0][0][3]);
+                dst[1] = make_float4(sc[0][1][0], sc[0][1][1], sc[0][1][2], sc[0][1][3]);
+            }
         bf16x8 pf[NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
@@ -617,17 +624,20 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Spans<CAP> t, int nq,
 }
 
 // ---------------------------------------------------------------------------------------
-// Few columns: the weight each slot received, and the ranges' join beside it in the same launch.  Scores are formed once more, from the keys (half of
-// what the first kernel read, and mostly still in the last-level cache), as S = Q K^T: a lane then has one slot and four columns of
-// each tile of 16, and the sum over the columns is three additions and two exchanges.  One lane owns a slot's sum: no atomics.
+// Few columns: the weight each slot received, and the ranges' join beside it in the same launch.  Up to kScoreCols columns have left their scores
+// in the workspace (STORED; four bytes a column and slot, where the keys would be 68), and a thread sums up a slot.  For more, scores are formed once
+// more from the keys (half of what the first kernel read, and mostly still in the last-level cache), as S = Q K^T: a lane then has one slot and four
+// columns of each tile of 16, and the sum over the columns is three additions and two exchanges.  One lane owns a slot's sum: no atomics.
 // A block works on the range of slots that the same block of k_kv4_few had; blocks past those join one unit each.
 // ---------------------------------------------------------------------------------------
-template <int D, int NT, int CAP>
+constexpr int kScoreCols = 8;
+
+template <int D, int NT, bool STORED, int CAP>
 __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, const Kv4View view, const bf16_t *__restrict__ q,
                                                          int64_t q_stride, const float *__restrict__ part_o,
                                                          const float *__restrict__ part_ml, const float *__restrict__ lse,
                                                          int blocks, int join_rows, bf16_t *__restrict__ out, int64_t out_stride,
-                                                         float *__restrict__ weights) {
+                                                         float *__restrict__ weights, const float *__restrict__ scores, int64_t score_stride) {
     constexpr int KS = D / 32, CB = D / 2, SB = D / 32;
     __shared__ float4 red[(256 / (D / 4) - 1) * (D / 4)];
     __shared__ float base_s[NT * 16];
@@ -650,13 +660,14 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
     const int cols = sp.rows * G;
     const float scale = 1.4426950408889634f / sqrtf((float)D);
     bf16x8 qf[NT][KS];
+    if constexpr (!STORED)
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-        const Column w = column_of(min(16 * c + m16, cols - 1), G, kvh);
-        const bf16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * (D / 4);
+        for (int c = 0; c < NT; ++c) {
+            const Column w = column_of(min(16 * c + m16, cols - 1), G, kvh);
+            const bf16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * (D / 4);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[c][s] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 8 * s));
-    }
+            for (int s = 0; s < KS; ++s) qf[c][s] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + 8 * s));
+        }
     // log2 of the columns' softmax sums: wave c makes those of tile c, four lanes a column
     if (wave < NT) {
         const int col = min(16 * wave + m16, cols - 1);
@@ -684,6 +695,28 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
         if (qd == 0) base_s[16 * wave + m16] = b;
     }
     __syncthreads();
+    float *dst = weights + head0;
+    if constexpr (STORED) {
+        const float *col[kScoreCols];
+#pragma unroll
+        for (int c = 0; c < kScoreCols; ++c) {
+            const Column w = column_of(min(c, cols - 1), G, kvh);
+            col[c] = scores + ((int64_t)(sp.row0 + w.row) * view.nq + w.head) * score_stride;
+        }
+        for (int key = t_begin * kFewTile + threadIdx.x; key < min(t_end * kFewTile, n_keys); key += 256) {
+            float v[kScoreCols], sum = 0.f;
+            const float was = dst[key];
+#pragma unroll
+            for (int c = 0; c < kScoreCols; ++c) v[c] = col[c][key];
+#pragma unroll
+            for (int c = 0; c < kScoreCols; ++c) {  // (a slot that a row does not see has the score -infinity)
+                const float p = __builtin_amdgcn_exp2f(fmaf(v[c], scale, -base_s[c]));
+                sum += c < cols ? p : 0.f;
+            }
+            dst[key] = was + sum;
+        }
+        return;
+    }
     float base[NT][4];
     int lim[NT][4];
 #pragma unroll
@@ -693,7 +726,6 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
             const int col = 16 * c + 4 * qd + r;
             base[c][r] = base_s[col], lim[c][r] = col < cols ? sp.len + col / G : -1;
         }
-    float *dst = weights + head0;
     for (int tile = t_begin + wave; tile < t_end; tile += kFewWaves) {
         const int key0 = tile * kFewTile;
         const int key = key0 + 16 * (qd & 1) + m16;  // the slot whose sum lanes of quarters 0 and 1 write
@@ -901,14 +933,27 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
     // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk, which takes some 14 us more to
     // get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
     const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
-    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, few && weights && most <= 64};
+    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, few && weights && most <= 64, 0, 0};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
     // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us against 6.5, on 512 6.2
     // against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7 against 6.7.)
     const int whole = few && !p.fused ? 512 / kFewTile : 0;
     p.blocks = cut_ranges(k, t, few ? kFewTile : kTileKeys, few ? kFewWaves : 1, whole, p.cols == 32 ? 256 : kKv4Blocks, groups);
-    for (int j = 0; j < t.n; ++j)
-        if (t.s[j].splits > 1 && t.s[j].rows > p.join) p.join = t.s[j].rows;
+    int64_t rows = 0, longest = 0, parts = 0;
+    for (int j = 0; j < t.n; ++j) {
+        const Kv4Span &s = t.s[j];
+        if (!s.rows) continue;
+        rows += s.rows;
+        longest = s.len + s.rows > longest ? s.len + s.rows : longest;
+        if (s.splits > 1) {
+            parts += (int64_t)s.splits * s.rows * k.c.n_q_heads;
+            p.join = s.rows > p.join ? s.rows : p.join;
+        }
+    }
+    // Scores are kept behind the partial outputs where there is room: 16 single tokens of 40 / 8 heads on 500 to 6000 slots 21.6 us with them, 24.2
+    // without; 64 on 500 to 1500 slots 25.9 against 30.3.
+    const int64_t stride = (longest + kFewTile - 1) / kFewTile * kFewTile, at = parts * k.c.head_dim;
+    if (p.fused && most <= kScoreCols && at + rows * k.c.n_q_heads * stride <= (int64_t)k.part_floats) p.score_at = at, p.score_stride = stride;
     return p;
 }
 
@@ -920,13 +965,14 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
     const Kv4AttendPlan plan = plan_kv4_attend(k, t, weights);
     const bool few = plan.cols < kTileCols, fused = plan.fused;
     const int blocks = plan.blocks, join = plan.join;
-    const int64_t most = plan.most;
+    const int64_t most = plan.most, score_stride = plan.score_stride;
+    float *scores = score_stride ? k.part_o + plan.score_at : nullptr;
     with_table(t, [&](auto tab) {
         constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
         const int nq = k.c.n_q_heads, units = join * nq;
 #define ST_FEW(DV, NTV)                                                                                                                  \
     hipLaunchKernelGGL((k_kv4_few<DV, NTV, CAP>), dim3(blocks), dim3(256), 0, k.stream, tab, view, q, q_stride, out, out_stride, k.part_o, \
-                       k.part_ml, lse)
+                       k.part_ml, lse, scores, score_stride)
         if (few && most <= 16) {
             if (D == 128) ST_FEW(128, 1);
             else ST_FEW(64, 1);
@@ -944,17 +990,19 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
                 tab.s[j].blk0 = blk;
                 if (tab.s[j].rows) blk += nkv * tab.s[j].splits;
             }
-#define ST_FEW_WEIGHTS(DV, NTV)                                                                                                           \
-    hipLaunchKernelGGL((k_kv4_few_weights<DV, NTV, CAP>), dim3(blk + units * tab.n), dim3(256), 0, k.stream, tab, view, q, q_stride, k.part_o, \
-                       k.part_ml, lse, blk, join, out, out_stride, weights)
+#define ST_FEW_WEIGHTS(DV, NTV, STORED)                                                                                                   \
+    hipLaunchKernelGGL((k_kv4_few_weights<DV, NTV, STORED, CAP>), dim3(blk + units * tab.n), dim3(256), 0, k.stream, tab, view, q, q_stride, k.part_o, \
+                       k.part_ml, lse, blk, join, out, out_stride, weights, scores, score_stride)
             if (D == 128) {
-                if (most <= 16) ST_FEW_WEIGHTS(128, 1);
-                else if (most <= 32) ST_FEW_WEIGHTS(128, 2);
-                else ST_FEW_WEIGHTS(128, 4);
+                if (scores) ST_FEW_WEIGHTS(128, 1, true);
+                else if (most <= 16) ST_FEW_WEIGHTS(128, 1, false);
+                else if (most <= 32) ST_FEW_WEIGHTS(128, 2, false);
+                else ST_FEW_WEIGHTS(128, 4, false);
             } else {
-                if (most <= 16) ST_FEW_WEIGHTS(64, 1);
-                else if (most <= 32) ST_FEW_WEIGHTS(64, 2);
-                else ST_FEW_WEIGHTS(64, 4);
+                if (scores) ST_FEW_WEIGHTS(64, 1, true);
+                else if (most <= 16) ST_FEW_WEIGHTS(64, 1, false);
+                else if (most <= 32) ST_FEW_WEIGHTS(64, 2, false);
+                else ST_FEW_WEIGHTS(64, 4, false);
             }
 #undef ST_FEW_WEIGHTS
         }

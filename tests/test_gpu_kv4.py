@@ -313,6 +313,16 @@ def test_attend_many_spans():
     check_attend(kv, 0, [(69 - j, (j * 37) % 190, 0, 1 + j % 3) for j in range(64)], rng)
 
 
+@pytest.mark.parametrize("n", [40, 64])
+def test_attend_weights_with_and_without_room_for_scores(n):
+    """Single tokens with a ledger, one of them on a long context: the scores of 40 x 40 heads x 3328 slots have room in the workspace (2^23 floats at
+    most), those of 64 x 40 x 3328 do not."""
+    print("attend: weights of", n, "spans", flush=True)
+    rng = np.random.default_rng(n)
+    kv = make(40, 8, 64, n_seq=64, max_seq=3300, max_rows=64, max_pos=64, fill=0xff)
+    check_attend(kv, 0, [(5, 3299, 0, 1)] + [((6 + j) % 64, 7 * j % 130, 0, 1) for j in range(n - 1)], rng)
+
+
 @pytest.mark.parametrize("rows", [1, 3, 50])
 @pytest.mark.parametrize("side", ["k", "v"])
 def test_a_group_without_numbers_reaches_the_rows_that_see_it_and_no_others(rows, side):
