@@ -1,5 +1,5 @@
-// Host-side internals of the 4-bit key/value cache (kv4.hip, kv4_attend.hip, kv4_evict.hip): its record, the span table that the kernels
-// take by value and the launchers the API layer calls.  Nothing here is part of the public ABI.
+// Host-side internals of the 4-bit key/value cache (kv4.hip, kv4_attend.hip, kv4_evict.hip): its record, the span table that
+// the kernels take by value and the launchers the API layer calls.  Nothing here is part of the public ABI.
 #pragma once
 
 #include "st_internal.h"
@@ -15,8 +15,8 @@ struct Kv4Span {
     int32_t per;                  // tiles of slots in a range
     int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
 };
-// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Three sizes, as a launch with the
-// largest costs the host 3.4 us and one with the smallest 2.4.
+// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Three sizes, as a
+// launch with the largest costs the host 3.4 us and one with the smallest 2.4.
 template <int CAP>
 struct Kv4Spans {
     int32_t n;
@@ -89,8 +89,8 @@ void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &
                       const int32_t *p_in, float *w_out, int32_t *p_out);
 
 #ifdef __HIPCC__
-// The span whose blocks block `b` belongs to: the last one that starts at or before it (spans without blocks share their
-// start with the next one).  Wave-uniform; all lanes must be active.
+// The span whose blocks block `b` belongs to: the last one that starts at or before it (spans without blocks share their start
+// with the next one).  Wave-uniform; all lanes must be active.
 template <int CAP>
 __device__ __forceinline__ int kv4_span_of(const Kv4Spans<CAP> &t, int b) {
     if constexpr (CAP == kKv4Few) {

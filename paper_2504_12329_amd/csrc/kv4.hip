@@ -1,10 +1,11 @@
 // A key/value cache held in 4 bits: the C entry points, and the two kernels that write and read single slots (append with the
 // norms of queries and keys and the rotation, and read).
 //
-// Format.  32 neighbouring channels of a head form a group with one scale 2^s, held as the byte s + 127, and 4-bit codes: sign and one
-// of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  s is the least with max |x| <= 7 * 2^s: the largest value is then clipped by less than the
-// rounding of its neighbours costs (mean error on normal data 19.0 dB below the data, against 18.75 with max |x| <= 6 * 2^s).  A slot is head_dim / 2
-// bytes of codes and head_dim / 32 of scales, in planes of their own, so that a wave reads whole lines of codes.
+// Format.  32 neighbouring channels of a head form a group with one scale 2^s, held as the byte s + 127, and 4-bit codes: sign
+// and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  s is the least with max |x| <= 7 * 2^s: the largest value is then clipped by less
+// than the rounding of its neighbours costs (mean error on normal data 19.0 dB below the data, against 18.75 with max |x| <= 6
+// * 2^s).  A slot is head_dim / 2 bytes of codes and head_dim / 32 of scales, in planes of their own, so that a wave reads
+// whole lines of codes.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -18,12 +19,13 @@ namespace st {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------------------
-// Append.  D/8 threads per head; a thread owns four neighbouring channels of each half of the head, i.e. four rotation
-// pairs, so that norm, rotation and quantisation need no exchange but the group's maximum (8 lanes) and the norm's sum.  Bound
-// by memory: 2 bytes per channel in, 2 out for the queries, 4.25 bits for keys and values.
+// Append.  D/8 threads per head; a thread owns four neighbouring channels of each half of the head, i.e. four rotation pairs,
+// so that norm, rotation and quantisation need no exchange but the group's maximum (8 lanes) and the norm's sum.  Bound by
+// memory: 2 bytes per channel in, 2 out for the queries, 4.25 bits for keys and values.  4096 rows of 40 / 8 heads 20.6 us, 5.3
+// TB/s (a large copy: 5.1); 16 rows 3.5 us.
 //
-// Every product and sum is rounded to fp32 by itself (no contraction) and the sum of squares adds neighbours first, so the codes are
-// a function of the inputs alone: no choice of the kernel's shape shows in them.
+// Every product and sum is rounded to fp32 by itself (no contraction) and the sum of squares adds neighbours first, so the
+// codes are a function of the inputs alone: no choice of the kernel's shape shows in them.
 // ---------------------------------------------------------------------------------------
 // sum / largest over the lanes of a group of 8 (16): quad swaps, then the mirrors, as every lane of a quad then holds the same
 __device__ __forceinline__ float sum_of_4(float v) {
@@ -122,8 +124,9 @@ __global__ __launch_bounds__(256) void k_kv4_append(const Kv4Spans<CAP> t, const
 }
 
 // ---------------------------------------------------------------------------------------
-// Read: slots [len, len + rows) of every span as the bf16 numbers they stand for (each is one exactly).  A thread turns four bytes of codes into
-// 16 of output; 1 << shift waves have RPW rows, so that heads too few for a block share it with other rows.  Bound by memory.
+// Read: slots [len, len + rows) of every span as the bf16 numbers they stand for (each is one exactly).  A thread turns four
+// bytes of codes into 16 of output; 1 << shift waves have RPW rows, so that heads too few for a block share it with other rows.
+// Bound by memory.
 // ---------------------------------------------------------------------------------------
 template <int D, int RPW, int CAP>
 __global__ __launch_bounds__(256) void k_kv4_read(const Kv4Spans<CAP> t, Kv4View view, size_t k_layer, size_t s_layer, int rows, int shift,
@@ -183,8 +186,8 @@ void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, con
 
 void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out) {
     const int units = 2 * k.c.n_kv_heads * (k.c.head_dim / 8), shift = units > 128 ? 2 : units > 64 ? 1 : 0, layers = layer_hi - layer_lo;
-    // Two rows a wave once that leaves the chip full: 16 x 1024 rows of 8 heads 16.8 us against 19.8 (5.1 TB/s), 28 x 512 of 2 heads 5.8 against 6.2; 12 x 35 of 4
-    // heads 2.8 against 2.5.
+    // Two rows a wave once that leaves the chip full: 16 x 1024 rows of 8 heads 16.8 us against 19.8 (5.1 TB/s), 28 x 512 of 2
+    // heads 5.8 against 6.2; 12 x 35 of 4 heads 2.8 against 2.5.
     const bool many = (int64_t)rows * layers << shift >= 12288;
     const int groups = many ? (rows + 1) / 2 : rows;
     with_table(t, [&](auto tab) {

@@ -1,15 +1,15 @@
 // Attention over the 4-bit key/value cache, and the attention weight each of its slots receives.
 //
-// Row i of a span (seq, len, rows) sees slots [0, len + i].  The query heads of a kv head are folded into columns: column i * G + h is row i of
-// head h.  With S^T = K Q^T (slots x columns) a lane holds one column, so the softmax is register arithmetic and P^T is the
-// second product's operand as it stands: O^T = V^T P^T.  Codes become bf16 in registers (v_cvt_scalef32_pk_bf16_fp4, two
-// values an instruction, exact); keys give eight channels of a slot to a lane, which is what the first product
-// wants, values come as channel pairs of one slot and are put together with the neighbouring slot's by a byte permute.
-// Scores, maxima, sums and outputs are fp32; the weights enter the second product as bf16 (rounded just below the running maximum's 1, where
-// that costs least), as the model's own attention does.
+// Row i of a span (seq, len, rows) sees slots [0, len + i].  The query heads of a kv head are folded into columns: column i * G
+// + h is row i of head h.  With S^T = K Q^T (slots x columns) a lane holds one column, so the softmax is register arithmetic
+// and P^T is the second product's operand as it stands: O^T = V^T P^T.  Codes become bf16 in registers
+// (v_cvt_scalef32_pk_bf16_fp4, two values an instruction, exact); keys give eight channels of a slot to a lane, which is what
+// the first product wants, values come as channel pairs of one slot and are put together with the neighbouring slot's by a byte
+// permute. Scores, maxima, sums and outputs are fp32; the weights enter the second product as bf16 (rounded just below the
+// running maximum's 1, where that costs least), as the model's own attention does.
 //
-// A value group that held an infinity or NaN reads as NaN, and reaches exactly the rows that see it: in tiles that some row sees only
-// in part such groups are multiplied as zeros and the rows that see them marked.
+// A value group that held an infinity or NaN reads as NaN, and reaches exactly the rows that see it: in tiles that some row
+// sees only in part such groups are multiplied as zeros and the rows that see them marked.
 #include <utility>
 
 #include "kv4.h"
@@ -30,8 +30,8 @@ __device__ __forceinline__ u32x4 keys8(uint32_t w, float unit) {  // eight chann
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// Eight slots of V as a lane loads them: NB bytes of codes (2 NB channels of one scale group) of slot j in c[j], and the scale bytes of
-// all groups, not taken apart until they are used, so that nothing waits for the load where it is issued.
+// Eight slots of V as a lane loads them: NB bytes of codes (2 NB channels of one scale group) of slot j in c[j], and the scale
+// bytes of all groups, not taken apart until they are used, so that nothing waits for the load where it is issued.
 template <int D, int NB>
 struct Values8 {
     uint32_t c[8], s[D / 16];
@@ -40,8 +40,8 @@ struct Values8 {
         return __builtin_amdgcn_ubfe(D == 128 ? s[j] : s[j >> 1], shift + (D == 128 ? 0 : 16 * (j & 1)), 8) << 23;
     }
 };
-// Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each.  TAIL: slots past `last` are read as `last` (no address
-// past it is formed).
+// Slots key .. key + 7 of one kv head: NB bytes of codes at byte `at` of each.  TAIL: slots past `last` are read as `last` (no
+// address past it is formed).
 template <int D, int NB, bool TAIL>
 __device__ __forceinline__ void load_values(Values8<D, NB> &v, const uint8_t *codes, const uint8_t *scales, int key, int last, int at) {
     constexpr int CB = D / 2, SB = D / 32;
@@ -111,15 +111,17 @@ struct Column {
 __device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Column{col / G, kvh * G + col % G}; }
 
 // ---------------------------------------------------------------------------------------
-// Few columns: single tokens and short runs.  With one group of columns bound by memory (the cache is read once), with more by the vector
-// pipe.
+// Few columns: single tokens and short runs.  With one group of columns bound by memory (the cache is read once): 16 tokens of
+// 40 / 8 heads on 500 to 6000 slots 15.8 us, 3.6 TB/s, one of 12 / 2 heads on 4608 slots 4.4 us, all latency.  With more by the
+// vector pipe: 310 vector and 32 matrix instructions a tile of 32 columns, 86 rows of 40 / 8 heads on 4096 slots 23 us (half of
+// the cycles issue, a quarter wait for loads; twice the blocks on half the slots each take as long).
 //
-// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end (four tiles no longer fit the
-// registers without moves: 36 us for 86 rows of 40 / 8 heads on 4096 slots, against 28 with two): S^T by 16x16x32 MFMAs whose A rows
-// are slots 8 (m / 4) + 4 t + m % 4, so that lane (column, quarter) ends up with the weights of slots 8 quarter .. + 7 -- the
-// B operand of the second product.  A lane reads 16 bytes (one scale group) of each of its two keys and, of eight value
-// slots, the D / 16 channels that make its row m of D / 16 products.  The next tile's loads are issued before
-// this tile's work.  A block's four waves take every fourth tile of its range and are joined through LDS; ranges are joined by k_kv4_join.
+// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end (four tiles no longer fit
+// the registers without moves: 36 us for 86 rows of 40 / 8 heads on 4096 slots, against 28 with two): S^T by 16x16x32 MFMAs
+// whose A rows are slots 8 (m / 4) + 4 t + m % 4, so that lane (column, quarter) ends up with the weights of slots 8 quarter ..
+// + 7 -- the B operand of the second product.  A lane reads 16 bytes (one scale group) of each of its two keys and, of eight
+// value slots, the D / 16 channels that make its row m of D / 16 products.  The next tile's loads are issued before this tile's
+// work.  A block's four waves take every fourth tile of its range and are joined through LDS; ranges are joined by k_kv4_join.
 // ---------------------------------------------------------------------------------------
 constexpr int kFewTile = 32, kFewWaves = 4;
 
@@ -344,10 +346,11 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans
 }
 
 // ---------------------------------------------------------------------------------------
-// Chunks.  A block is 128 columns of one kv head (four waves of 32) on a range of tiles of 128 slots.  The tile's codes are loaded one
-// tile ahead into registers, turned into bf16 once for all four waves and put into LDS as the MFMA operands that the
-// waves read: 1 KB fragments, 16 bytes a lane, no bank conflicts in writing or reading.  Two blocks share a compute
-// unit, so that one's products run beside the other's softmax.
+// Chunks, bound by the matrix pipe and, in turn with it, the vector pipe: 4096 rows of 40 / 8 heads on 4096 slots 515 us, 1.0
+// PFLOP/s (staging left out 448 us, exponentials left out 497).  A block is 128 columns of one kv head (four waves of 32) on a
+// range of tiles of 128 slots.  The tile's codes are loaded one tile ahead into registers, turned into bf16 once for all four
+// waves and put into LDS as the MFMA operands that the waves read: 1 KB fragments, 16 bytes a lane, no bank conflicts in
+// writing or reading.  Two blocks share a compute unit, so that one's products run beside the other's softmax.
 //   K: a thread has one scale group (32 channels) of one or two slots;  V: eight slots x eight channels.
 //   S^T rows: fragment row m of 32 slots is slot swap(m) (bits 2 and 3 exchanged): registers 0-7 and 8-15 of a lane are then eight
 //   consecutive slots each, as the second product wants them.
@@ -560,9 +563,9 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Spans<CAP> t, con
 }
 
 // ---------------------------------------------------------------------------------------
-// Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them are fetched at
-// once; then D / 4 lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range whose
-// slots the row does not see has sum 0 and an unused output.
+// Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them
+// are fetched at once; then D / 4 lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range
+// whose slots the row does not see has sum 0 and an unused output.  Latency: 3 to 4.6 us.
 // ---------------------------------------------------------------------------------------
 template <int D, int WPU>
 __device__ __forceinline__ void join_unit(const Kv4Span &sp, int unit, bool live, int nq, const float *__restrict__ part_o,
@@ -624,11 +627,13 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Spans<CAP> t, int nq,
 }
 
 // ---------------------------------------------------------------------------------------
-// Few columns: the weight each slot received, and the ranges' join beside it in the same launch.  Up to kScoreCols columns have left their scores
-// in the workspace (STORED; four bytes a column and slot, where the keys would be 68), and a thread sums up a slot.  For more, scores are formed once
-// more from the keys (half of what the first kernel read, and mostly still in the last-level cache), as S = Q K^T: a lane then has one slot and four
-// columns of each tile of 16, and the sum over the columns is three additions and two exchanges.  One lane owns a slot's sum: no atomics.
-// A block works on the range of slots that the same block of k_kv4_few had; blocks past those join one unit each.
+// Few columns: the weight each slot received, and the ranges' join beside it in the same launch.  Up to kScoreCols columns have
+// left their scores in the workspace (STORED; four bytes a column and slot, where the keys would be 68), and a thread sums up a
+// slot: 6 us for 16 tokens of 40 / 8 heads on 500 to 6000 slots, 10 from the keys.  For more, scores are formed once more from
+// the keys (half of what the first kernel read, and mostly still in the last-level cache), as S = Q K^T: a lane then has one
+// slot and four columns of each tile of 16, and the sum over the columns is three additions and two exchanges.  One lane owns a
+// slot's sum: no atomics. A block works on the range of slots that the same block of k_kv4_few had; blocks past those join one
+// unit each.
 // ---------------------------------------------------------------------------------------
 constexpr int kScoreCols = 8;
 
@@ -770,10 +775,11 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
 }
 
 // ---------------------------------------------------------------------------------------
-// Chunks: the weight each slot received, sum over the columns that see it of exp2(score - lse), the scores formed once more (K only).  A block
-// is 64 slots, its keys in registers as bf16; its W waves take every W-th tile of 32 columns, S = Q K^T, so that a lane has one slot and
-// the sum over the columns stays in the lane.  One block owns a slot's sum: no atomics, the same order in every run.  Bound by the matrix and the
-// vector pipe in turn (an exponential and two more operations a score): 2048 rows of 40 / 8 heads on 4096 slots 212 us, 0.51 PFLOP/s; 86 rows 13.5 us.
+// Chunks: the weight each slot received, sum over the columns that see it of exp2(score - lse), the scores formed once more (K
+// only).  A block is 64 slots, its keys in registers as bf16; its W waves take every W-th tile of 32 columns, S = Q K^T, so
+// that a lane has one slot and the sum over the columns stays in the lane.  One block owns a slot's sum: no atomics, the same
+// order in every run.  Bound by the matrix and the vector pipe in turn (an exponential and two more operations a score): 2048
+// rows of 40 / 8 heads on 4096 slots 212 us, 0.51 PFLOP/s; 86 rows 13.5 us.
 // ---------------------------------------------------------------------------------------
 constexpr int kWeightKeys = 64;
 
@@ -803,7 +809,8 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 2) void k_kv4_weights(const Kv
     u32x4 qw[32 / RPL];
     float base;
     int lim;
-    // A load is whole columns, side by side (a lane's own column would be a line of its own for each lane); LDS brings them into the operand's order.
+    // A load is whole columns, side by side (a lane's own column would be a line of its own for each lane); LDS brings them
+    // into the operand's order.
     auto load = [&]() {
         const Column own = column(min(ct * 32 + l32, cols - 1));
         lim = ct * 32 + l32 < cols ? sp.len + own.row : -1;
@@ -889,9 +896,10 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 2) void k_kv4_weights(const Kv
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`, at least `whole` of them if no span has more), as short as leaves at most `want` blocks, kKv4Ranges
-// ranges and the partial results within their buffer; returns the blocks.  blocks_of(span): blocks of one range.  (Steps grow with the range: a long
-// context with few rows tries some dozen lengths, not thousands.)
+// Cuts the spans' tiles of `tile` slots into ranges of Kv4Span::per tiles (a multiple of `step`, at least `whole` of them if no
+// span has more), as short as leaves at most `want` blocks, kKv4Ranges ranges and the partial results within their buffer;
+// returns the blocks.  blocks_of(span): blocks of one range.  (Steps grow with the range: a long context with few rows tries
+// some dozen lengths, not thousands.)
 template <class F>
 static int cut_ranges(const Kv4 &k, Kv4Table &t, int tile, int step, int whole, int want, F blocks_of) {
     const int64_t nq = k.c.n_q_heads;
@@ -930,13 +938,15 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
         few_tiles += (cols + 31) / 32 * nkv * ((held + kFewTile - 1) / kFewTile);
         chunk_tiles += (cols + kTileCols - 1) / kTileCols * nkv * ((held + kTileKeys - 1) / kTileKeys);
     }
-    // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk, which takes some 14 us more to
-    // get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
+    // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk,
+    // which takes some 14 us more to get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows
+    // 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
     const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
     Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, few && weights && most <= 64, 0, 0};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
-    // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us against 6.5, on 512 6.2
-    // against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7 against 6.7.)
+    // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us
+    // against 6.5, on 512 6.2 against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7
+    // against 6.7.)
     const int whole = few && !p.fused ? 512 / kFewTile : 0;
     p.blocks = cut_ranges(k, t, few ? kFewTile : kTileKeys, few ? kFewWaves : 1, whole, p.cols == 32 ? 256 : kKv4Blocks, groups);
     int64_t rows = 0, longest = 0, parts = 0;
@@ -950,8 +960,8 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
             p.join = s.rows > p.join ? s.rows : p.join;
         }
     }
-    // Scores are kept behind the partial outputs where there is room: 16 single tokens of 40 / 8 heads on 500 to 6000 slots 21.6 us with them, 24.2
-    // without; 64 on 500 to 1500 slots 25.9 against 30.3.
+    // Scores are kept behind the partial outputs where there is room: 16 single tokens of 40 / 8 heads on 500 to 6000 slots
+    // 21.6 us with them, 24.2 without; 64 on 500 to 1500 slots 25.9 against 30.3.
     const int64_t stride = (longest + kFewTile - 1) / kFewTile * kFewTile, at = parts * k.c.head_dim;
     if (p.fused && most <= kScoreCols && at + rows * k.c.n_q_heads * stride <= (int64_t)k.part_floats) p.score_at = at, p.score_stride = stride;
     return p;
@@ -1022,8 +1032,9 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
         }
         with_table(t, [&](auto tab) {
             constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
-            // Eight waves share a block's columns while there is at most one block a compute unit: 125 rows of 12 / 2 heads on 3000 slots 23.6 us with the
-            // attention against 26.4, 86 rows of 40 / 8 heads on 4096 (528 blocks) 44.6 against 40.4.
+            // Eight waves share a block's columns while there is at most one block a compute unit: 125 rows of 12 / 2 heads on
+            // 3000 slots 23.6 us with the attention against 26.4, 86 rows of 40 / 8 heads on 4096 (528 blocks) 44.6 against
+            // 40.4.
             const bool wide = blk <= 256;
             auto *kern = D == 128 ? (wide ? k_kv4_weights<128, 8, CAP> : k_kv4_weights<128, 4, CAP>) : (wide ? k_kv4_weights<64, 8, CAP> : k_kv4_weights<64, 4, CAP>);
             hipLaunchKernelGGL(kern, dim3(blk), dim3(wide ? 512 : 256), 0, k.stream, tab, view, q, q_stride, lse, weights);
