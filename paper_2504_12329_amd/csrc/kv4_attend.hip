@@ -822,6 +822,9 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 2) void k_kv4_weights(const Kv
         }
     };
     if (ct * 32 < cols) load();
+    const bool owns = threadIdx.x < kWeightKeys && key0 + (int)threadIdx.x <= last;
+    float *dst = weights + head0 + key0 + threadIdx.x;
+    const float was = owns ? *dst : 0.f;
     bf16x8 kf[2][ST];  // slot key0 + 32 u + l32, channels hf D / 2 + 8 s
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -885,11 +888,11 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : 2) void k_kv4_weights(const Kv
         if (hf == 0) sums[wave][32 * u + l32] = v;
     }
     __syncthreads();
-    if (threadIdx.x < kWeightKeys && key0 + (int)threadIdx.x <= last) {
+    if (owns) {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) v += sums[w][threadIdx.x];
-        weights[head0 + key0 + threadIdx.x] += v;
+        *dst = was + v;
     }
 }
 
@@ -942,7 +945,10 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
     // which takes some 14 us more to get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows
     // 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
     const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
-    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, few && weights && most <= 64, 0, 0};
+    // The weights of up to 64 columns beside the join, in one launch; of more than 32 only while that launch is short.  Rows of 40 / 8 heads, one launch against
+    // two: 4 sequences x 12 rows on 500 to 4000 slots 22.6 : 23.7 us, 16 x 12 rows 69.2 : 57.4, 16 x 6 rows 32.8 : 45.6.
+    const bool fused = weights && few && (most <= 32 || (most <= 64 && few_tiles <= 6000));
+    Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, fused, 0, 0};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
     // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us
     // against 6.5, on 512 6.2 against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7
