@@ -9,7 +9,7 @@
 // k_kv4_evict, one block per head, finds the keep-th by histograms of 11-bit digits in LDS until at most 128 slots share the
 // digits so far, and ranks those against each other; it writes a bit per slot and moves.  Bound by latency: weights and
 // positions are read once, the 32 bits kept in LDS (up to 24576 slots; beyond, they are read again for every digit).  128 heads
-// of 500 to 6000 slots to 1024: 21 us, of which 3 us are loads and the first histogram, 5 us the threshold and the bits, 3 us
+// of 500 to 6000 slots to 1024: 20 us, of which 3 us are loads and the first histogram, 5 us the threshold and the bits, 2 us
 // the lists, 4 us the moves and the rest launch and drain; 56 heads of 577 slots to 512: 8.6 us. (Histograms over the range the
 // weights span, which need no second digit, cost a reduction first: 0.4 to 3 us slower.)  k_kv4_move: where few heads move many
 // slots, the moves by several blocks per head.
@@ -92,64 +92,41 @@ __device__ __forceinline__ uint64_t late_word(uint64_t bits, int i, int n, int k
     return s0 + 64 <= keep ? 0 : bits & held & (s0 >= keep ? ~0ull : ~((1ull << (keep - s0)) - 1));
 }
 
-// LDS of list_moves
-template <int THREADS>
-struct MoveLists {
-    int pre[2][THREADS], cnt[2][THREADS / 64];
-    uint64_t xs[2][THREADS];
-};
-// Entries r0 .. r0 + SIZE - 1 of the freed slots and of the late ones, in order, into list[0] and list[1]; returns how many
-// there are of each.  A thread counts a word's bits, then a wave takes a word and a lane a bit, four words at a time.  All
-// THREADS threads; ends with a barrier.
+// Entries r0 .. r0 + SIZE - 1 of the freed slots and of the late ones, in order, into list[0] and list[1]; returns how many there are
+// of each.  Every wave counts all words' bits, 64 words at a time with a word to a lane, so that no wave waits for another; then it
+// takes every WAVES-th word, with a bit to a lane.  All THREADS threads; ends with a barrier.
 template <int THREADS, int SIZE>
-__device__ __forceinline__ int list_moves(const uint64_t *bits, int n, int keep, int r0, int *freed, int *late, MoveLists<THREADS> &m) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), words = (n + 63) / 64;
+__device__ __forceinline__ int list_moves(const uint64_t *bits, int n, int keep, int r0, int *freed, int *late) {
+    constexpr int WAVES = THREADS / 64, U = 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), words = (n + 63) / 64;
     int total[2] = {0, 0};
-    for (int i0 = 0; i0 < words; i0 += THREADS) {
-        const uint64_t b = i0 + tid < words ? bits[i0 + tid] : 0;
-        const uint64_t x[2] = {i0 + tid < words ? freed_word(b, i0 + tid, keep) : 0, i0 + tid < words ? late_word(b, i0 + tid, n, keep) : 0};
-        int run[2];
+    for (int i0 = 0; i0 < words; i0 += 64 * U) {
+        uint64_t b[U];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            run[h] = wave_running_sum(__popcll(x[h]));
-            if (lane == 63) m.cnt[h][wave] = run[h];
-        }
-        __syncthreads();
+        for (int e = 0; e < U; ++e) b[e] = bits[min(i0 + 64 * e + lane, words - 1)];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            int first = total[h] + run[h] - __popcll(x[h]);
+        for (int e = 0; e < U; ++e) {
+            const int w0 = i0 + 64 * e, w = w0 + lane;
+            if (w0 >= words) break;
+            const uint64_t x[2] = {w < words ? freed_word(b[e], w, keep) : 0, w < words ? late_word(b[e], w, n, keep) : 0};
 #pragma unroll
-            for (int v = 0; v < THREADS / 64; ++v) {
-                first += v < wave ? m.cnt[h][v] : 0;
-                total[h] += m.cnt[h][v];
-            }
-            m.pre[h][tid] = first - r0, m.xs[h][tid] = x[h];
-        }
-        __syncthreads();
-        const int have = min(THREADS, words - i0);
-        for (int h = 0; h < 2; ++h) {
-            // (freed slots are in the words up to keep's, late ones in those from it on)
-            const int from = h ? max(keep / 64 - i0, 0) : 0, to = h ? have : min((keep + 63) / 64 - i0, have);
-            int *list = h ? late : freed;
-            for (int j0 = from + wave; j0 < to; j0 += THREADS / 16) {
-                uint64_t y[4];
-                int at[4];
+            for (int h = 0; h < 2; ++h) {
+                const int own = __popcll(x[h]), run = wave_running_sum(own), first = total[h] + run - own - r0;
+                const int all = __builtin_amdgcn_readlane(run, 63);
+                total[h] += all;
+                if (!all || total[h] - all >= r0 + SIZE || total[h] <= r0) continue;  // none of the entries is in these words
+                int *list = h ? late : freed;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = min(j0 + e * (THREADS / 64), THREADS - 1);
-                    y[e] = m.xs[h][j], at[e] = m.pre[h][j];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + e * (THREADS / 64), first = __builtin_amdgcn_readfirstlane(at[e]);
-                    if (j >= to || first >= SIZE || first <= -64) continue;  // nothing of these entries
-                    const int r = first + __popcll(y[e] & ((1ull << lane) - 1));
-                    if ((y[e] >> lane & 1) && r >= 0 && r < SIZE) list[r] = (i0 + j) * 64 + lane;
+                for (int k = 0; k < 64; k += WAVES) {
+                    const uint32_t y0 = __builtin_amdgcn_readlane((int)(uint32_t)x[h], k + wave), y1 = __builtin_amdgcn_readlane((int)(x[h] >> 32), k + wave);
+                    if (!(y0 | y1)) continue;
+                    const int r = __builtin_amdgcn_readlane(first, k + wave) + __builtin_amdgcn_mbcnt_hi(y1, __builtin_amdgcn_mbcnt_lo(y0, 0));
+                    if (((lane < 32 ? y0 : y1) >> (lane & 31) & 1) && r >= 0 && r < SIZE) list[r] = (w0 + k + wave) * 64 + lane;
                 }
             }
         }
-        __syncthreads();
     }
+    __syncthreads();
     return total[1];
 }
 
@@ -220,7 +197,7 @@ template <int D, int THREADS, bool HELD, int CAP>
 __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, const EvictArgs a) {
     constexpr int COPIES = THREADS / 256, WAVES = THREADS / 64;
     extern __shared__ __align__(16) uint64_t dyn[];  // the bits, then the slots' 32 bits
-    __shared__ __align__(16) int hist[COPIES * kBins + 2048];  // (and later the lists of moves)
+    __shared__ __align__(16) int hist[COPIES * kBins];  // (and later the lists of moves)
     __shared__ __align__(16) int wsum[WAVES], res[3], n_near;
     __shared__ __align__(16) uint32_t near_o[kDirect], near_p[kDirect];
     __shared__ __align__(16) int near_s[kDirect], near_rank[kDirect];
@@ -374,11 +351,10 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
     if (a.parts) return;
     // the moves; the histogram's memory holds the lists
     constexpr int kList = THREADS;
-    static_assert(2 * kList * sizeof(int) + sizeof(MoveLists<THREADS>) <= sizeof(hist), "lists in the histogram");
+    static_assert(2 * kList * sizeof(int) <= sizeof(hist), "lists in the histogram");
     int *freed = hist, *late = hist + kList;
-    MoveLists<THREADS> &lists = *reinterpret_cast<MoveLists<THREADS> *>(hist + 2 * kList);
     for (int r0 = 0;; r0 += kList) {
-        const int total = list_moves<THREADS, kList>(bits, n, keep, r0, freed, late, lists);
+        const int total = list_moves<THREADS, kList>(bits, n, keep, r0, freed, late);
         move_slots<D, THREADS>(pl, late, freed, min(total - r0, kList));
         if (r0 + kList >= total) return;
         __syncthreads();
@@ -392,14 +368,13 @@ constexpr int kMoveThreads = 1024, kMovesPer = 256;
 template <int D, int CAP>
 __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t, const EvictArgs a) {
     __shared__ int freed[kMovesPer], late[kMovesPer];
-    __shared__ MoveLists<kMoveThreads> lists;
     const Kv4Span sp = t.s[blockIdx.y];
     const int n = sp.len, keep = a.keep, kvh = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     if (n <= keep) return;
     const Planes pl = planes_of<D>(a, sp, kvh, blockIdx.z);
     const uint64_t *bits = a.kept + (((size_t)blockIdx.z * t.n + blockIdx.y) * a.view.nkv + kvh) * a.kept_words;
     for (int r0 = part * kMovesPer;; r0 += a.parts * kMovesPer) {
-        const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, r0, freed, late, lists);
+        const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, r0, freed, late);
         move_slots<D, kMoveThreads>(pl, late, freed, min(total - r0, kMovesPer));
         if (r0 + a.parts * kMovesPer >= total) return;
         __syncthreads();
@@ -416,7 +391,11 @@ static void evict_in(const Kv4 &k, const Kv4Spans<CAP> &t, const EvictArgs &a, i
     auto raised = [](auto *kern) {  // once per kernel: up to 115 KB of LDS asked for at the launch
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 4 + kHeldSlots / 8);
     };
-    if (longest <= 2048) {  // a block of 256 threads: cheaper barriers and scans
+    // Blocks of 256 threads for short contexts (cheaper barriers and scans) and, where there is more than one block a compute unit, for longer ones, as two
+    // of 1024 threads do not run side by side.  256 : 1024 threads, 56 heads of 300 slots 8.0 : 9.5 us, of 1100 16.6 : 11.9; 320 heads of 700 slots
+    // 11.7 : 19.6, of 2500 25.5 : 27.4, of 4000 47.6 : 42.0.
+    const int64_t heads = (int64_t)grid.x * grid.y * grid.z;
+    if (longest <= (heads > 256 ? 2560 : 768)) {
         hipLaunchKernelGGL((k_kv4_evict<D, 256, true, CAP>), grid, dim3(256), bit_bytes + 4 * (size_t)longest, k.stream, t, a);
     } else if (longest <= kHeldSlots) {
         static std::once_flag once;

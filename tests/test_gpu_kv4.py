@@ -458,6 +458,20 @@ def test_evict(d, kind):
         check_evict(kv, (1, 2), spans, keep, recent, w, p, into=True)
 
 
+@pytest.mark.parametrize("layers,n_seq,spans,keep", [
+    (9, 4, [(1, 1100, 1100, 0), (0, 900, 2000, 0), (3, 1001, 1001, 0), (2, 770, 770, 0)], 769),    # 288 heads
+    (2, 1, [(0, 768, 768, 0)], 700), (2, 1, [(0, 769, 769, 0)], 700), (2, 1, [(0, 2049, 2049, 0)], 64),
+])
+def test_evict_by_blocks_of_either_size(layers, n_seq, spans, keep):
+    print("evict:", layers, "layers", spans, flush=True)
+    rng = np.random.default_rng(keep)
+    kv = make(8, 8, 64, n_seq=n_seq, max_seq=2050 if n_seq == 1 else 1100, n_layers=layers)
+    kv.cache.copy_(torch.from_numpy(rng.integers(0, 256, kv.cache.numel()).astype(np.uint8)))
+    for kind in ("spread", "ties"):
+        w, p = random_ledger(kv, spans, rng, kind)
+        check_evict(kv, (0, layers), spans, keep, keep // 5, w, p, into=kind == "ties")
+
+
 def test_evict_long():
     print("evict: 40000 slots", flush=True)
     rng = np.random.default_rng(8)
