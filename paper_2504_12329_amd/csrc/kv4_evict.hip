@@ -7,12 +7,11 @@
 //
 // A slot's rank is that of 64 bits: its class and weight (32 bits, larger first), then its position (lower first).
 // k_kv4_evict, one block per head, finds the keep-th by histograms of 11-bit digits in LDS until at most 128 slots share the
-// digits so far, and ranks those against each other; it writes a bit per slot and moves.  Bound by latency: weights and
-// positions are read once, the 32 bits kept in LDS (up to 24576 slots; beyond, they are read again for every digit).  128 heads
-// of 500 to 6000 slots to 1024: 20 us, of which 3 us are loads and the first histogram, 5 us the threshold and the bits, 2 us
-// the lists, 4 us the moves and the rest launch and drain; 56 heads of 577 slots to 512: 8.6 us. (Histograms over the range the
-// weights span, which need no second digit, cost a reduction first: 0.4 to 3 us slower.)  k_kv4_move: where few heads move many
-// slots, the moves by several blocks per head.
+// digits so far, and ranks those against each other; it writes a bit per slot and moves.  Weights and positions are read once,
+// the 32 bits kept in LDS (up to 24576 slots; beyond, they are read again for every digit).  Bound by latency, also of
+// instructions, as every line runs but a few times: 128 heads of 500 to 6000 slots to 1024 19 us, 21 with loops unrolled 8 and 16
+// times; 56 heads of 577 slots to 512 8.0 us.  (Histograms over the range that the weights span, which need no second digit, cost
+// a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the moves by several blocks per head.
 #include <mutex>
 
 #include "kv4.h"
@@ -140,7 +139,7 @@ struct Planes {  // of one layer, sequence and head
 // Slots late[i] to freed[i], i < m: D / 16 threads a slot, 16 bytes of codes each, a few slots' loads in flight
 template <int D, int THREADS>
 __device__ __forceinline__ void move_slots(const Planes &p, const int *late, const int *freed, int m) {
-    constexpr int CB = D / 2, SB = D / 32, TPM = CB / 16 * 2, U = 8;
+    constexpr int CB = D / 2, SB = D / 32, TPM = CB / 16 * 2, U = 4;
     for (int u0 = threadIdx.x; u0 < m * TPM; u0 += U * THREADS) {
         u32x4 x[U];
         uint32_t y[U];
@@ -221,7 +220,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
     int *mine = hist + (wave % COPIES) * kBins;
     // f(slot, its 32 bits) for all slots; whole waves, `in` says which lanes have one
     auto each = [&](auto f) {
-        constexpr int U = 4;
+        constexpr int U = HELD ? 1 : 4;
         for (int i0 = 0; i0 < n; i0 += U * THREADS) {
             uint32_t o[U];
 #pragma unroll
@@ -240,7 +239,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
         if (b && lane == 0) atomicAdd(&mine[0], __popcll(b));
     };
     if constexpr (HELD) {
-        constexpr int U = THREADS == 1024 ? 16 : 8;
+        constexpr int U = 4;
         for (int i0 = 0; i0 < n; i0 += U * THREADS) {
             int p[U];
             float w[U];
