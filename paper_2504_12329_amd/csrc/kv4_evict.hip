@@ -115,12 +115,14 @@ __device__ __forceinline__ int list_moves(const uint64_t *bits, int n, int keep,
                 total[h] += all;
                 if (!all || total[h] - all >= r0 + SIZE || total[h] <= r0) continue;  // none of the entries is in these words
                 int *list = h ? late : freed;
+                const bool inside = total[h] - all >= r0 && total[h] <= r0 + SIZE;
 #pragma unroll
                 for (int k = 0; k < 64; k += WAVES) {
                     const uint32_t y0 = __builtin_amdgcn_readlane((int)(uint32_t)x[h], k + wave), y1 = __builtin_amdgcn_readlane((int)(x[h] >> 32), k + wave);
                     if (!(y0 | y1)) continue;
                     const int r = __builtin_amdgcn_readlane(first, k + wave) + __builtin_amdgcn_mbcnt_hi(y1, __builtin_amdgcn_mbcnt_lo(y0, 0));
-                    if (((lane < 32 ? y0 : y1) >> (lane & 31) & 1) && r >= 0 && r < SIZE) list[r] = (w0 + k + wave) * 64 + lane;
+                    if (__builtin_amdgcn_inverse_ballot_w64((uint64_t)y1 << 32 | y0) && (inside || (uint32_t)r < (uint32_t)SIZE))
+                        list[r] = (w0 + k + wave) * 64 + lane;
                 }
             }
         }
@@ -232,11 +234,11 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
             for (int e = 0; e < U; ++e) f(i0 + e * THREADS + tid, o[e], i0 + e * THREADS + tid < n);
         }
     };
-    // a histogram entry; those that stay anyway are many, share a bin, and are counted by wave
-    auto count = [&](int bin, bool in, bool same) {
-        const uint64_t b = __builtin_amdgcn_ballot_w64(in && same);
-        if (in && !same) atomicAdd(&mine[bin], 1);
-        if (b && lane == 0) atomicAdd(&mine[0], __popcll(b));
+    // a histogram entry; those that stay anyway are many, share bin 0, and are counted aside
+    int anyway = 0;
+    auto count = [&](uint32_t o) {
+        if (o >> 21) atomicAdd(&mine[o >> 21], 1);
+        else ++anyway;
     };
     if constexpr (HELD) {
         constexpr int U = 4;
@@ -252,13 +254,19 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
             for (int e = 0; e < U; ++e) {
                 const int i = i0 + e * THREADS + tid;
                 const uint32_t o = order_of(w[e], p[e] >= fixed_from);
-                if (i < n) held[i] = o;
-                if (i0 + e * THREADS < n) count(o >> 21, i < n, o >> 21 == 0);
+                if (i < n) {
+                    held[i] = o;
+                    count(o);
+                }
             }
         }
     } else {
-        each([&](int, uint32_t o, bool in) { count(o >> 21, in, o >> 21 == 0); });
+        each([&](int, uint32_t o, bool in) {
+            if (in) count(o);
+        });
     }
+    anyway = wave_running_sum(anyway);
+    if (lane == 63 && anyway) atomicAdd(&mine[0], anyway);
     __syncthreads();
     // Digits of the 64 bits until few slots share them: `prefix` of the first `top` bits, of which `need` slots stay
     Bin b = find_bin<THREADS, COPIES>(hist, wsum, res, keep);
@@ -289,7 +297,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
         each([&](int i, uint32_t o, bool in) {
             const uint64_t word = all ? __builtin_amdgcn_ballot_w64(in && o <= high) : __builtin_amdgcn_ballot_w64(in && o < low);
             if (lane == 0 && in) bits[i >> 6] = word;
-            const bool like = in && o >= low && o <= high;
+            const bool like = in && o - low <= high - low;
             if (ranked && __builtin_amdgcn_ballot_w64(like)) {
                 if (like) {
                     const int at = atomicAdd(&n_near, 1);
