@@ -175,6 +175,13 @@ __device__ __forceinline__ void move_slots(const Planes &p, const int *late, con
     }
 }
 
+// The ledger's entries of the slots from `first` on that stay where they are, to another ledger
+template <int THREADS>
+__device__ __forceinline__ void copy_kept(const Planes &p, const uint64_t *bits, int first, int end) {
+    for (int i = first + threadIdx.x; i < end; i += THREADS)
+        if (bits[i >> 6] >> (i & 63) & 1) p.w_out[i] = p.w_in[i], p.p_out[i] = p.p_in[i];
+}
+
 struct EvictArgs {
     Kv4View view;  // of the first layer
     size_t k_layer, s_layer, layer_slots;
@@ -352,10 +359,8 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
             atomicOr(reinterpret_cast<unsigned long long *>(&bits[near_s[tid] >> 6]), 1ull << (near_s[tid] & 63));
         __syncthreads();
     }
-    if (copy)
-        for (int i = tid; i < keep; i += THREADS)
-            if (bits[i >> 6] >> (i & 63) & 1) pl.w_out[i] = pl.w_in[i], pl.p_out[i] = pl.p_in[i];
     if (a.parts) return;
+    if (copy) copy_kept<THREADS>(pl, bits, 0, keep);
     // the moves; the histogram's memory holds the lists
     constexpr int kList = THREADS;
     static_assert(2 * kList * sizeof(int) <= sizeof(hist), "lists in the histogram");
@@ -368,7 +373,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
     }
 }
 
-// Moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer further, of a head.  Bound by latency: listing 3 us,
+// Ledger entries of a part of the slots that stay, moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer further, of a head.  Bound by latency: listing 3 us,
 // then loads and stores.  16 heads with 2000 moves each: 28.0 us with the selection at 256 moves a block, 29.5 at 512, 31.2 at
 // 128.
 constexpr int kMoveThreads = 1024, kMovesPer = 256;
@@ -380,6 +385,10 @@ __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t
     if (n <= keep) return;
     const Planes pl = planes_of<D>(a, sp, kvh, blockIdx.z);
     const uint64_t *bits = a.kept + (((size_t)blockIdx.z * t.n + blockIdx.y) * a.view.nkv + kvh) * a.kept_words;
+    if (a.w_out != a.w_in) {
+        const int share = (keep + a.parts - 1) / a.parts;
+        copy_kept<kMoveThreads>(pl, bits, part * share, min(keep, (part + 1) * share));
+    }
     for (int r0 = part * kMovesPer;; r0 += a.parts * kMovesPer) {
         const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, r0, freed, late);
         move_slots<D, kMoveThreads>(pl, late, freed, min(total - r0, kMovesPer));

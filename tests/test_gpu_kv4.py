@@ -483,6 +483,18 @@ def test_evict_long():
         check_evict(kv, (0, 1), spans, keep, recent, w, p, into=keep == 700)
 
 
+@pytest.mark.parametrize("n,keep", [(9000, 4111), (30001, 12345), (7000, 5800)])
+def test_evict_long_into_another_ledger(n, keep):
+    """Many moves of few heads (their own launch, some of its blocks without any), the ledger's entries written elsewhere."""
+    print("evict: into another ledger", n, keep, flush=True)
+    rng = np.random.default_rng(n)
+    kv = make(2, 2, 64, n_seq=2, max_seq=n, n_layers=2)
+    kv.cache.copy_(torch.from_numpy(rng.integers(0, 256, kv.cache.numel()).astype(np.uint8)))
+    spans = [(1, n, 2 * n, 0), (0, keep + 3, keep + 3, 0)]
+    w, p = random_ledger(kv, spans, rng, "spread")
+    check_evict(kv, (0, 2), spans, keep, 100, w, p, into=True)
+
+
 def test_evict_with_positions_that_repeat():
     """A ledger that no append wrote: exactly `keep` slots stay all the same."""
     print("evict: repeated positions", flush=True)
