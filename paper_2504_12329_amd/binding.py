@@ -547,10 +547,12 @@ class Kv4Ledger:
             raise StError(ST_EINVAL, f"weights are float32 and positions int32, got {weights.dtype} and {positions.dtype}")
         if weights.shape != positions.shape or not weights.is_contiguous() or not positions.is_contiguous():
             raise StError(ST_EINVAL, "weights and positions are contiguous and of one shape")
-        if not weights.is_cuda or not positions.is_cuda:
-            raise StError(ST_EINVAL, "weights and positions must live on the GPU")
+        if not weights.is_cuda or positions.device != weights.device:
+            raise StError(ST_EINVAL, "weights and positions must live on one GPU")
         self.weights, self.positions = weights, positions
+        self.shape, self.device = tuple(weights.shape), weights.device
         self.c = st_kv4_ledger(weights.data_ptr(), positions.data_ptr())
+        self.ref = C.byref(self.c)
 
 
 def rope_table(max_pos, head_dim, theta, device="cuda"):
@@ -585,14 +587,14 @@ class Kv4Cache:
                 cache = torch.empty(cb.value, dtype=torch.uint8, device=dev)
         if cache.device != dev or cache.dtype != torch.uint8 or not cache.is_contiguous():
             raise StError(ST_EINVAL, "cache is a contiguous uint8 tensor on the device of rope")
-        self.cache, self.rope, self._dev = cache, rope, dev
+        self.cache, self.rope, self._dev, self._index = cache, rope, dev, dev.index
         h = C.c_void_p()
         _check(lib().st_kv4_create(C.byref(c), rope.data_ptr(), cache.data_ptr(), cache.numel(), self._ws.data_ptr(),
                                    wb.value, self.stream, C.byref(h)))
         self._h = h
         self._slots = (cfg["n_layers"], cfg["n_seq"], cfg["n_kv_heads"], cfg["max_seq"])
         self._nq, self._nkv, self._d = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"]
-        self._proto = torch.empty(0, dtype=torch.bfloat16, device=dev)
+        self._new = torch.empty(0, dtype=torch.bfloat16, device=dev).new_empty
         L = lib()
         self._append, self._attend, self._evict, self._read = L.st_kv4_append, L.st_kv4_attend, L.st_kv4_evict, L.st_kv4_read
 
@@ -610,18 +612,18 @@ class Kv4Cache:
     # A decode step makes these calls for every layer, so the checks below stay at a few attribute reads.
     def _alloc(self, *shape):
         if not self._own_stream:
-            return self._proto.new_empty(shape)
+            return self._new(*shape)
         with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self._dev)):
-            return self._proto.new_empty(shape)
+            return self._new(*shape)
 
     def _enter(self):
-        if not self._own_stream and torch._C._cuda_getCurrentRawStream(self._dev.index) != self.stream:
+        if not self._own_stream and torch._C._cuda_getCurrentRawStream(self._index) != self.stream:
             raise StError(ST_EINVAL, "called under another stream than the cache was made on")
 
     def _matrix(self, name, x, rows, heads):
         """(pointer, row stride) of bf16 [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
         d, shape = self._d, x.shape
-        if x.dtype is not torch.bfloat16 or x.device != self._dev:
+        if x.dtype is not torch.bfloat16 or x.get_device() != self._index:
             raise StError(ST_EINVAL, f"{name} is bfloat16 on {self._dev}, got {x.dtype} on {x.device}")
         if x.is_contiguous() and (shape == (rows, heads, d) or shape == (rows, heads * d)):
             return x.data_ptr(), heads * d
@@ -634,11 +636,11 @@ class Kv4Cache:
     def _ledger(self, ledger):
         if ledger is None:
             return None
-        if ledger.weights.shape != self._slots:
-            raise StError(ST_EINVAL, f"the ledger has shape {tuple(ledger.weights.shape)}, needs {self._slots}")
-        if ledger.weights.device != self._dev:
-            raise StError(ST_EINVAL, f"the ledger is on {ledger.weights.device}, the cache on {self._dev}")
-        return C.byref(ledger.c)
+        if ledger.shape != self._slots:
+            raise StError(ST_EINVAL, f"the ledger has shape {ledger.shape}, needs {self._slots}")
+        if ledger.device != self._dev:
+            raise StError(ST_EINVAL, f"the ledger is on {ledger.device}, the cache on {self._dev}")
+        return ledger.ref
 
     def append(self, layer, spans, qkv, q_norm=None, k_norm=None, ledger=None):
         """Norms (bf16 [head_dim], or None), rotation and the write of the spans' new rows; qkv: bf16, a row per new token, all query
@@ -658,7 +660,7 @@ class Kv4Cache:
     def _norm(self, name, w):
         if w is None:
             return None
-        if w.dtype is not torch.bfloat16 or w.shape != (self._d,) or not w.is_contiguous() or w.device != self._dev:
+        if w.dtype is not torch.bfloat16 or w.shape != (self._d,) or not w.is_contiguous() or w.get_device() != self._index:
             raise StError(ST_EINVAL, f"{name} is bfloat16 [{self._d}] on {self._dev}, got {w.dtype} {tuple(w.shape)}")
         return w.data_ptr()
 
