@@ -9,9 +9,10 @@
 // k_kv4_evict, one block per head, finds the keep-th by histograms of 11-bit digits in LDS until at most 128 slots share the
 // digits so far, and ranks those against each other; it writes a bit per slot and moves.  Weights and positions are read once,
 // the 32 bits kept in LDS (up to 24576 slots; beyond, they are read again for every digit).  Bound by latency, also of
-// instructions, as every line runs but a few times: 128 heads of 500 to 6000 slots to 1024 19 us, 21 with loops unrolled 8 and 16
-// times; 56 heads of 577 slots to 512 8.0 us.  (Histograms over the range that the weights span, which need no second digit, cost
-// a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the moves by several blocks per head.
+// instructions, as every line runs but a few times: 128 heads of 500 to 6000 slots to 1024 18 us, 21 with loops unrolled 8 and
+// 16 times; 56 heads of 577 slots to 512 8.0 us, 16 heads of 16385 slots 15.4 us.  (Histograms over the range that the weights
+// span, which need no second digit, cost a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the
+// moves by several blocks per head.
 #include <mutex>
 
 #include "kv4.h"
@@ -373,9 +374,9 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
     }
 }
 
-// Ledger entries of a part of the slots that stay, moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer further, of a head.  Bound by latency: listing 3 us,
-// then loads and stores.  16 heads with 2000 moves each: 28.0 us with the selection at 256 moves a block, 29.5 at 512, 31.2 at
-// 128.
+// Ledger entries of a part of the slots that stay, and moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer
+// further, of a head.  Bound by latency: listing, then loads and stores.  16 heads with 2000 moves each 10.9 us; with the
+// selection, measured at the time, 28.0 us at 256 moves a block, 29.5 at 512, 31.2 at 128.
 constexpr int kMoveThreads = 1024, kMovesPer = 256;
 template <int D, int CAP>
 __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t, const EvictArgs a) {
