@@ -941,12 +941,15 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
         few_tiles += (cols + 31) / 32 * nkv * ((held + kFewTile - 1) / kFewTile);
         chunk_tiles += (cols + kTileCols - 1) / kTileCols * nkv * ((held + kTileKeys - 1) / kTileKeys);
     }
-    // A tile of 32 columns x 32 slots takes the chip about 1 ns in k_kv4_few, one of 128 x 128 about 8.8 ns in k_kv4_chunk,
-    // which takes some 14 us more to get going.  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 : 21.5 us, 64 rows
-    // 21.9 : 30.8, 160 rows 37.9 : 43.0, 260 rows 59.2 : 56.0.
-    const bool few = most <= 16 || few_tiles <= 14000 + 88 * chunk_tiles / 10;
-    // The weights of up to 64 columns beside the join, in one launch; of more than 32 only while that launch is short.  Rows of 40 / 8 heads, one launch against
-    // two: 4 sequences x 12 rows on 500 to 4000 slots 22.6 : 23.7 us, 16 x 12 rows 69.2 : 57.4, 16 x 6 rows 32.8 : 45.6.
+    // k_kv4_chunk takes longer to get going and to join its larger partial results, k_kv4_few dequantises for 32 columns at a
+    // time: a line between them over the tiles of 32 x 32 and of 128 x 128 that each has, fitted to 96 shapes of 1 to 32
+    // sequences (0.8 % lost to the better form in the mean).  40 / 8 heads on 4096 slots, few against chunk: 20 rows 15.2 :
+    // 21.5 us, 86 rows 26.6 : 31.7, 200 rows 35.9 : 44.5, 300 rows 55.6 : 53.2, 500 rows 83.6 : 74.8; 12 sequences with 150 to
+    // 300 rows on 128 to 1500 slots 110 : 76.
+    const bool few = most <= 16 || few_tiles <= 10000 + 116 * chunk_tiles / 10;
+    // The weights of up to 64 columns beside the join, in one launch; of more than 32 only while that launch is short.  Rows of
+    // 40 / 8 heads, one launch against two: 4 sequences x 12 rows on 500 to 4000 slots 22.6 : 23.7 us, 16 x 12 rows 69.2 :
+    // 57.4, 16 x 6 rows 32.8 : 45.6.
     const bool fused = weights && few && (most <= 32 || (most <= 64 && few_tiles <= 6000));
     Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, fused, 0, 0};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };

@@ -82,7 +82,7 @@ def test_the_reference_is_the_plain_one():
 SHAPES = [                                               # and whether the slots are cut into ranges
     (40, 8, 128, [(1, 1490, 0, 523)], True),
     (14, 2, 64, [(0, 0, 0, 1100), (2, 777, 0, 901), (1, 5, 0, 0), (3, 3000, 0, 300)], True),
-    (5, 5, 128, [(0, 9000, 0, 768)], True),
+    (5, 5, 128, [(0, 9000, 0, 968)], True),
     (16, 1, 64, [(0, 8003, 0, 300)], True),
     (16, 1, 128, [(1, 3, 0, 1500), (0, 1, 0, 1501)], False),    # little but the diagonal
     (40, 8, 64, [(0, 0, 0, 1300)], False),
@@ -102,7 +102,7 @@ def test_chunks(nq, nkv, d, spans, cut):
     run(kv, spans, rng, with_ledger=False, scale=2.0)
 
 
-@pytest.mark.parametrize("nq,nkv,d,n,rows", [(40, 8, 128, 1490, 523), (14, 2, 64, 1500, 1600), (5, 5, 128, 9000, 768)])
+@pytest.mark.parametrize("nq,nkv,d,n,rows", [(40, 8, 128, 1490, 523), (14, 2, 64, 1500, 1600), (5, 5, 128, 9000, 968)])
 @pytest.mark.parametrize("side", [0, 1])
 def test_chunks_with_groups_without_numbers(nq, nkv, d, n, rows, side):
     """In a slot that every row sees, in one on the diagonal and in the last one, each in another kv head."""
