@@ -703,9 +703,11 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
     float *dst = weights + head0;
     if constexpr (STORED) {
         const float *col[kScoreCols];
+        int lim[kScoreCols];  // last slot the column sees
 #pragma unroll
         for (int c = 0; c < kScoreCols; ++c) {
             const Column w = column_of(min(c, cols - 1), G, kvh);
+            lim[c] = c < cols ? sp.len + w.row : -1;
             col[c] = scores + ((int64_t)(sp.row0 + w.row) * view.nq + w.head) * score_stride;
         }
         for (int key = t_begin * kFewTile + threadIdx.x; key < min(t_end * kFewTile, n_keys); key += 256) {
@@ -714,9 +716,9 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
 #pragma unroll
             for (int c = 0; c < kScoreCols; ++c) v[c] = col[c][key];
 #pragma unroll
-            for (int c = 0; c < kScoreCols; ++c) {  // (a slot that a row does not see has the score -infinity)
+            for (int c = 0; c < kScoreCols; ++c) {  // (selected, as a row without numbers has none for the slots it does not see either)
                 const float p = __builtin_amdgcn_exp2f(fmaf(v[c], scale, -base_s[c]));
-                sum += c < cols ? p : 0.f;
+                sum += key <= lim[c] ? p : 0.f;
             }
             dst[key] = was + sum;
         }

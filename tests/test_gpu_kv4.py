@@ -369,6 +369,31 @@ def test_a_query_without_numbers_stays_in_its_row_and_head():
         assert torch.equal(good, bad)
 
 
+@pytest.mark.parametrize("d,rows,context", [(64, 2, 40), (128, 2, 700), (128, 3, 513), (64, 4, 0), (128, 7, 60), (64, 7, 900), (128, 14, 300),
+                                            (128, 30, 33), (64, 40, 500)])
+@pytest.mark.parametrize("odd", [math.nan, math.inf])
+def test_a_query_without_numbers_leaves_weights_of_slots_that_its_row_does_not_see(d, rows, context, odd):
+    """In the first row and in one within: the weights of the slots that those rows see are no numbers, those of later rows' slots and of the other kv head are.
+    Rows of two heads a kv head, in every form that sums up weights: from stored scores (up to 8 columns), beside the join, by columns in blocks."""
+    print("attend: a query without numbers, weights", d, rows, context, odd, flush=True)
+    rng = np.random.default_rng(rows + context)
+    kv = make(4, 2, d, max_seq=context + rows + 3, fill=0xff)
+    for bad in sorted({0, rows // 2}):
+        k, v = put(kv, 0, 1, context + rows, rng)
+        q = bf16(rng.standard_normal((rows, 4, d)) * 0.3)
+        q[bad, 1, d - 3] = odd
+        led = ledger_for(kv, rng)
+        w0 = f64(led.weights)
+        kv.attend(0, B.Kv4Spans([(1, context, 0, rows)]), q, led)
+        q[bad, 1, d - 3] = math.nan                      # (an infinity times any key is none either: all of the row's scores are without numbers)
+        w0[0, 1, :, :context + rows] += R.attention(f64(q), k, v, context)[2]
+        got = f64(led.weights)
+        assert np.isnan(w0).sum() == context + bad + 1
+        assert np.array_equal(np.isnan(got), np.isnan(w0)), np.argwhere(np.isnan(got) != np.isnan(w0))[:5]
+        fine = ~np.isnan(w0)
+        assert (np.abs(got - w0)[fine] <= WEIGHT_TOL * w0[fine]).all()
+
+
 def test_offsets_past_32_bits():
     """Planes of more than 4 GB: the last sequence of 40, its context at the end of its slots."""
     print("planes of 5 GB", flush=True)
