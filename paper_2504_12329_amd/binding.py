@@ -616,9 +616,11 @@ class Kv4Cache:
         with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self._dev)):
             return self._new(*shape)
 
-    def _enter(self):
+    def _elsewhere(self):
+        """Whether another GPU than the cache's is current: a launch would go there, whichever GPU its pointers are on."""
         if not self._own_stream and torch._C._cuda_getCurrentRawStream(self._index) != self.stream:
             raise StError(ST_EINVAL, "called under another stream than the cache was made on")
+        return torch._C._cuda_getDevice() != self._index
 
     def _matrix(self, name, x, rows, heads):
         """(pointer, row stride) of bf16 [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
@@ -645,7 +647,9 @@ class Kv4Cache:
     def append(self, layer, spans, qkv, q_norm=None, k_norm=None, ledger=None):
         """Norms (bf16 [head_dim], or None), rotation and the write of the spans' new rows; qkv: bf16, a row per new token, all query
         heads, then key heads, then value heads.  Returns the rotated queries, bf16 [rows][n_q_heads][head_dim]."""
-        self._enter()
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.append(layer, spans, qkv, q_norm, k_norm, ledger)
         p, stride = self._matrix("qkv", qkv, spans.rows, self._nq + 2 * self._nkv)
         qn = kn = None
         if q_norm is not None or k_norm is not None:
@@ -667,7 +671,9 @@ class Kv4Cache:
     def attend(self, layer, spans, q, ledger=None, out=None):
         """Attention of the spans' rows over their sequences' slots; q: bf16, n_q_heads * head_dim a row.  With a ledger its weights grow by what every
         slot received.  Returns bf16 [rows][n_q_heads][head_dim] (or `out`)."""
-        self._enter()
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.attend(layer, spans, q, ledger, out)
         p, stride = self._matrix("q", q, spans.rows, self._nq)
         if out is None:
             out = self._alloc(spans.rows, self._nq, self._d)
@@ -689,12 +695,16 @@ class Kv4Cache:
 
     def evict(self, layer_lo, layer_hi, spans, keep, recent, ledger, into=None):
         """Brings the spans' sequences to `keep` slots in layers [layer_lo, layer_hi) (see st_kv4_evict); the ledger's entries move along, in place or to `into`."""
-        self._enter()
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.evict(layer_lo, layer_hi, spans, keep, recent, ledger, into)
         _check(self._evict(self._h, layer_lo, layer_hi, spans.c, spans.n, keep, recent, self._ledger(ledger), self._ledger(into)))
 
     def read(self, layer_lo, layer_hi, spans):
         """Slots [len, len + rows) of the spans as bf16 (k, v), each [layers][rows][n_kv_heads][head_dim]."""
-        self._enter()
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.read(layer_lo, layer_hi, spans)
         layers = max(layer_hi - layer_lo, 0)
         k = self._alloc(layers, spans.rows, self._nkv, self._d)
         v = self._alloc(layers, spans.rows, self._nkv, self._d)
