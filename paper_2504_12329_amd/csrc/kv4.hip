@@ -311,8 +311,7 @@ static int check_ledger(const st_kv4_ledger *l, const char *name) {
     if (((uintptr_t)l->weights | (uintptr_t)l->positions) & 3) return fail(ST_EINVAL, "%s is not aligned to 4 bytes", name);
     return ST_OK;
 }
-static int launched(const char *what) {
-    const hipError_t e = hipGetLastError();
+static int launched(const char *what, hipError_t e) {
     return e == hipSuccess ? ST_OK : fail(ST_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
@@ -378,7 +377,7 @@ int st_kv4_append(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     launch_kv4_append(*k, layer, t, rows, (const bf16_t *)qkv, qkv_stride, (const bf16_t *)q_norm, (const bf16_t *)k_norm,
                       (bf16_t *)q_out, q_stride, ledger ? ledger->weights + base : nullptr,
                       ledger ? ledger->positions + base : nullptr);
-    return launched("st_kv4_append");
+    return launched("st_kv4_append", hipGetLastError());
 }
 
 int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n, const void *q, int64_t q_stride, void *out,
@@ -400,7 +399,7 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
     const size_t base = (size_t)layer * k->c.n_seq * k->c.n_kv_heads * k->c.max_seq;
     launch_kv4_attend(*k, layer, t, (const bf16_t *)q, q_stride, (bf16_t *)out, out_stride,
                       ledger ? ledger->weights + base : nullptr);
-    return launched("st_kv4_attend");
+    return launched("st_kv4_attend", hipGetLastError());
 }
 
 int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32_t n, int32_t with_ledger, int32_t *columns, int32_t *blocks,
@@ -446,8 +445,7 @@ int st_kv4_evict(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_spa
     if (partly(into->weights, ledger->weights) || partly(into->positions, ledger->positions))
         return fail(ST_EINVAL, "into and ledger overlap");
     if (!n || layer_lo == layer_hi) return ST_OK;
-    launch_kv4_evict(*k, layer_lo, layer_hi, t, keep, recent, ledger->weights, ledger->positions, into->weights, into->positions);
-    return launched("st_kv4_evict");
+    return launched("st_kv4_evict", launch_kv4_evict(*k, layer_lo, layer_hi, t, keep, recent, ledger->weights, ledger->positions, into->weights, into->positions));
 }
 
 int st_kv4_read(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, void *k_out, void *v_out) {
@@ -461,7 +459,7 @@ int st_kv4_read(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_span
     if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return fail(ST_EINVAL, "k_out or v_out is not aligned to 16 bytes");
     if (!rows || layer_lo == layer_hi) return ST_OK;
     launch_kv4_read(*k, layer_lo, layer_hi, t, rows, (bf16_t *)k_out, (bf16_t *)v_out);
-    return launched("st_kv4_read");
+    return launched("st_kv4_read", hipGetLastError());
 }
 
 }  // extern "C"

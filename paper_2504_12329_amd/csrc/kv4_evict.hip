@@ -13,7 +13,7 @@
 // 16 times; 56 heads of 577 slots to 512 8.0 us, 16 heads of 16385 slots 15.4 us.  (Histograms over the range that the weights
 // span, which need no second digit, cost a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the
 // moves by several blocks per head.
-#include <mutex>
+#include <atomic>
 
 #include "kv4.h"
 #include "st_device.h"
@@ -402,12 +402,24 @@ __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t
 // in two launches, 20.9 in one)
 constexpr int kMoveMany = 1024, kMoveHeads = 128;
 
+// Up to 99 KB of LDS are asked for at the launch of a block of 1024 threads: allowed once per kernel and GPU
 template <int D, int CAP>
-static void evict_in(const Kv4 &k, const Kv4Spans<CAP> &t, const EvictArgs &a, int longest, dim3 grid) {
+static hipError_t allow_held_lds() {
+    static std::atomic<uint64_t> allowed{0};  // a bit per GPU; those past 64 are asked every time
+    int gpu = 0;
+    hipError_t e = hipGetDevice(&gpu);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = gpu >= 0 && gpu < 64 ? 1ull << gpu : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_kv4_evict<D, 1024, true, CAP>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kHeldSlots * 4 + kHeldSlots / 8);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
+template <int D, int CAP>
+static hipError_t evict_in(const Kv4 &k, const Kv4Spans<CAP> &t, const EvictArgs &a, int longest, dim3 grid) {
     const size_t bit_bytes = (size_t)((longest + 63) / 64) * 8;
-    auto raised = [](auto *kern) {  // once per kernel: up to 115 KB of LDS asked for at the launch
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 4 + kHeldSlots / 8);
-    };
     // Blocks of 256 threads for short contexts (cheaper barriers and scans) and, where there is more than one block a compute unit, for longer ones, as two
     // of 1024 threads do not run side by side.  256 : 1024 threads, 56 heads of 300 slots 8.0 : 9.5 us, of 1100 16.6 : 11.9; 320 heads of 700 slots
     // 11.7 : 19.6, of 2500 25.5 : 27.4, of 4000 47.6 : 42.0.
@@ -415,16 +427,17 @@ static void evict_in(const Kv4 &k, const Kv4Spans<CAP> &t, const EvictArgs &a, i
     if (longest <= (heads > 256 ? 2560 : 768)) {
         hipLaunchKernelGGL((k_kv4_evict<D, 256, true, CAP>), grid, dim3(256), bit_bytes + 4 * (size_t)longest, k.stream, t, a);
     } else if (longest <= kHeldSlots) {
-        static std::once_flag once;
-        std::call_once(once, [&] { raised(k_kv4_evict<D, 1024, true, CAP>); });
+        const hipError_t e = allow_held_lds<D, CAP>();
+        if (e != hipSuccess) return e;
         hipLaunchKernelGGL((k_kv4_evict<D, 1024, true, CAP>), grid, dim3(1024), bit_bytes + 4 * (size_t)longest, k.stream, t, a);
     } else {
         hipLaunchKernelGGL((k_kv4_evict<D, 1024, false, CAP>), grid, dim3(1024), longest <= kBitSlots ? bit_bytes : kBitSlots / 8, k.stream, t, a);
     }
     if (a.parts) hipLaunchKernelGGL((k_kv4_move<D, CAP>), dim3(grid.x * a.parts, grid.y, grid.z), dim3(kMoveThreads), 0, k.stream, t, a);
+    return hipGetLastError();
 }
 
-void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
+hipError_t launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
                       const int32_t *p_in, float *w_out, int32_t *p_out) {
     const int nkv = k.c.n_kv_heads, layers = layer_hi - layer_lo;
     const size_t slots = (size_t)k.c.n_seq * nkv * k.c.max_seq, off = slots * layer_lo;
@@ -434,10 +447,12 @@ void launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &
     const int parts = moves > kMoveMany && nkv * t.n * layers < kMoveHeads ? (moves + kMovesPer - 1) / kMovesPer : 0;
     const EvictArgs a = {k.view(layer_lo), k.per_layer[0], k.per_layer[2], slots, keep, recent, parts, w_in + off, p_in + off, w_out + off,
                          p_out + off, k.kept, k.kept_words};
+    hipError_t e = hipSuccess;
     with_table(t, [&](auto tab) {
-        if (k.c.head_dim == 128) evict_in<128>(k, tab, a, longest, dim3(nkv, t.n, layers));
-        else evict_in<64>(k, tab, a, longest, dim3(nkv, t.n, layers));
+        const dim3 grid(nkv, t.n, layers);
+        e = k.c.head_dim == 128 ? evict_in<128>(k, tab, a, longest, grid) : evict_in<64>(k, tab, a, longest, grid);
     });
+    return e;
 }
 
 }  // namespace st
