@@ -460,7 +460,7 @@ int st_kv4_attend_plan(const st_kv4_config *cfg, const st_kv4_span *spans, int32
  * equal weights by the lower position, a NaN below every weight.  The slots below `keep` that are freed take, in ascending order, the slots at or above it that stay, in
  * ascending order; nothing else moves.  Pass len = keep from then on.  The ledger's entries move along: in `ledger` itself if `into` is
  * NULL, else to the slots [0, min(len, keep)) of `into`, and `ledger` stays as it was.  ST_EINVAL: keep <= 0, recent outside [0, keep],
- * `into` and `ledger` overlap in part. */
+ * `into` is neither the ledger itself nor two arrays apart from each other and from the ledger's. */
 int st_kv4_evict(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, int32_t keep,
                  int32_t recent, const st_kv4_ledger *ledger, const st_kv4_ledger *into);
 

@@ -438,11 +438,13 @@ int st_kv4_evict(st_kv4 *h, int32_t layer_lo, int32_t layer_hi, const st_kv4_spa
     if ((into->weights == ledger->weights) != (into->positions == ledger->positions))
         return fail(ST_EINVAL, "into shares one array with ledger and not the other");
     const size_t bytes = 4 * (size_t)k->c.n_layers * k->c.n_seq * k->c.n_kv_heads * k->c.max_seq;
-    auto partly = [&](const void *a, const void *b) {
+    auto overlap = [&](const void *a, const void *b) {
         const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-        return x != y && (x < y ? y - x : x - y) < bytes;
+        return (x < y ? y - x : x - y) < bytes;
     };
-    if (partly(into->weights, ledger->weights) || partly(into->positions, ledger->positions))
+    if (into->weights != ledger->weights &&
+        (overlap(into->weights, ledger->weights) || overlap(into->positions, ledger->positions) || overlap(into->weights, ledger->positions) ||
+         overlap(into->positions, ledger->weights) || overlap(into->weights, into->positions)))
         return fail(ST_EINVAL, "into and ledger overlap");
     if (!n || layer_lo == layer_hi) return ST_OK;
     return launched("st_kv4_evict", launch_kv4_evict(*k, layer_lo, layer_hi, t, keep, recent, ledger->weights, ledger->positions, into->weights, into->positions));

@@ -210,3 +210,20 @@ def test_ranges_stay_within_what_the_workspace_holds(L):
                         assert rc == B.ST_OK and min(ranges) >= 1 and max(ranges) <= 64
                         assert blocks == sum(r * nkv * -(-rows * (nq // nkv) // columns) for r in ranges)
                         assert not cut or (blocks <= 512 and sum(cut) * rows * nq <= held), (nq, nkv, max_rows, n, rows, length)
+
+
+def test_evict_into_the_other_array_of_the_ledger(L, kv):
+    """`into` may be the ledger or lie apart from it: its weights where the ledger's positions are, or the reverse, is refused as any other overlap."""
+    s, n = spans((0, 300, 500, 0))
+    size, base = 4 * 3 * 5 * 2 * 1000, 0x10000000
+    led, far = B.st_kv4_ledger(base, base + 4 * size), base + 64 * size
+    for off in (0, 4, size - 4, -4, 4 - size):
+        for into in ((base + 4 * size + off, far), (far, base + off)):
+            assert L.st_kv4_evict(kv, 0, 3, s, n, 100, 10, C.byref(led), C.byref(B.st_kv4_ledger(*into))) == B.ST_EINVAL
+            assert b"overlap" in L.st_last_error()
+    assert L.st_kv4_evict(kv, 0, 3, s, n, 100, 10, C.byref(led), C.byref(B.st_kv4_ledger(led.positions, led.weights))) == B.ST_EINVAL
+    for off in (0, 4, 4 - size):                          # an `into` whose arrays share memory
+        assert L.st_kv4_evict(kv, 0, 3, s, n, 100, 10, C.byref(led), C.byref(B.st_kv4_ledger(far, far + off))) == B.ST_EINVAL
+    none = spans()
+    for off in (size, -size):                             # side by side
+        assert L.st_kv4_evict(kv, 0, 3, *none, 100, 10, C.byref(led), C.byref(B.st_kv4_ledger(base + 4 * size + off, far))) == B.ST_OK
