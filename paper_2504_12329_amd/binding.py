@@ -530,11 +530,19 @@ def st_generate_batch(small, large, prompts, n_out, n_seg, vocab, kw=None, delim
     return dict(seqs=seqs, srcs=srcs, stats={k: getattr(stats, k) for k, _ in st_gen_stats._fields_})
 
 
+def _fits32(what, *numbers):
+    """ctypes cuts numbers down to 32 bits without a word."""
+    if min(numbers) < -2 ** 31 or max(numbers) >= 2 ** 31:
+        raise StError(ST_ERANGE, f"{what}: {numbers} does not fit 32 bits")
+
+
 class Kv4Spans:
     """The spans of a call, (seq, len, pos, rows) each (see st_kv4_span); made once for all layers of a step."""
 
     def __init__(self, spans):
         self.spans = [tuple(int(x) for x in s) for s in spans]
+        if self.spans:
+            _fits32("spans", min(map(min, self.spans)), max(map(max, self.spans)))
         self.n, self.rows = len(self.spans), sum(s[3] for s in self.spans)
         self.c = (st_kv4_span * max(self.n, 1))(*self.spans)
 
@@ -570,6 +578,7 @@ class Kv4Cache:
 
     def __init__(self, cfg, rope, cache=None, stream=None):
         self.cfg = dict(cfg)
+        _fits32("config", *(cfg[n] for n, t in st_kv4_config._fields_ if t is C.c_int32))
         c = st_kv4_config(*(cfg[n] for n, _ in st_kv4_config._fields_))
         cb, wb = C.c_size_t(), C.c_size_t()
         _check(lib().st_kv4_query_sizes(C.byref(c), C.byref(cb), C.byref(wb)))
@@ -656,6 +665,8 @@ class Kv4Cache:
             qn, kn = self._norm("q_norm", q_norm), self._norm("k_norm", k_norm)
         out = self._alloc(spans.rows, self._nq, self._d)
         if spans.rows:
+            if not 0 <= layer < self._slots[0]:
+                raise StError(ST_ERANGE, f"layer {layer} outside [0, {self._slots[0]})")
             rc = self._append(self._h, layer, spans.c, spans.n, p, stride, qn, kn, out.data_ptr(), self._nq * self._d, self._ledger(ledger))
             if rc:
                 _check(rc)
@@ -681,6 +692,8 @@ class Kv4Cache:
         else:
             po, so = self._matrix("out", out, spans.rows, self._nq)
         if spans.rows:
+            if not 0 <= layer < self._slots[0]:
+                raise StError(ST_ERANGE, f"layer {layer} outside [0, {self._slots[0]})")
             rc = self._attend(self._h, layer, spans.c, spans.n, p, stride, po, so, self._ledger(ledger))
             if rc:
                 _check(rc)
@@ -698,6 +711,8 @@ class Kv4Cache:
         if self._elsewhere():
             with torch.cuda.device(self._index):
                 return self.evict(layer_lo, layer_hi, spans, keep, recent, ledger, into)
+        if (layer_lo | layer_hi | keep | recent) >> 31:     # one of them is negative, or large
+            _fits32("evict", layer_lo, layer_hi, keep, recent)
         _check(self._evict(self._h, layer_lo, layer_hi, spans.c, spans.n, keep, recent, self._ledger(ledger), self._ledger(into)))
 
     def read(self, layer_lo, layer_hi, spans):
@@ -705,6 +720,8 @@ class Kv4Cache:
         if self._elsewhere():
             with torch.cuda.device(self._index):
                 return self.read(layer_lo, layer_hi, spans)
+        if (layer_lo | layer_hi) >> 31:
+            _fits32("read", layer_lo, layer_hi)
         layers = max(layer_hi - layer_lo, 0)
         k = self._alloc(layers, spans.rows, self._nkv, self._d)
         v = self._alloc(layers, spans.rows, self._nkv, self._d)

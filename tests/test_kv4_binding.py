@@ -69,3 +69,42 @@ def test_errors_of_the_library_are_raised_on_any_device(monkeypatch):
             with pytest.raises(B.StError) as e:
                 call()
             assert e.value.code == B.ST_EINVAL and device.current == current
+
+
+class Test32Bits:
+    """Numbers past 32 bits are refused: ctypes would cut them down, and position 2^32 + 5 would be position 5."""
+
+    @pytest.mark.parametrize("field", range(4))
+    @pytest.mark.parametrize("value", [2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 63, -2 ** 31 - 1, -2 ** 32])
+    def test_spans(self, field, value):
+        span = [0, 1, 2, 1]
+        span[field] = value
+        for spans in ([span], [(0, 0, 0, 1), span], [span, (3, 0, 0, 1)]):
+            with pytest.raises(B.StError) as e:
+                B.Kv4Spans(spans)
+            assert e.value.code == B.ST_ERANGE
+
+    def test_spans_that_fit(self):
+        s = B.Kv4Spans([(0, 2 ** 31 - 1, 2 ** 31 - 1, 1), (-2 ** 31, -1, 0, 0)])
+        assert [(x.seq, x.len, x.pos, x.rows) for x in s.c] == s.spans == [(0, 2 ** 31 - 1, 2 ** 31 - 1, 1), (-2 ** 31, -1, 0, 0)]
+        assert B.Kv4Spans([]).rows == 0 and B.Kv4Spans(iter([[1, 2, 3, 4]])).spans == [(1, 2, 3, 4)]
+
+    @pytest.mark.parametrize("past", [2 ** 32, -2 ** 32])
+    def test_arguments(self, past, monkeypatch):
+        seen, one, x = [], B.Kv4Spans([(0, 0, 0, 1)]), torch.zeros(1, 8 * 64, dtype=torch.bfloat16)
+        kv = cache_on(1, seen)
+        monkeypatch.setattr(kv, "_elsewhere", lambda: False, raising=False)
+        for call in (lambda: kv.append(past, one, x), lambda: kv.attend(past, one, x[:, :256]), lambda: kv.evict(past, past + 1, one, 1, 0, None),
+                     lambda: kv.evict(0, past + 1, one, 1, 0, None), lambda: kv.evict(0, 1, one, past + 1, 0, None), lambda: kv.evict(0, 1, one, 1, past, None),
+                     lambda: kv.read(past, past + 1, one), lambda: kv.read(0, past + 1, one)):
+            with pytest.raises(B.StError) as e:
+                call()
+            assert e.value.code == B.ST_ERANGE
+        assert not seen
+
+    def test_configurations(self):
+        cfg = dict(n_layers=1, n_seq=1, n_q_heads=2, n_kv_heads=1, head_dim=64, max_seq=8, max_rows=8, max_pos=8, rms_eps=1e-6)
+        for name in set(cfg) - {"rms_eps"}:
+            with pytest.raises(B.StError) as e:
+                B.Kv4Cache(dict(cfg, **{name: cfg[name] + 2 ** 32}), torch.zeros(8, 32, 2))
+            assert e.value.code == B.ST_ERANGE
