@@ -83,8 +83,8 @@ void launch_kv4_append(const Kv4 &k, int layer, const Kv4Table &t, int rows, con
                        const bf16_t *q_norm, const bf16_t *k_norm, bf16_t *q_out, int64_t q_stride, float *weights,
                        int32_t *positions);
 void launch_kv4_read(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int rows, bf16_t *k_out, bf16_t *v_out);
-void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
-                       float *weights);
+int launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
+                      float *weights);  // ST_ERANGE, and nothing launched, where no grid holds the weights' blocks
 hipError_t launch_kv4_evict(const Kv4 &k, int layer_lo, int layer_hi, const Kv4Table &t, int keep, int recent, const float *w_in,
                             const int32_t *p_in, float *w_out, int32_t *p_out);  // with the error that its launches ended in
 

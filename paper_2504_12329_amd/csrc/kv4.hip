@@ -397,8 +397,9 @@ int st_kv4_attend(st_kv4 *h, int32_t layer, const st_kv4_span *spans, int32_t n,
         if (int rc = check_ledger(ledger, "ledger")) return rc;
     if (!rows) return ST_OK;
     const size_t base = (size_t)layer * k->c.n_seq * k->c.n_kv_heads * k->c.max_seq;
-    launch_kv4_attend(*k, layer, t, (const bf16_t *)q, q_stride, (bf16_t *)out, out_stride,
-                      ledger ? ledger->weights + base : nullptr);
+    if (int rc = launch_kv4_attend(*k, layer, t, (const bf16_t *)q, q_stride, (bf16_t *)out, out_stride,
+                                   ledger ? ledger->weights + base : nullptr))
+        return rc;
     return launched("st_kv4_attend", hipGetLastError());
 }
 

@@ -978,8 +978,8 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
     return p;
 }
 
-void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
-                       float *weights) {
+int launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, int64_t q_stride, bf16_t *out, int64_t out_stride,
+                      float *weights) {
     const int nkv = k.c.n_kv_heads, D = k.c.head_dim;
     const Kv4View view = k.view(layer);
     float *lse = weights ? k.lse : nullptr;
@@ -988,6 +988,12 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
     const int blocks = plan.blocks, join = plan.join;
     const int64_t most = plan.most, score_stride = plan.score_stride;
     float *scores = score_stride ? k.part_o + plan.score_at : nullptr;
+    int64_t weight_blocks = 0;  // of k_kv4_weights
+    if (weights && !fused)
+        for (int j = 0; j < t.n; ++j)
+            if (t.s[j].rows) weight_blocks += (int64_t)nkv * ((t.s[j].len + t.s[j].rows + kWeightKeys - 1) / kWeightKeys);
+    // a launch has at most 2^32 - 1 threads a direction (asked before anything is launched)
+    if (weight_blocks >= 1 << 24) return fail(ST_ERANGE, "weights of 2^30 slots or more, over all spans and kv heads");
     with_table(t, [&](auto tab) {
         constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
         const int nq = k.c.n_q_heads, units = join * nq;
@@ -1046,11 +1052,12 @@ void launch_kv4_attend(const Kv4 &k, int layer, Kv4Table &t, const bf16_t *q, in
             // Eight waves share a block's columns while there is at most one block a compute unit: 125 rows of 12 / 2 heads on
             // 3000 slots 23.6 us with the attention against 26.4, 86 rows of 40 / 8 heads on 4096 (528 blocks) 44.6 against
             // 40.4.
-            const bool wide = blk <= 256;
+            const bool wide = weight_blocks <= 256;
             auto *kern = D == 128 ? (wide ? k_kv4_weights<128, 8, CAP> : k_kv4_weights<128, 4, CAP>) : (wide ? k_kv4_weights<64, 8, CAP> : k_kv4_weights<64, 4, CAP>);
-            hipLaunchKernelGGL(kern, dim3(blk), dim3(wide ? 512 : 256), 0, k.stream, tab, view, q, q_stride, lse, weights);
+            hipLaunchKernelGGL(kern, dim3(weight_blocks), dim3(wide ? 512 : 256), 0, k.stream, tab, view, q, q_stride, lse, weights);
         });
     }
+    return ST_OK;
 }
 
 }  // namespace st

@@ -123,11 +123,31 @@ static int lds_refused() {
     return 0;
 }
 
+// Whole contexts of 64 sequences with a ledger: a grid that the runtime would refuse is refused before anything is launched
+static int grids_of_weights() {
+    st_kv4 *h = cache({1, 64, 40, 8, 64, 1 << 21, 1 << 20, 64, 1e-6f});
+    CHECK(h);
+    st_kv4_span s[64];
+    for (int rows : {1, 2, 6, 10, 13, 100, 1000})
+        for (int n : {64, 63, 1})
+            for (int short_by : {0, 63, 64, 65}) {  // the last sequence ends in a block of slots less, or not
+                for (int j = 0; j < n; ++j) s[j] = {j, (1 << 21) - rows - (j == 63 ? short_by : 0), 0, rows};
+                launches.clear();
+                const int rc = st_kv4_attend(h, 0, s, n, p, 1 << 20, (char *)p + (1ll << 45), 1 << 20, &led);
+                CHECK(!refused && (rc == ST_OK ? !launches.empty() : rc == ST_ERANGE && launches.empty()));
+                CHECK((rc == ST_ERANGE) == (n == 64 && short_by < 64 && rows * 5 > 32));
+                launches.clear();
+                CHECK(st_kv4_attend(h, 0, s, n, p, 1 << 20, (char *)p + (1ll << 45), 1 << 20, nullptr) == ST_OK && !refused);
+            }
+    st_kv4_destroy(h);
+    return 0;
+}
+
 int main(int argc, char **argv) {
     const struct {
         const char *name;
         int (*f)();
-    } tests[] = {{"lds_on_every_gpu", lds_on_every_gpu}, {"lds_refused", lds_refused}};
+    } tests[] = {{"lds_on_every_gpu", lds_on_every_gpu}, {"lds_refused", lds_refused}, {"grids_of_weights", grids_of_weights}};
     for (const auto &t : tests)
         if (argc == 2 && !std::strcmp(argv[1], t.name)) {
             if (t.f()) return 1;

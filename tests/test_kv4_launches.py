@@ -42,3 +42,7 @@ def run(exe, name):
 @pytest.mark.parametrize("name", ["lds_on_every_gpu", "lds_refused"])
 def test_lds_of_long_evictions(driver, name):
     run(driver, name)
+
+
+def test_grids_of_weights(driver):
+    run(driver, "grids_of_weights")
