@@ -374,8 +374,8 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
     }
 }
 
-// Ledger entries of a part of the slots that stay, and moves part * kMovesPer .. + kMovesPer - 1, and every parts * kMovesPer
-// further, of a head.  Bound by latency: listing, then loads and stores.  16 heads with 2000 moves each 10.9 us; with the
+// Ledger entries of a part of the slots that stay, and moves part * kMovesPer .. + kMovesPer - 1 of a head, which has blocks for all the
+// moves that it can have.  Bound by latency: listing, then loads and stores.  16 heads with 2000 moves each 10.9 us; with the
 // selection, measured at the time, 28.0 us at 256 moves a block, 29.5 at 512, 31.2 at 128.
 constexpr int kMoveThreads = 1024, kMovesPer = 256;
 template <int D, int CAP>
@@ -390,12 +390,8 @@ __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t
         const int share = (keep + a.parts - 1) / a.parts;
         copy_kept<kMoveThreads>(pl, bits, part * share, min(keep, (part + 1) * share));
     }
-    for (int r0 = part * kMovesPer;; r0 += a.parts * kMovesPer) {
-        const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, r0, freed, late);
-        move_slots<D, kMoveThreads>(pl, late, freed, min(total - r0, kMovesPer));
-        if (r0 + a.parts * kMovesPer >= total) return;
-        __syncthreads();
-    }
+    const int total = list_moves<kMoveThreads, kMovesPer>(bits, n, keep, part * kMovesPer, freed, late);
+    move_slots<D, kMoveThreads>(pl, late, freed, min(total - part * kMovesPer, kMovesPer));
 }
 
 // Moves by blocks of their own from so many moves of one head, and below so many heads (128 heads of up to 1024 moves: 27.9 us

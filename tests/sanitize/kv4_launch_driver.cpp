@@ -143,11 +143,35 @@ static int grids_of_weights() {
     return 0;
 }
 
+// Where moves are a launch of their own, a block does 256 of them once: the grid has to have room for the most that a head can have
+static int blocks_of_moves() {
+    st_kv4 *h = cache({1, 4, 4, 2, 64, 1 << 20, 8, 64, 1e-6f});
+    CHECK(h);
+    int two = 0;
+    for (int len : {2049, 2050, 2304, 2305, 5000, 24576, 24577, 40000, 131072, 131073, 1 << 20})
+        for (int keep : {1, 1023, 1024, 1025, 1279, 1280, 1281, 2048, len / 2 - 1, len / 2, len / 2 + 1, len - 1281, len - 1280, len - 1025, len - 1}) {
+            if (keep <= 0) continue;
+            const st_kv4_span s[] = {{2, keep / 2, len, 0}, {0, len, len, 0}, {1, len / 2, len, 0}};
+            launches.clear();
+            CHECK(st_kv4_evict(h, 0, 1, s, 3, keep, 0, &led, nullptr) == ST_OK && !refused);
+            const int moves = len - keep < keep ? len - keep : keep;
+            CHECK(launches.size() == (moves > 1024 ? 2u : 1u));
+            if (launches.size() == 2) {
+                const dim3 g = launches[1].grid;
+                CHECK(g.x % 2 == 0 && (int)(g.x / 2) * 256 >= moves && g.y == 3 && g.z == 1);
+                ++two;
+            }
+        }
+    CHECK(two > 20);
+    st_kv4_destroy(h);
+    return 0;
+}
+
 int main(int argc, char **argv) {
     const struct {
         const char *name;
         int (*f)();
-    } tests[] = {{"lds_on_every_gpu", lds_on_every_gpu}, {"lds_refused", lds_refused}, {"grids_of_weights", grids_of_weights}};
+    } tests[] = {{"lds_on_every_gpu", lds_on_every_gpu}, {"lds_refused", lds_refused}, {"grids_of_weights", grids_of_weights}, {"blocks_of_moves", blocks_of_moves}};
     for (const auto &t : tests)
         if (argc == 2 && !std::strcmp(argv[1], t.name)) {
             if (t.f()) return 1;

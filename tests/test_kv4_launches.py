@@ -46,3 +46,7 @@ def test_lds_of_long_evictions(driver, name):
 
 def test_grids_of_weights(driver):
     run(driver, "grids_of_weights")
+
+
+def test_blocks_of_moves(driver):
+    run(driver, "blocks_of_moves")
