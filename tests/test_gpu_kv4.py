@@ -531,6 +531,31 @@ def test_evict_with_positions_that_repeat():
         check_evict(kv, (0, 1), [(0, 2999, 100, 0)], 1500, 200, w, p, into=False)
 
 
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "odd"])
+@pytest.mark.parametrize("n,other,keep,recent", [(131900, 131050, 131000, 999), (131073, 131072, 130500, 0), (140003, 90000, 70001, 5000), (262145, 70, 1, 1)])
+def test_evict_past_the_slots_whose_bits_fit_a_block(n, other, keep, recent, kind):
+    """More than 131072 slots, whose bits are in the workspace, moved by the block that selects and by blocks of their own, beside a sequence with fewer."""
+    print("evict:", n, "and", other, "slots,", kind, flush=True)
+    rng = np.random.default_rng(n + keep)
+    kv = make(2, 1, 64, n_seq=3, max_seq=n)
+    kv.cache.copy_(torch.from_numpy(rng.integers(0, 256, kv.cache.numel()).astype(np.uint8)))
+    spans = [(2, n, n + 100, 0), (0, other, other, 0)]
+    w, p = random_ledger(kv, spans, rng, kind)
+    check_evict(kv, (0, 1), spans, keep, recent, w, p, into=kind == "spread")
+
+
+@pytest.mark.parametrize("n,keep", [(30001, 12000), (30001, 29500), (24577, 64), (140003, 139700)])
+def test_evict_long_with_positions_that_repeat(n, keep):
+    """Slots alike in weight and position where the weights are read again for every digit: the first of them stay."""
+    print("evict: repeated positions", n, keep, flush=True)
+    rng = np.random.default_rng(n + keep)
+    kv = make(2, 1, 64, n_seq=1, max_seq=n)
+    kv.cache.copy_(torch.from_numpy(rng.integers(0, 256, kv.cache.numel()).astype(np.uint8)))
+    w = rng.integers(0, 2, (1, 1, 1, n)).astype(np.float32)
+    for p in (np.zeros_like(w, dtype=np.int32), rng.integers(-5, 5, w.shape).astype(np.int32), np.full(w.shape, 2 ** 31 - 1, dtype=np.int32)):
+        check_evict(kv, (0, 1), [(0, n, 100, 0)], keep, min(keep, 200), w, p, into=False)
+
+
 # ---- together ----
 
 def test_a_context_is_thinned_and_goes_on():
