@@ -59,12 +59,12 @@ class Context:
         self.evictions += 1
 
     def prefill(self, x, rows):
-        """forward() in passes of at most max_rows rows of each sequence."""
-        parts, last = x.split(rows), None
+        """forward() in passes of at most max_rows rows of each sequence.  Returns the outputs of all rows, in the order of x."""
+        parts, passes = x.split(rows), []
         for at in range(0, max(rows), self.max_rows):
             now = [p[at:at + self.max_rows] for p in parts]
-            last = self.forward(torch.cat(now), [len(p) for p in now])
-        return last
+            passes.append(self.forward(torch.cat(now), [len(p) for p in now]).split([len(p) for p in now]))
+        return torch.cat([p[s] for s in range(len(rows)) for p in passes]) if passes else x
 
 
 def trace(small, large, n_seq, prompt, tokens, seed=0, segment=N2, takeover=N1):
