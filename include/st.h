@@ -447,6 +447,7 @@ int st_kv4_append(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n,
 /* Causal attention over the cache: row i of a span attends to slots [0, len + i] of its sequence, those of the span's own rows, appended before,
  * among them; scores are scaled by head_dim^-1/2.  q, out: bf16, n_q_heads * head_dim a row; they share no memory.  With a ledger the weight of every slot
  * grows by the attention it received, summed over the rows and over the query heads of its kv head, in an order that does not change from run to run.
+ * Values are summed by weights of up to 1 each and divided by the weights' sum afterwards, so values above 2^127 / slots can overflow.
  * ST_ERANGE: a span outside the cache, too many rows, or a ledger with 2^30 slots over all spans and kv heads and more than 32 columns (rows x query heads
  * of a kv head) in a span. */
 int st_kv4_attend(st_kv4 *c, int32_t layer, const st_kv4_span *spans, int32_t n, const void *q, int64_t q_stride, void *out,

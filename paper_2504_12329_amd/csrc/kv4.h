@@ -15,8 +15,8 @@ struct Kv4Span {
     int32_t per;                  // tiles of slots in a range
     int32_t part0;                // its first row of partial results (rows x query heads of range 0, of range 1, ...)
 };
-// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Three sizes, as a
-// launch with the largest costs the host 3.4 us and one with the smallest 2.4.
+// Passed to the kernels by value: no copy to the device precedes them, and a captured launch keeps it.  Three sizes: an append of
+// 64 spans costs the host 4.3 us, one of up to four 3.5 (the C call through ctypes).
 template <int CAP>
 struct Kv4Spans {
     int32_t n;

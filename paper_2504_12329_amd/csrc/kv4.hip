@@ -21,8 +21,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // ---------------------------------------------------------------------------------------
 // Append.  D/8 threads per head; a thread owns four neighbouring channels of each half of the head, i.e. four rotation pairs,
 // so that norm, rotation and quantisation need no exchange but the group's maximum (8 lanes) and the norm's sum.  Bound by
-// memory: 2 bytes per channel in, 2 out for the queries, 4.25 bits for keys and values.  4096 rows of 40 / 8 heads 20.6 us, 5.3
-// TB/s (a large copy: 5.1); 16 rows 3.5 us.
+// memory: 2 bytes per channel in, 2 out for the queries, 4.25 bits for keys and values.  4096 rows of 40 / 8 heads, 105 MB and 2
+// of the rotation table, 20.9 us, 5.1 TB/s (a large copy: 5.1); 16 rows 3.5 us.  64 channels, 4096 rows of 4 / 2 heads: 4.4 us.
 //
 // Every product and sum is rounded to fp32 by itself (no contraction) and the sum of squares adds neighbours first, so the
 // codes are a function of the inputs alone: no choice of the kernel's shape shows in them.

@@ -112,9 +112,10 @@ __device__ __forceinline__ Column column_of(int col, int G, int kvh) { return Co
 
 // ---------------------------------------------------------------------------------------
 // Few columns: single tokens and short runs.  With one group of columns bound by memory (the cache is read once): 16 tokens of
-// 40 / 8 heads on 500 to 6000 slots 15.8 us, 3.6 TB/s, one of 12 / 2 heads on 4608 slots 4.4 us, all latency.  With more by the
-// vector pipe: 310 vector and 32 matrix instructions a tile of 32 columns, 86 rows of 40 / 8 heads on 4096 slots 23 us (half of
-// the cycles issue, a quarter wait for loads; twice the blocks on half the slots each take as long).
+// 40 / 8 heads on 500 to 6000 slots 17.0 us, 3.4 TB/s, one of 12 / 2 heads on 4608 slots 4.6 us, all latency.  With more by the
+// vector pipe and latency: 350 vector and 32 matrix instructions a tile of 32 columns, 86 rows of 40 / 8 heads on 4096 slots 24 us.
+// With one wave a SIMD a tile takes 2900 cycles; of the waves' cycles 60 % issue (52 % vector instructions), 29 % wait for loads
+// and results, 11 % for their turn.  (Twice the blocks on half the slots each take as long.)
 //
 // A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end (four tiles no longer fit
 // the registers without moves: 36 us for 86 rows of 40 / 8 heads on 4096 slots, against 28 with two): S^T by 16x16x32 MFMAs
@@ -346,11 +347,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_kv4_few(const Kv4Spans
 }
 
 // ---------------------------------------------------------------------------------------
-// Chunks, bound by the matrix pipe and, in turn with it, the vector pipe: 4096 rows of 40 / 8 heads on 4096 slots 515 us, 1.0
-// PFLOP/s (staging left out 448 us, exponentials left out 497).  A block is 128 columns of one kv head (four waves of 32) on a
-// range of tiles of 128 slots.  The tile's codes are loaded one tile ahead into registers, turned into bf16 once for all four
-// waves and put into LDS as the MFMA operands that the waves read: 1 KB fragments, 16 bytes a lane, no bank conflicts in
-// writing or reading.  Two blocks share a compute unit, so that one's products run beside the other's softmax.
+// Chunks, bound by the matrix pipe and, in turn with it, the vector pipe: 4096 rows of 40 / 8 heads on 4096 slots 520 us, 1.0
+// PFLOP/s (measured at 515: staging left out 448 us, exponentials left out 497).  A block is 128 columns of one kv head (four waves
+// of 32) on a range of tiles of 128 slots.  The tile's codes are loaded one tile ahead into registers, turned into bf16 once for
+// all four waves and put into LDS as the MFMA operands that the waves read: 1 KB fragments, 16 bytes a lane (bank conflicts take
+// 14 % of the LDS cycles).  Two blocks share a compute unit, so that one has work for either pipe while the other waits: the
+// matrix pipe is busy for 42 % of the cycles and the vector pipe for 53 %, so little of them overlaps.
 //   K: a thread has one scale group (32 channels) of one or two slots;  V: eight slots x eight channels.
 //   S^T rows: fragment row m of 32 slots is slot swap(m) (bits 2 and 3 exchanged): registers 0-7 and 8-15 of a lane are then eight
 //   consecutive slots each, as the second product wants them.
@@ -565,7 +567,7 @@ __global__ __launch_bounds__(256, 2) void k_kv4_chunk(const Kv4Spans<CAP> t, con
 // ---------------------------------------------------------------------------------------
 // Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them
 // are fetched at once; then D / 4 lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range
-// whose slots the row does not see has sum 0 and an unused output.  Latency: 3 to 4.6 us.
+// whose slots the row does not see has sum 0 and an unused output.  Latency: 3 to 4.7 us; 4096 rows of 4 heads 9.2 us.
 // ---------------------------------------------------------------------------------------
 template <int D, int WPU>
 __device__ __forceinline__ void join_unit(const Kv4Span &sp, int unit, bool live, int nq, const float *__restrict__ part_o,
@@ -780,8 +782,9 @@ __global__ __launch_bounds__(256) void k_kv4_few_weights(const Kv4Spans<CAP> t, 
 // Chunks: the weight each slot received, sum over the columns that see it of exp2(score - lse), the scores formed once more (K
 // only).  A block is 64 slots, its keys in registers as bf16; its W waves take every W-th tile of 32 columns, S = Q K^T, so
 // that a lane has one slot and the sum over the columns stays in the lane.  One block owns a slot's sum: no atomics, the same
-// order in every run.  Bound by the matrix and the vector pipe in turn (an exponential and two more operations a score): 2048
-// rows of 40 / 8 heads on 4096 slots 212 us, 0.51 PFLOP/s; 86 rows 13.5 us.
+// order in every run.  2048 rows of 40 / 8 heads on 4096 slots 202 us, 0.53 PFLOP/s (the products alone at a large product's rate:
+// 78); 86 rows 13.2 us.  The vector pipe is busy for 54 % of the cycles (an exponential and two more operations a score), the matrix
+// pipe for 23 %; a wave waits 41 % of its own for its turn and 18 % for loads and LDS, as each stages its columns by itself.
 // ---------------------------------------------------------------------------------------
 constexpr int kWeightKeys = 64;
 
@@ -955,6 +958,9 @@ Kv4AttendPlan plan_kv4_attend(const Kv4 &k, Kv4Table &t, bool weights) {
     const bool fused = weights && few && (most <= 32 || (most <= 64 && few_tiles <= 6000));
     Kv4AttendPlan p{most <= 16 ? 16 : few ? 32 : kTileCols, 0, 0, most, fused, 0, 0};
     auto groups = [&](const Kv4Span &s) { return nkv * ((s.rows * G + p.cols - 1) / p.cols); };
+    // A call that fills `want` blocks as it is stays uncut, so it lasts as long as its longest span: 40 / 8 heads, a single token on
+    // 16001 slots beside 32 on 201 slots 13.5 us (32 ranges), beside 63 of them, which are 512 blocks, 93 (one range).  256 blocks
+    // of 32 columns were measured on single spans.
     // Up to 512 slots stay in one range where a join would be a launch of its own: one row of 12 / 2 heads on 128 slots 4.1 us
     // against 6.5, on 512 6.2 against 6.7; 16 rows of 40 / 8 heads on 512 slots each 6.7 against 9.6.  (On 1024 slots 8.7
     // against 6.7.)

@@ -9,10 +9,10 @@
 // k_kv4_evict, one block per head, finds the keep-th by histograms of 11-bit digits in LDS until at most 128 slots share the
 // digits so far, and ranks those against each other; it writes a bit per slot and moves.  Weights and positions are read once,
 // the 32 bits kept in LDS (up to 24576 slots; beyond, they are read again for every digit).  Bound by latency, also of
-// instructions, as every line runs but a few times: 128 heads of 500 to 6000 slots to 1024 18 us, 21 with loops unrolled 8 and
-// 16 times; 56 heads of 577 slots to 512 8.0 us, 16 heads of 16385 slots 15.4 us.  (Histograms over the range that the weights
-// span, which need no second digit, cost a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the
-// moves by several blocks per head.
+// instructions, as every line runs but a few times: 128 heads of 500 to 6000 slots to 1024 19 us (measured at 18: 21 with loops
+// unrolled 8 and 16 times); 56 heads of 577 slots to 512 8.2 us, 16 heads of 16385 slots 15.8 us.  Read again for every digit: 8
+// heads of 32768 slots 46 us, two of 200000 260.  (Histograms over the range that the weights span, which need no second digit, cost
+// a reduction first: 0.4 to 3 us more.)  k_kv4_move: where few heads move many slots, the moves by several blocks per head.
 #include <atomic>
 
 #include "kv4.h"
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(THREADS) void k_kv4_evict(const Kv4Spans<CAP> t, co
 }
 
 // Ledger entries of a part of the slots that stay, and moves part * kMovesPer .. + kMovesPer - 1 of a head, which has blocks for all the
-// moves that it can have.  Bound by latency: listing, then loads and stores.  16 heads with 2000 moves each 10.9 us; with the
+// moves that it can have.  Bound by latency: listing, then loads and stores.  16 heads with 2000 moves each 10.6 us; with the
 // selection, measured at the time, 28.0 us at 256 moves a block, 29.5 at 512, 31.2 at 128.
 constexpr int kMoveThreads = 1024, kMovesPer = 256;
 template <int D, int CAP>
@@ -394,8 +394,13 @@ __global__ __launch_bounds__(kMoveThreads) void k_kv4_move(const Kv4Spans<CAP> t
     move_slots<D, kMoveThreads>(pl, late, freed, min(total - part * kMovesPer, kMovesPer));
 }
 
-// Moves by blocks of their own from so many moves of one head, and below so many heads (128 heads of up to 1024 moves: 27.9 us
-// in two launches, 20.9 in one)
+// Moves by blocks of their own from so many moves of one head, and below so many heads.  One launch : two, both of these kernels, us:
+//   slots, kept      2048, 1024   2500, 1250   3000, 1500   4096, 2048   8192, 4096   16385, 4096
+//     8 heads       10.8 : 12.1  11.9 : 12.5  12.9 : 13.0  15.8 : 13.4  26.3 : 15.6   44.1 : 20.6
+//    32 heads       11.0 : 12.5  12.2 : 12.9  13.2 : 13.6  17.1 : 15.0  28.3 : 19.6   48.5 : 29.2
+//    96 heads       11.8 : 16.5  13.3 : 16.2  14.6 : 17.9  19.0 : 23.5  31.3 : 33.1   52.0 : 47.5
+//   128 heads       12.3 : 18.6  13.6 : 18.6  15.1 : 20.9  19.9 : 26.2  33.3 : 38.9   56.9 : 58.2
+// (one is the better for 64 heads and more below some 3000 moves, and up to 1500 moves: the rule loses up to 4.5 us there)
 constexpr int kMoveMany = 1024, kMoveHeads = 128;
 
 // Up to 99 KB of LDS are asked for at the launch of a block of 1024 threads: allowed once per kernel and GPU
