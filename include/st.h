@@ -471,6 +471,109 @@ int st_kv4_evict(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_spa
  * [layer_hi - layer_lo][rows of all spans][n_kv_heads][head_dim], 16-byte aligned.  Fewer than 2^24 rows. */
 int st_kv4_read(st_kv4 *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, void *k_out, void *v_out);
 
+/* ---- A key/value cache in pages, and drafted tokens ----
+ *
+ * Speculative decoding beside the hand-over loop: a draft model writes some tokens ahead, the target reads them all in one pass and the
+ * drafts that it would have written itself stay (the comparison system of the paper's Section 4).  These are the operators around that pass, as
+ * calls of one layer or several for callers that run the rest of a decoder themselves: norms and rotation with the write (append), attention with
+ * each draft seeing its own branch (attend), the verdict (st_verify_drafts), and the rows that stay brought together (keep).  The same cache
+ * serves single tokens and chunks without drafts.
+ *
+ * The cache holds 16-bit numbers, in pages of page_size slots that any sequence may own:
+ *     [K | V][layer][page][kv head][slot of the page][head_dim].
+ * Slot i of sequence s is slot i % page_size of page table[s * max_pages + i / page_size]; the table (device int32, borrowed) is read by every call when
+ * it runs, so it may change between calls.  An entry outside [0, n_pages) is a hole: what is written there is dropped, and no row sees its slots.
+ * Pages may be shared by sequences that only read them.
+ *
+ * Spans are those of the 4-bit cache (st_kv4_span): `len` slots are held, `rows` new rows are in slots len, len + 1, ....  With drafts a
+ * span's row 0 is the last decided token and the others are drafts, each after the row it follows (its parent). */
+enum { ST_BF16 = 0, ST_F16 = 1, ST_F32 = 2 };                /* types */
+enum { ST_PAIRS_HALVES = 0, ST_PAIRS_NEIGHBOURS = 1 };       /* rotation pairs (i, i + rot_dim / 2) or (2 i, 2 i + 1) */
+typedef struct st_paged st_paged;
+typedef struct {
+    int32_t n_layers, n_seq, n_q_heads, n_kv_heads, head_dim;
+    int32_t n_pages;   /* pages of a layer; the same number means the same page in every layer */
+    int32_t page_size; /* slots of a page: a power of two from 16 to 1024 */
+    int32_t max_pages; /* table entries of a sequence */
+    int32_t max_rows;  /* most new rows of one call */
+    int32_t max_pos;   /* positions the rotation table has */
+    int32_t dtype;     /* ST_BF16 or ST_F16: cache, queries, keys, values, outputs and norms */
+    int32_t rot_dim;   /* channels of a head that rotate, from its first on: a multiple of 16, 0 for none */
+    int32_t rot_pairs; /* ST_PAIRS_* */
+    float rms_eps;     /* of the norms of queries and keys */
+} st_paged_config;
+/* Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, at most 16 times as many; page_size * max_pages <= 2^24, max_rows <= 2^20. */
+
+/* The branches of a call's rows, in device memory of the caller's, rows of all spans one after the other; rows of a span are counted from 0. */
+typedef struct {
+    const int32_t *parent; /* [rows]: the row that a row follows, before it; a span's row 0 follows none (its entry is not read) */
+    const int32_t *depth;  /* [rows]: a row's position is the span's pos + depth */
+    const uint64_t *sees;  /* [rows][words], 8-byte aligned: bit j % 64 of word j / 64: the row attends to row j of its span */
+    int32_t words;         /* 1 to 16; spans have at most 64 * words rows */
+    int32_t width;         /* most rows that follow one row, 1 to 64; st_verify_drafts does not try more */
+} st_draft_tree;
+
+/* As st_query_sizes. */
+int st_paged_query_sizes(const st_paged_config *cfg, size_t *cache_bytes, size_t *workspace_bytes);
+/* rope: device fp32 [max_pos][rot_dim / 2][2], (cos, sin) of every position and pair, 16-byte aligned (not read if rot_dim is 0; positions scaled for long
+ * contexts are a matter of its numbers).  table: device int32 [n_seq][max_pages].  cache and workspace: device memory, 256-byte aligned; neither needs clearing.
+ * All are borrowed until st_paged_destroy.  Every call enqueues on `stream` and returns without waiting; calls of one handle, and graphs captured
+ * from them, share its workspace and must not run at the same time. */
+int st_paged_create(const st_paged_config *cfg, const float *rope, const int32_t *table, void *cache, size_t cache_bytes, void *workspace,
+                    size_t workspace_bytes, void *stream, st_paged **out);
+void st_paged_destroy(st_paged *c);
+
+/* Norms, rotation and the write of new rows, as st_kv4_append: qkv holds all query heads, then the key heads, then the value heads of a row; q_norm and
+ * k_norm ([head_dim], both or neither).  Row i is at position pos + i, with `tree` at pos + tree->depth[i] (cut to the rotation table; its other members are not
+ * read).  Rotated queries go to q_out.  ST_ERANGE: a span outside the table or the rotation table, too many rows. */
+int st_paged_append(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_t n, const st_draft_tree *tree, const void *qkv, int64_t qkv_stride,
+                    const void *q_norm, const void *k_norm, void *q_out, int64_t q_stride);
+
+/* Attention over the cache, scores scaled by head_dim^-1/2.  Without `tree` row i of a span attends to slots [0, len + i]; with it to slots [0, len) and
+ * to those of the span's rows that tree->sees names (only sees and words are read), itself only if it is named.  A row that sees nothing gets zeros.  What is in
+ * slots that a row does not see, infinities and NaN too, does not reach it.  q, out: n_q_heads * head_dim a row; they share no memory.
+ * ST_ERANGE: a span outside the table, too many rows, more rows of a span than `sees` has bits, more than 2^24 blocks of work. */
+int st_paged_attend(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_t n, const st_draft_tree *tree, const void *q, int64_t q_stride,
+                    void *out, int64_t out_stride);
+
+/* Host only: how such a call of st_paged_attend is dealt out; see st_kv4_attend_plan. */
+int st_paged_attend_plan(const st_paged_config *cfg, const st_kv4_span *spans, int32_t n, int32_t with_tree, int32_t *columns, int32_t *blocks,
+                         int32_t *ranges);
+
+/* In layers [layer_lo, layer_hi) the keys and values of rows path[j * path_stride + i], i < accepted[j], of span j move to slots len + 1 + i: after it the
+ * sequence has len + 1 + accepted[j] slots.  path and accepted are device int32, as st_verify_drafts writes them; rows are taken while they ascend
+ * within (0, rows), and what follows one that does not stays where it is.  Slots of holes are neither read nor written. */
+int st_paged_keep(st_paged *c, int32_t layer_lo, int32_t layer_hi, const st_kv4_span *spans, int32_t n, const int32_t *path, int32_t path_stride,
+                  const int32_t *accepted);
+
+/* The verdict over drafts from given random numbers: tokens that stay are distributed as the target's own. */
+typedef struct st_verify st_verify;
+typedef struct {
+    int32_t vocab;     /* up to 2^24 */
+    int32_t dtype;     /* of the logits: ST_BF16, ST_F16 or ST_F32 */
+    int32_t max_rows;  /* most rows of a call, up to 32767 */
+    int32_t max_width; /* most width of a tree, 1 to 64 */
+} st_verify_config;
+int st_verify_query_sizes(const st_verify_config *cfg, size_t *workspace_bytes);
+int st_verify_create(const st_verify_config *cfg, void *workspace, size_t workspace_bytes, void *stream, st_verify **out);
+void st_verify_destroy(st_verify *v);
+/* n sequences (at most ST_KV4_MAX_SPANS) with rows[j] rows each (host array; 1 to 1024, row 0 the last decided token), the rows of a call one after the other.
+ * tree: parent and width are read; NULL: every row follows the one before.  tokens: device int32 [all rows].  target, draft: device, row i the
+ * logits of what follows row i, rows strides elements apart; draft is what the drafts were drawn from, or NULL where they are certain (a model's
+ * best tokens).  temperature: host [n].  accept (device, [all rows]) and sample (device, [n]): uniform random numbers in [0, 1), independent of the drafts.
+ *
+ * From row 0 on, in 64 bits: p = softmax(target / T), q = softmax(draft / T) of the row; the rows that follow it are tried in ascending order.  Row c with token t
+ * stays if accept[c] < p(t) / q(t) (accept[c] < p(t) without draft logits); if not, p becomes max(p - q, 0) (p without t), scaled to the sum 1, for the next.  From the
+ * row that stays it goes on; where none does, the next token is the least x with p(0) + ... + p(x) > sample[j] (p's own sum in the place of 1).
+ * A temperature of 0: the row that has the largest target logit's token (the lowest token among equals) stays, and the next token is that token.
+ * A p that rounding leaves empty is taken as it was before the first draft failed.  A row of logits with a NaN, with none above -infinity, or (T > 0) with +infinity has no
+ * distribution: no row after it stays, and the next token is -1.  Tokens outside the vocabulary do not stay.
+ *
+ * path (device int32 [n][path_stride], path_stride >= rows[j]): the rows that stay, -1 behind them up to path_stride; accepted: their number; next: the token. */
+int st_verify_drafts(st_verify *v, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
+                     int64_t target_stride, const void *draft, int64_t draft_stride, const float *temperature, const double *accept,
+                     const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next);
+
 const char *st_last_error(void);
 
 #ifdef __cplusplus

@@ -14,6 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libst.so")
 
 ST_OK, ST_EINVAL, ST_ENOMEM, ST_ERANGE, ST_EHIP = 0, -1, -2, -3, -4
+ST_BF16, ST_F16, ST_F32 = 0, 1, 2
+ST_PAIRS_HALVES, ST_PAIRS_NEIGHBOURS = 0, 1
 ST_TOKENS_DEVICE, ST_OUT_DEVICE, ST_TOKEN_CHAINED, ST_PREFILL_TWO_TERM, ST_PREFILL_FAST = 1, 2, 4, 8, 16
 
 EXPORTS = ("st_query_sizes", "st_prefill_plan_check", "st_prefill_plan_forms", "st_model_create", "st_model_destroy", "st_kv_len",
@@ -23,7 +25,9 @@ EXPORTS = ("st_query_sizes", "st_prefill_plan_check", "st_prefill_plan_forms", "
            "st_generate", "st_generate_policy", "st_batch_query_sizes", "st_batch_create", "st_batch_destroy",
            "st_batch_kv_len", "st_batch_truncate", "st_batch_prefill", "st_batch_prefill_many", "st_batch_decode_step",
            "st_generate_batch", "st_kv4_query_sizes", "st_kv4_create", "st_kv4_destroy", "st_kv4_append", "st_kv4_attend",
-           "st_kv4_attend_plan", "st_kv4_evict", "st_kv4_read", "st_last_error")
+           "st_kv4_attend_plan", "st_kv4_evict", "st_kv4_read", "st_paged_query_sizes", "st_paged_create", "st_paged_destroy",
+           "st_paged_append", "st_paged_attend", "st_paged_attend_plan", "st_paged_keep", "st_verify_query_sizes", "st_verify_create",
+           "st_verify_destroy", "st_verify_drafts", "st_last_error")
 
 
 class StError(RuntimeError):
@@ -75,6 +79,19 @@ class st_kv4_span(C.Structure):
 
 class st_kv4_ledger(C.Structure):
     _fields_ = [("weights", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class st_paged_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seq", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_size", "max_pages",
+                                         "max_rows", "max_pos", "dtype", "rot_dim", "rot_pairs")] + [("rms_eps", C.c_float)]
+
+
+class st_draft_tree(C.Structure):
+    _fields_ = [("parent", C.c_void_p), ("depth", C.c_void_p), ("sees", C.c_void_p), ("words", C.c_int32), ("width", C.c_int32)]
+
+
+class st_verify_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("vocab", "dtype", "max_rows", "max_width")]
 
 
 _lib = None
@@ -148,6 +165,22 @@ def lib():
         L.st_kv4_attend_plan.argtypes = [C.POINTER(st_kv4_config), spans, C.c_int32, C.c_int32] + [C.POINTER(C.c_int32)] * 3
         L.st_kv4_evict.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_int32, C.c_int32, ledger, ledger]
         L.st_kv4_read.argtypes = [C.c_void_p, C.c_int32, C.c_int32, spans, C.c_int32, C.c_void_p, C.c_void_p]
+        L.st_paged_query_sizes.argtypes = [C.POINTER(st_paged_config), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        L.st_paged_create.argtypes = [C.POINTER(st_paged_config), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
+                                      C.c_void_p, C.POINTER(C.c_void_p)]
+        L.st_paged_destroy.argtypes = [C.c_void_p]
+        L.st_paged_destroy.restype = None
+        L.st_paged_append.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_int64]
+        L.st_paged_attend.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
+        L.st_paged_attend_plan.argtypes = [C.POINTER(st_paged_config), C.c_void_p, C.c_int32, C.c_int32, i32p, i32p, i32p]
+        L.st_paged_keep.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
+        L.st_verify_query_sizes.argtypes = [C.POINTER(st_verify_config), C.POINTER(C.c_size_t)]
+        L.st_verify_create.argtypes = [C.POINTER(st_verify_config), C.c_void_p, C.c_size_t, C.c_void_p, C.POINTER(C.c_void_p)]
+        L.st_verify_destroy.argtypes = [C.c_void_p]
+        L.st_verify_destroy.restype = None
+        L.st_verify_drafts.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -728,3 +761,285 @@ class Kv4Cache:
         if layers and spans.rows:
             _check(self._read(self._h, layer_lo, layer_hi, spans.c, spans.n, k.data_ptr(), v.data_ptr()))
         return k, v
+
+
+class DraftSpans(Kv4Spans):
+    """Spans whose rows are the last decided token and drafts after it: parents[j][i] is the row of span j that its row i follows, before it
+    (parents[j][0] is not read).  Made once for all layers of a step; a branch's rows see each other and the context, and a row's position is
+    the span's pos and the number of rows before it in its branch."""
+
+    def __init__(self, spans, parents, device="cuda"):
+        super().__init__(spans)
+        if len(parents) != self.n or any(len(p) != s[3] for p, s in zip(parents, self.spans)):
+            raise StError(ST_EINVAL, "parents holds a list for every span, with an entry for every row")
+        most = max([s[3] for s in self.spans], default=0)
+        if most > 1024:
+            raise StError(ST_ERANGE, f"{most} rows of a span, trees have at most 1024")
+        words = max(1, -(-most // 64))
+        parent, depth = np.full(self.rows, -1, dtype=np.int32), np.zeros(self.rows, dtype=np.int32)
+        sees, at, width = np.zeros((self.rows, words), dtype=np.uint64), 0, 1
+        for ps in parents:
+            after = [0] * len(ps)
+            for i, p in enumerate(ps):
+                if i:
+                    p = int(p)
+                    if not 0 <= p < i:
+                        raise StError(ST_EINVAL, f"row {i} follows row {p}: not a row before it")
+                    parent[at + i], depth[at + i], sees[at + i] = p, depth[at + p] + 1, sees[at + p]
+                    after[p] += 1
+                sees[at + i, i // 64] |= np.uint64(1 << (i % 64))
+            width = max(width, *after, 1)
+            at += len(ps)
+        if width > 64:
+            raise StError(ST_ERANGE, f"{width} rows follow one row, at most 64 are supported")
+        bits = torch.from_numpy(np.concatenate([sees.reshape(-1).view(np.int64), np.concatenate([parent, depth]).view(np.int64)])).to(device)
+        cut = self.rows * words
+        self._take(bits[cut:].view(torch.int32)[:self.rows], bits[cut:].view(torch.int32)[self.rows:], bits[:cut].view(self.rows, words), width)
+
+    @classmethod
+    def of_tensors(cls, spans, parent=None, depth=None, sees=None, width=1):
+        """From tensors on the GPU, for trees that are made there: parent and depth int32 [rows], sees int64 [rows][words] (see st_draft_tree); a call that
+        reads one that is None is refused."""
+        self = cls.__new__(cls)
+        Kv4Spans.__init__(self, spans)
+        for name, x, t, dims in (("parent", parent, torch.int32, 1), ("depth", depth, torch.int32, 1), ("sees", sees, torch.int64, 2)):
+            if x is not None and (x.dtype != t or x.dim() != dims or x.shape[0] != self.rows or not x.is_contiguous() or not x.is_cuda):
+                raise StError(ST_EINVAL, f"{name} is a contiguous {t} CUDA tensor of {self.rows} rows, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        self._take(parent, depth, sees, int(width))
+        return self
+
+    def _take(self, parent, depth, sees, width):
+        self.parent, self.depth, self.sees, self.width = parent, depth, sees, width
+        ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        self._tree = st_draft_tree(ptr(parent), ptr(depth), ptr(sees), 1 if sees is None else sees.shape[1], width)
+        self.tree = C.byref(self._tree)
+        self.devices = {x.device for x in (parent, depth, sees) if x is not None}
+
+
+class _OnStream:
+    """Calls that enqueue on one stream of one GPU: the stream that was current when the object was made (they are refused under another one), or a
+    raw handle, where ordering other streams' work against them is the caller's part."""
+
+    def _bind(self, dev, stream):
+        self._own_stream = stream is not None
+        self.stream = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
+        self._dev, self._index = dev, dev.index
+        with self._on():
+            self._new = torch.empty(0, dtype=torch.uint8, device=dev).new_empty
+
+    def _on(self):
+        # what is allocated belongs to the stream that uses it: freed, it does not go to another one while calls are still running
+        return torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self._dev) if self._own_stream else torch.cuda.current_stream(self._dev))
+
+    def _empty(self, shape, dtype):
+        if not self._own_stream:
+            return self._new(shape, dtype=dtype)
+        with self._on():
+            return self._new(shape, dtype=dtype)
+
+    def _elsewhere(self):
+        """Whether another GPU is current: a launch would go there, whichever GPU its pointers are on."""
+        if not self._own_stream and torch._C._cuda_getCurrentRawStream(self._index) != self.stream:
+            raise StError(ST_EINVAL, "called under another stream than it was made on")
+        return torch._C._cuda_getDevice() != self._index
+
+    def _tree_of(self, spans):
+        if not isinstance(spans, DraftSpans):
+            return None
+        if not all(d == self._dev for d in spans.devices):
+            raise StError(ST_EINVAL, f"the tree of the spans is on {spans.devices}, the call on {self._dev}")
+        return spans.tree
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_TYPE_OF = {torch.bfloat16: ST_BF16, torch.float16: ST_F16, torch.float32: ST_F32}
+_PAIRS_OF = {"halves": ST_PAIRS_HALVES, "neighbours": ST_PAIRS_NEIGHBOURS}
+
+
+def _device_of(device):
+    dev = torch.device(device)
+    if dev.type != "cuda":
+        raise StError(ST_EINVAL, f"needs a GPU, got {dev}")
+    return dev if dev.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+
+class PagedCache(_OnStream):
+    """st_paged over torch-owned device buffers: a key/value cache in pages, with append, attend and keep for chains, chunks and trees of drafts.
+
+    cfg: dict of the fields of st_paged_config, dtype a torch type (bfloat16 or float16), rot_dim head_dim where it is not given, rot_pairs "halves" (the
+    default) or "neighbours".  table: int32 [n_seq][max_pages], read when a call runs (its entries may change, the tensor is kept).  cache: [2][n_layers]
+    [n_pages][n_kv_heads][page_size][head_dim]; allocated here if it is not given."""
+
+    def __init__(self, cfg, rope, table, cache=None, stream=None):
+        cfg = dict(dict(rot_dim=cfg["head_dim"], rot_pairs="halves", dtype=torch.bfloat16), **cfg)
+        if cfg["dtype"] not in (torch.bfloat16, torch.float16):
+            raise StError(ST_EINVAL, f"dtype is bfloat16 or float16, got {cfg['dtype']}")
+        if cfg["rot_pairs"] not in _PAIRS_OF:
+            raise StError(ST_EINVAL, f"rot_pairs is 'halves' or 'neighbours', got {cfg['rot_pairs']!r}")
+        self.cfg, self.dtype = cfg, cfg["dtype"]
+        numbers = dict(cfg, dtype=_TYPE_OF[cfg["dtype"]], rot_pairs=_PAIRS_OF[cfg["rot_pairs"]])
+        _fits32("config", *(numbers[n] for n, t in st_paged_config._fields_ if t is C.c_int32))
+        self._c = st_paged_config(*(numbers[n] for n, _ in st_paged_config._fields_))
+        cb, wb = C.c_size_t(), C.c_size_t()
+        _check(lib().st_paged_query_sizes(C.byref(self._c), C.byref(cb), C.byref(wb)))
+        shape = (2, cfg["n_layers"], cfg["n_pages"], cfg["n_kv_heads"], cfg["page_size"], cfg["head_dim"])
+        if not table.is_cuda or table.dtype != torch.int32 or not table.is_contiguous() or tuple(table.shape) != (cfg["n_seq"], cfg["max_pages"]):
+            raise StError(ST_EINVAL, f"table is a contiguous int32 CUDA tensor [n_seq][max_pages], got {table.dtype} {tuple(table.shape)}")
+        dev = table.device
+        if cfg["rot_dim"] and (rope is None or rope.device != dev or rope.dtype != torch.float32 or not rope.is_contiguous() or
+                               tuple(rope.shape) != (cfg["max_pos"], cfg["rot_dim"] // 2, 2)):
+            raise StError(ST_EINVAL, "rope is a contiguous float32 tensor [max_pos][rot_dim / 2][2] on the device of table")
+        self._bind(dev, stream)
+        self._ws = self._empty((wb.value,), torch.uint8)
+        if cache is None:
+            cache = self._empty(shape, self.dtype)
+        if cache.device != dev or cache.dtype != self.dtype or not cache.is_contiguous() or tuple(cache.shape) != shape:
+            raise StError(ST_EINVAL, f"cache is a contiguous {self.dtype} tensor {shape} on the device of table, got {cache.dtype} {tuple(cache.shape)} on {cache.device}")
+        self.cache, self.rope, self.table = cache, rope, table
+        h = C.c_void_p()
+        _check(lib().st_paged_create(C.byref(self._c), rope.data_ptr() if cfg["rot_dim"] else None, table.data_ptr(), cache.data_ptr(),
+                                     cache.numel() * 2, self._ws.data_ptr(), wb.value, self.stream, C.byref(h)))
+        L = lib()
+        self._h, self._destroy = h, L.st_paged_destroy
+        self._append, self._attend, self._keep = L.st_paged_append, L.st_paged_attend, L.st_paged_keep
+        self._nq, self._nkv, self._d, self._layers = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"], cfg["n_layers"]
+
+    def _matrix(self, name, x, rows, heads):
+        """(pointer, row stride) of [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
+        d, shape = self._d, x.shape
+        if x.dtype is not self.dtype or x.get_device() != self._index:
+            raise StError(ST_EINVAL, f"{name} is {self.dtype} on {self._dev}, got {x.dtype} on {x.device}")
+        if x.is_contiguous() and (shape == (rows, heads, d) or shape == (rows, heads * d)):
+            return x.data_ptr(), heads * d
+        stride = x.stride()
+        if not (shape == (rows, heads * d) and stride[1] == 1 or
+                shape == (rows, heads, d) and stride[2] == 1 and (stride[1] == d or heads == 1)):
+            raise StError(ST_EINVAL, f"{name} has shape {tuple(shape)} and strides {stride}, needs {rows} rows of {heads} x {d}")
+        return x.data_ptr(), stride[0] if rows > 1 else max(stride[0], heads * d)
+
+    def _norm(self, name, w):
+        if w is None:
+            return None
+        if w.dtype is not self.dtype or w.shape != (self._d,) or not w.is_contiguous() or w.get_device() != self._index:
+            raise StError(ST_EINVAL, f"{name} is {self.dtype} [{self._d}] on {self._dev}, got {w.dtype} {tuple(w.shape)}")
+        return w.data_ptr()
+
+    def _layer(self, layer):
+        if not 0 <= layer < self._layers:
+            raise StError(ST_ERANGE, f"layer {layer} outside [0, {self._layers})")
+
+    def append(self, layer, spans, qkv, q_norm=None, k_norm=None):
+        """Norms ([head_dim], or None), rotation and the write of the spans' new rows; qkv: a row per new token, all query heads, then key heads, then
+        value heads.  Returns the rotated queries, [rows][n_q_heads][head_dim]."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.append(layer, spans, qkv, q_norm, k_norm)
+        p, stride = self._matrix("qkv", qkv, spans.rows, self._nq + 2 * self._nkv)
+        qn, kn = self._norm("q_norm", q_norm), self._norm("k_norm", k_norm)
+        out = self._empty((spans.rows, self._nq, self._d), self.dtype)
+        if spans.rows:
+            self._layer(layer)
+            rc = self._append(self._h, layer, spans.c, spans.n, self._tree_of(spans), p, stride, qn, kn, out.data_ptr(), self._nq * self._d)
+            if rc:
+                _check(rc)
+        return out
+
+    def attend(self, layer, spans, q, out=None):
+        """Attention of the spans' rows over their sequences' slots; q: n_q_heads * head_dim a row.  With DraftSpans a row sees the context and its
+        branch, else what lies before it and itself.  Returns [rows][n_q_heads][head_dim] (or `out`)."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.attend(layer, spans, q, out)
+        p, stride = self._matrix("q", q, spans.rows, self._nq)
+        if out is None:
+            out = self._empty((spans.rows, self._nq, self._d), self.dtype)
+            po, so = out.data_ptr(), self._nq * self._d
+        else:
+            po, so = self._matrix("out", out, spans.rows, self._nq)
+        if spans.rows:
+            self._layer(layer)
+            rc = self._attend(self._h, layer, spans.c, spans.n, self._tree_of(spans), p, stride, po, so)
+            if rc:
+                _check(rc)
+        return out
+
+    def attend_plan(self, spans, with_tree=False):
+        """(columns of a block, blocks, key ranges of every span) of such an attend (see st_paged_attend_plan)."""
+        columns, blocks, ranges = C.c_int32(), C.c_int32(), (C.c_int32 * max(spans.n, 1))()
+        _check(lib().st_paged_attend_plan(C.byref(self._c), spans.c, spans.n, int(with_tree), C.byref(columns), C.byref(blocks), ranges))
+        return columns.value, blocks.value, list(ranges)[:spans.n]
+
+    def keep(self, layer_lo, layer_hi, spans, path, accepted):
+        """Moves the rows that stay, path[j][:accepted[j]] of span j (int32 tensors on the GPU, as DraftVerifier.verify returns them), to the slots behind the
+        span's row 0 in layers [layer_lo, layer_hi).  The sequence then has len + 1 + accepted[j] slots."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.keep(layer_lo, layer_hi, spans, path, accepted)
+        if (layer_lo | layer_hi) >> 31:
+            _fits32("keep", layer_lo, layer_hi)
+        for name, x, shape in (("path", path, (spans.n, path.shape[-1])), ("accepted", accepted, (spans.n,))):
+            if x.dtype is not torch.int32 or x.get_device() != self._index or x.shape != shape or not x.is_contiguous():
+                raise StError(ST_EINVAL, f"{name} is contiguous int32 with a row for each of {spans.n} spans on {self._dev}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        if spans.n:
+            _check(self._keep(self._h, layer_lo, layer_hi, spans.c, spans.n, path.data_ptr(), path.shape[1], accepted.data_ptr()))
+
+
+class DraftVerifier(_OnStream):
+    """st_verify over a torch-owned workspace: the verdict over drafted tokens (see st_verify_drafts)."""
+
+    def __init__(self, vocab, max_rows, max_width=1, dtype=torch.float32, device="cuda", stream=None):
+        if dtype not in _TYPE_OF:
+            raise StError(ST_EINVAL, f"dtype is float32, bfloat16 or float16, got {dtype}")
+        _fits32("config", vocab, max_rows, max_width)
+        c = st_verify_config(vocab, _TYPE_OF[dtype], max_rows, max_width)
+        wb = C.c_size_t()
+        _check(lib().st_verify_query_sizes(C.byref(c), C.byref(wb)))
+        self.vocab, self.dtype = vocab, dtype
+        self._bind(_device_of(device), stream)
+        self._ws = self._empty((wb.value,), torch.uint8)
+        h = C.c_void_p()
+        _check(lib().st_verify_create(C.byref(c), self._ws.data_ptr(), wb.value, self.stream, C.byref(h)))
+        self._h, self._destroy, self._drafts = h, lib().st_verify_destroy, lib().st_verify_drafts
+
+    def _logits(self, name, x, rows):
+        if x.dtype is not self.dtype or x.get_device() != self._index or x.shape != (rows, self.vocab) or (x.stride(1) != 1 and self.vocab > 1):
+            raise StError(ST_EINVAL, f"{name} is {self.dtype} [{rows}][{self.vocab}] on {self._dev}, got {x.dtype} {tuple(x.shape)} {x.stride()} on {x.device}")
+        return x.data_ptr(), x.stride(0) if rows > 1 else max(x.stride(0), self.vocab)
+
+    def _numbers(self, name, x, n, dtype):
+        if x.dtype is not dtype or x.get_device() != self._index or x.shape != (n,) or not x.is_contiguous():
+            raise StError(ST_EINVAL, f"{name} is {dtype} [{n}] on {self._dev}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
+
+    def verify(self, spans, tokens, target, temperature, accept, sample, draft=None):
+        """spans: the rows of every sequence, each a tree (DraftSpans) or a chain.  tokens int32 [rows]; target, draft: logits [rows][vocab] of what follows each
+        row; temperature: a number, or one of each sequence; accept [rows] and sample [sequences]: float64 random numbers of [0, 1).
+        Returns (path [sequences][most rows] with -1 behind the rows that stay, their numbers [sequences], next tokens [sequences]), int32."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.verify(spans, tokens, target, temperature, accept, sample, draft)
+        n, rows = spans.n, spans.rows
+        counts = [s[3] for s in spans.spans]
+        heat = [float(temperature)] * n if isinstance(temperature, (int, float)) else [float(x) for x in temperature]
+        if len(heat) != n:
+            raise StError(ST_EINVAL, f"{len(heat)} temperatures for {n} sequences")
+        pt, st = self._logits("target", target, rows)
+        pd, sd = (None, 0) if draft is None else self._logits("draft", draft, rows)
+        pk = self._numbers("tokens", tokens, rows, torch.int32)
+        pa, ps = self._numbers("accept", accept, rows, torch.float64), self._numbers("sample", sample, n, torch.float64)
+        most = max(counts, default=0)
+        path, accepted, after = self._empty((n, most), torch.int32), self._empty((n,), torch.int32), self._empty((n,), torch.int32)
+        if n:
+            _check(self._drafts(self._h, (C.c_int32 * n)(*counts), n, self._tree_of(spans), pk, pt, st, pd, sd, (C.c_float * n)(*heat), pa, ps,
+                                path.data_ptr(), most, accepted.data_ptr(), after.data_ptr()))
+        return path, accepted, after

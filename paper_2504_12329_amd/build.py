@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libst.so")
 SOURCES = ["api.hip", "decode.hip", "prefill.hip", "trigger.hip", "persist.hip", "kv4.hip", "kv4_attend.hip",
-           "kv4_evict.hip"]
+           "kv4_evict.hip", "paged.hip", "paged_attend.hip", "verify.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

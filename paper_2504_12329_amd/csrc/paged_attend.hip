@@ -1,0 +1,700 @@
+// Attention over the key/value cache in pages: causal, or for drafted rows that each see the context and their own branch.
+//
+// The query heads of a kv head are folded into columns: column i * G + h is row i of head h.  With S^T = K Q^T (slots x columns) a lane holds one column, so the
+// softmax is register arithmetic and P^T is the second product's operand as it stands: O^T = V^T P^T.  Scores, maxima, sums and outputs are fp32; the weights
+// enter the second product in 16 bits (rounded just below the running maximum's 1, where that costs least), as the framework's other attention does.
+//
+// What a column sees of a tile is a word of bits: all of the context, of the span's own rows the first i + 1 or those that `sees` names, nothing of a hole and
+// nothing past the end.  It is only made where some column does not see all of the tile ("part").  There the values are looked through as well: an infinity or NaN
+// times a weight of zero would reach columns that do not see it, so such numbers are multiplied as zeros, and added to the columns that see them.
+#include <algorithm>
+#include <atomic>
+#include <utility>
+
+#include "checks.h"
+#include "paged.h"
+#include "st_device.h"
+
+namespace st {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// Bits of slots key0 .. key0 + 63 that row `row` of a span sees, holes aside
+__device__ __forceinline__ uint64_t seen_bits(const uint64_t *__restrict__ sees, int words, int len, int rows, int row0, int row, int key0) {
+    const int j0 = key0 - len;  // the span's row in slot key0
+    auto below = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; };  // the first n bits
+    if (!sees) return below(row + 1 - j0);
+    if (j0 <= -64) return ~0ull;
+    const uint64_t *w = sees + (int64_t)(row0 + row) * words;
+    uint64_t own;
+    if (j0 <= 0) {
+        own = below(-j0) | w[0] << -j0;
+    } else {
+        const int i = j0 >> 6, s = j0 & 63;
+        own = i < words ? w[i] >> s : 0ull;
+        if (s && i + 1 < words) own |= w[i + 1] << (64 - s);
+    }
+    return own & below(rows - j0);
+}
+
+// One column's query: row of the span and head
+struct PagedColumn {
+    int row, head;
+};
+__device__ __forceinline__ PagedColumn paged_column(int col, int G, int kvh) { return PagedColumn{col / G, kvh * G + col % G}; }
+
+// ---------------------------------------------------------------------------------------
+// Few columns: single tokens and short runs, bound by reading the cache once.
+//
+// A wave works on its own, on tiles of 32 slots, with NT tiles of 16 columns and no LDS until the end: S^T by 16x16x32 MFMAs whose A rows are slots 8 (m / 4) + 4 t +
+// m % 4, so that lane (column, quarter) ends up with the weights of slots 8 quarter .. + 7 -- the B operand of the second product.  Keys are read as the first
+// product wants them, 64 bytes of 16 slots an instruction; of eight slots of values a lane reads the D / 16 channels that make its row m of D / 16 products, whole
+// slots an instruction, and puts the slots of a channel together by byte permutes.  The next tile's loads are issued before this tile's work, its pages' numbers (wave-uniform, in
+// scalar registers) one tile before that.  A block's four waves take every fourth tile of its range and are joined through LDS; ranges are joined by k_paged_join.
+// ---------------------------------------------------------------------------------------
+constexpr int kFewTile = 32, kFewWaves = 4;
+
+template <class T, int D, int NT, int CAP>
+__global__ __launch_bounds__(256, 2) void k_paged_few(const Kv4Spans<CAP> t, const PagedView view, const uint64_t *__restrict__ sees, int words,
+                                                      const uint16_t *__restrict__ q, int64_t q_stride, uint16_t *__restrict__ out, int64_t out_stride,
+                                                      float *__restrict__ part_o, float *__restrict__ part_ml) {
+    constexpr int KS = D / 32, DPL = D / 16, VW = DPL / 2;  // VW: words of values of a slot and lane
+    typedef typename T::vec8 vec8;
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m16 = lane & 15, qd = lane >> 4;
+    const int nkv = view.nkv, G = view.nq / nkv;
+    const int cols = sp.rows * G, n_cb = (cols + 16 * NT - 1) / (16 * NT), local = blockIdx.x - sp.blk0;
+    const int kvh = local % nkv, z = local / nkv / n_cb, c0 = local / nkv % n_cb * (16 * NT);  // c0: the block's first column
+    const int n_keys = sees ? sp.len + sp.rows : sp.len + min(c0 + 16 * NT - 1, cols - 1) / G + 1, last = n_keys - 1;
+    const int n_tiles = (n_keys + kFewTile - 1) / kFewTile;
+    const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
+    const int32_t *__restrict__ pages = view.table + (int64_t)sp.seq * view.max_pages;
+    const int mask = (1 << view.shift) - 1;
+    const int all_see = sees ? sp.len - 1 : sp.len + c0 / G;  // last slot that all of its columns see
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+
+    vec8 qf[NT][KS];
+    int row[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const PagedColumn w = paged_column(min(c0 + 16 * c + m16, cols - 1), G, kvh);
+        row[c] = w.row;
+        const uint16_t *src = q + (int64_t)(sp.row0 + w.row) * q_stride + w.head * D + qd * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[c][s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4 *>(src + 32 * s));
+    }
+    f32x4 o[NT][DPL];
+    float m_i[NT], l_i[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        m_i[c] = -INFINITY, l_i[c] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Pages {  // of slots 0-15 and 16-31 of a tile
+        int a, b;
+    };
+    struct Tile {
+        u32x4 k[2][KS];
+        uint32_t v[8][VW];
+        Pages at;
+    };
+    auto look_up = [&](int tile) {
+        const int key0 = tile * kFewTile;
+        return Pages{page_of(pages, view.n_pages, min(key0, last) >> view.shift), page_of(pages, view.n_pages, min(key0 + 16, last) >> view.shift)};
+    };
+    auto load = [&](Tile &x, int tile, Pages at) {
+        const int key0 = tile * kFewTile;
+        x.at = at;
+        const size_t a = ((size_t)max(at.a, 0) * nkv + kvh) << view.shift, b = ((size_t)max(at.b, 0) * nkv + kvh) << view.shift;
+        const uint16_t *kp = view.k + (m16 >= 8 ? b : a) * D + qd * 8, *vp = view.v + (qd >= 2 ? b : a) * D + m16 * DPL;
+        const bool whole = key0 + kFewTile <= n_keys;
+        // (slots past the last one are read as the last, so that no address past it is formed)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int slot = min(key0 + 8 * (m16 >> 2) + 4 * u + (m16 & 3), last) & mask;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) x.k[u][s] = *reinterpret_cast<const u32x4 *>(kp + slot * D + 32 * s);
+        }
+        auto value = [&](int j, int slot) {
+            if constexpr (VW == 4) {
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(vp + slot * D);
+                x.v[j][0] = w.x, x.v[j][1] = w.y, x.v[j][2] = w.z, x.v[j][3] = w.w;
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2 *>(vp + slot * D);
+                x.v[j][0] = w.x, x.v[j][1] = w.y;
+            }
+        };
+        if (whole) {
+            const int first = (key0 + 8 * qd) & mask;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) value(j, first + j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) value(j, min(key0 + 8 * qd + j, last) & mask);
+        }
+    };
+    auto work = [&](Tile &x, int tile) {
+        const int key0 = tile * kFewTile;
+        f32x4 sc[NT][2];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) sc[c][0] = sc[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) sc[c][u] = T::mfma16(__builtin_bit_cast(vec8, x.k[u][s]), qf[c][s], sc[c][u]);
+        const bool part = key0 + kFewTile - 1 > all_see || (x.at.a | x.at.b) < 0;
+        uint32_t seen[NT];
+        bool spoiled = false;
+        if (part) {
+            const uint32_t held = (x.at.a < 0 ? 0u : 0xffffu) | (x.at.b < 0 ? 0u : 0xffff0000u);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                seen[c] = (uint32_t)seen_bits(sees, words, sp.len, sp.rows, sp.row0, row[c], key0) & held;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!(seen[c] >> (8 * qd + 4 * u + r) & 1)) sc[c][u][r] = -INFINITY;
+            }
+            uint32_t bad = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int w = 0; w < VW; ++w) bad |= not_finite<T>(x.v[j][w]);
+            spoiled = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+            if (spoiled)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) x.v[j][w] &= ~halves_of(not_finite<T>(x.v[j][w]));
+        }
+        vec8 pf[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            float mx = sc[c][0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[c][u][r]);
+            float a, b;
+            with_xor16(mx, a, b);
+            mx = max_xor32(fmaxf(a, b));
+            const float cand = mx * scale;
+            const bool raise = cand > m_i[c];
+            const float m_new = raise ? cand : m_i[c];
+            const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
+            if (__builtin_amdgcn_ballot_w64(raise)) {
+                const float corr = raise ? __builtin_amdgcn_exp2f(m_i[c] - base) : 1.0f;
+                l_i[c] *= corr;
+#pragma unroll
+                for (int d = 0; d < DPL; ++d) o[c][d] *= corr;
+            }
+            m_i[c] = m_new;
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p[j] = __builtin_amdgcn_exp2f(fmaf(sc[c][j >> 2][j & 3], scale, -base));
+                l_i[c] += p[j];
+            }
+            pf[c] = __builtin_bit_cast(vec8, u32x4{T::pack(p[0], p[1]), T::pack(p[2], p[3]), T::pack(p[4], p[5]), T::pack(p[6], p[7])});
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+            const u32x4 even = {low_halves(x.v[0][w], x.v[1][w]), low_halves(x.v[2][w], x.v[3][w]), low_halves(x.v[4][w], x.v[5][w]), low_halves(x.v[6][w], x.v[7][w])};
+            const u32x4 odd = {high_halves(x.v[0][w], x.v[1][w]), high_halves(x.v[2][w], x.v[3][w]), high_halves(x.v[4][w], x.v[5][w]), high_halves(x.v[6][w], x.v[7][w])};
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                o[c][2 * w] = T::mfma16(__builtin_bit_cast(vec8, even), pf[c], o[c][2 * w]);
+                o[c][2 * w + 1] = T::mfma16(__builtin_bit_cast(vec8, odd), pf[c], o[c][2 * w + 1]);
+            }
+        }
+        if (spoiled)  // this lane's channels are (4 qd + r) DPL + d
+            for (int j = 0; j < kFewTile && key0 + j < n_keys; ++j) {
+                const int page = j < 16 ? x.at.a : x.at.b;
+                if (page < 0) continue;
+                const uint16_t *src = view.v + ((((size_t)page * nkv + kvh) << view.shift) + ((key0 + j) & mask)) * D + 4 * qd * DPL;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int d = 0; d < DPL; d += 2) {
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(src + r * DPL + d), b = not_finite<T>(w);
+#pragma unroll
+                        for (int c = 0; c < NT; ++c) {
+                            if ((b & 0x8000u) && (seen[c] >> j & 1)) o[c][d][r] += T::lo(w);
+                            if ((b >> 31) && (seen[c] >> j & 1)) o[c][d + 1][r] += T::hi(w);
+                        }
+                    }
+            }
+    };
+    Tile a, b;
+    int i = t_begin + wave;
+    if (i < t_end) {
+        load(a, i, look_up(i));
+        Pages next = look_up(min(i + kFewWaves, t_end - 1));
+        while (true) {
+            if (i + kFewWaves < t_end) {
+                load(b, i + kFewWaves, next);
+                next = look_up(min(i + 2 * kFewWaves, t_end - 1));
+            }
+            work(a, i);
+            i += kFewWaves;
+            if (i >= t_end) break;
+            if (i + kFewWaves < t_end) {
+                load(a, i + kFewWaves, next);
+                next = look_up(min(i + 2 * kFewWaves, t_end - 1));
+            }
+            work(b, i);
+            i += kFewWaves;
+            if (i >= t_end) break;
+        }
+    }
+
+    // the four waves' results, one tile of columns after another
+    constexpr int LD = D + 4;
+    __shared__ __align__(16) float so[kFewWaves][16][LD];
+    __shared__ float sm[kFewWaves][16], sl[kFewWaves][16];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const float l = sum_xor32(sum_xor16(l_i[c]));
+        if (c) __syncthreads();
+        if (qd == 0) sm[wave][m16] = m_i[c], sl[wave][m16] = l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int d = 0; d < DPL; d += 4)
+                *reinterpret_cast<float4 *>(&so[wave][m16][(4 * qd + r) * DPL + d]) =
+                    make_float4(o[c][d][r], o[c][d + 1][r], o[c][d + 2][r], o[c][d + 3][r]);
+        __syncthreads();
+        const int col = c0 + 16 * c + (threadIdx.x >> 4), n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DPL;
+        if (col >= cols) continue;
+        float M = sm[0][n], L = 0.f;
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) M = fmaxf(M, sm[v][n]);
+        float x[DPL];
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v) {
+            if (sl[v][n] == 0.f) continue;  // a wave that saw nothing
+            const float w = __builtin_amdgcn_exp2f(sm[v][n] - M);
+            L += w * sl[v][n];
+#pragma unroll
+            for (int e = 0; e < DPL; ++e) x[e] = fmaf(w, so[v][n][d0 + e], x[e]);
+        }
+        const PagedColumn where = paged_column(col, G, kvh);
+        if (sp.splits == 1) {
+            const float inv = L == 0.f ? 0.f : 1.0f / L;
+            uint16_t *dst = out + (int64_t)(sp.row0 + where.row) * out_stride + where.head * D + d0;
+            if constexpr (DPL == 8)
+                *reinterpret_cast<u32x4 *>(dst) = u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(x[4] * inv, x[5] * inv),
+                                                        T::pack(x[6] * inv, x[7] * inv)};
+            else
+                *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv)};
+        } else {
+            const size_t pr = (size_t)sp.part0 + ((size_t)z * sp.rows + where.row) * view.nq + where.head;
+#pragma unroll
+            for (int e = 0; e < DPL; e += 4)
+                *reinterpret_cast<float4 *>(part_o + pr * D + d0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            if (d0 == 0) *reinterpret_cast<float2 *>(part_ml + pr * 2) = make_float2(M, L);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Many columns: trees and chunks.  A block is 128 columns of one kv head, 32 to a wave, on a range of tiles of 64 slots.  Keys and values go from memory to LDS
+// directly (a wave loads 16 slots of a tile, which lie in one page), a tile ahead, 16-byte chunks swapped by the slot so that neither the reads of S^T
+// fragments nor the transposing reads of V^T meet in a bank.  S^T rows: fragment row m of 32 slots is slot m with bits 2 and 3 exchanged: registers 0-7 and
+// 8-15 of a lane are then eight consecutive slots each, as the second product wants them.
+// ---------------------------------------------------------------------------------------
+constexpr int kChunkTile = 64, kChunkCols = kPagedColumns;
+template <int D>
+constexpr int kChunkTileBytes = kChunkTile * D * 2;
+template <int D>
+constexpr int kChunkLds = 4 * kChunkTileBytes<D> + 64;  // two tiles of keys, two of values, and eight words: whether a wave's values were not finite
+
+// 64 lanes x 16 bytes from per-lane addresses to 1 KB of LDS starting at lds_off (wave-uniform)
+__device__ __forceinline__ void to_lds16(const void *g, uint32_t lds_off) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(__builtin_amdgcn_readfirstlane(lds_off)) : "memory");
+}
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <class T, int D, int CAP>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, const PagedView view, const uint64_t *__restrict__ sees, int words,
+                                                        const uint16_t *__restrict__ q, int64_t q_stride, uint16_t *__restrict__ out, int64_t out_stride,
+                                                        float *__restrict__ part_o, float *__restrict__ part_ml) {
+    constexpr int ST = D / 16, TT = D / 32, RB = D * 2, CPR = RB / 16, SPI = 64 / CPR;  // RB: bytes of a slot, CPR: its chunks, SPI: slots a load instruction fills
+    typedef typename T::vec8 vec8;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const Kv4Span sp = t.s[kv4_span_of(t, blockIdx.x)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+    const int nkv = view.nkv, G = view.nq / nkv, cols = sp.rows * G, n_cb = (cols + kChunkCols - 1) / kChunkCols;
+    const int local = blockIdx.x - sp.blk0, kvh = local % nkv, z = local / nkv / n_cb;
+    const int cb = n_cb - 1 - local / nkv % n_cb;  // the blocks with the most slots first
+    const int c0 = cb * kChunkCols + wave * 32, col = min(c0 + l32, cols - 1);
+    const bool active = c0 < cols;
+    const PagedColumn where = paged_column(col, G, kvh);
+    // the last slot that all columns of the block (wave) see, and the last that some column of the wave does
+    const int block_all = sees ? sp.len - 1 : sp.len + cb * kChunkCols / G;
+    const int wave_all = sees ? sp.len - 1 : sp.len + min(c0, cols - 1) / G;
+    const int wave_last = sees ? sp.len + sp.rows - 1 : sp.len + min(c0 + 31, cols - 1) / G;
+    const int n_keys = sees ? sp.len + sp.rows : sp.len + min(cb * kChunkCols + kChunkCols - 1, cols - 1) / G + 1, last = n_keys - 1;
+    const int n_tiles = (n_keys + kChunkTile - 1) / kChunkTile;
+    const int t_begin = z * sp.per, t_end = min(n_tiles, t_begin + sp.per);
+    const int32_t *__restrict__ pages = view.table + (int64_t)sp.seq * view.max_pages;
+    const int mask = (1 << view.shift) - 1;
+    const float scale = 1.4426950408889634f / sqrtf((float)D);
+
+    vec8 qf[ST];
+    {
+        const uint16_t *src = q + (int64_t)(sp.row0 + where.row) * q_stride + where.head * D + 8 * hf;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) qf[s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4 *>(src + 16 * s));
+    }
+    f32x16 o[TT];
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[tt][r] = 0.f;
+    float m_i = -INFINITY, l_i = 0.f;
+
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    typedef __attribute__((address_space(3))) uint32_t lds_u32;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    auto k_at = [&](int i) { return lds0 + (i & 1) * kChunkTileBytes<D>; };
+    auto v_at = [&](int i) { return lds0 + (2 + (i & 1)) * kChunkTileBytes<D>; };
+    auto flags_at = [&](int i) { return lds0 + 4 * kChunkTileBytes<D> + (i & 1) * 16; };
+    // Chunk c of slot r lies at position c ^ swap(r).  D 128: the 16 slots of an S^T read take 16 different positions, and so do the (slot, chunk) pairs of a
+    // transposing read.  D 64: slots of 128 bytes, two to a row of banks: every other slot of a read takes every position.
+    auto swap = [](int r) { return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (r >> 1) & 7; };
+    // Pages of the tile's four runs of 16 slots: lane i < 4 looks up run i
+    auto look_up = [&](int tile) { return page_of(pages, view.n_pages, min(tile * kChunkTile + 16 * (lane & 3), last) >> view.shift); };
+    auto held_runs = [&](int at) { return (uint32_t)__builtin_amdgcn_ballot_w64(at >= 0) & 15u; };
+    auto load = [&](int tile, int at) {
+        const int key0 = tile * kChunkTile + 16 * wave;
+        const int page = max(__builtin_amdgcn_readlane(at, wave), 0);
+        const size_t head0 = (((size_t)page * nkv + kvh) << view.shift) * D;
+#pragma unroll
+        for (int e = 0; e < 16 / SPI; ++e) {
+            const int r = 16 * wave + e * SPI + lane / CPR, slot = min(key0 + e * SPI + lane / CPR, last) & mask;
+            const size_t off = head0 + (uint32_t)(slot * D + ((lane % CPR) ^ swap(r)) * 8);
+            to_lds16(view.k + off, k_at(tile) + (16 * wave + e * SPI) * RB);
+            to_lds16(view.v + off, v_at(tile) + (16 * wave + e * SPI) * RB);
+        }
+    };
+    auto is_part = [&](int tile, uint32_t held) { return tile * kChunkTile + kChunkTile - 1 > block_all || held != 15u; };
+    // Looks through the values this wave has loaded: what is not finite becomes zero, and is noted
+    auto look_through = [&](int tile) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int e = 0; e < 16 * RB / 1024; ++e) {
+            lds_u32x4 *p = (lds_u32x4 *)(uintptr_t)(v_at(tile) + 16 * wave * RB + e * 1024 + lane * 16);
+            u32x4 w = *p;
+            uint32_t bad = 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t b = not_finite<T>(w[x]);
+                bad |= b;
+                w[x] &= ~halves_of(b);
+            }
+            if (bad) *p = w;
+            any |= bad;
+        }
+        const bool spoiled = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+        if (lane == 0) *((lds_u32 *)(uintptr_t)(flags_at(tile) + 4 * wave)) = spoiled;
+    };
+    // S^T: lane i of a 32-slot fragment reads slot swap23(i);  V^T: lane 4 r + x of a group of 16 reads four channels of slot r
+    const int krow = (l32 & 19) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+    const int vr = (lane & 15) >> 2, vx = lane & 3, vg = (lane >> 4) & 1;
+    auto compute = [&](int tile, uint32_t held, bool part) {
+        const int key0 = tile * kChunkTile;
+        f32x16 sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[u][r] = 0.f;
+        const uint32_t kt = k_at(tile) + krow * RB, ksw = swap(krow);
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {  // (32 slots on do not change the swap)
+                const u32x4 w = *((const lds_u32x4 *)(uintptr_t)(kt + u * 32 * RB + (((2 * s + hf) ^ ksw) << 4)));
+                sc[u] = T::mfma32(__builtin_bit_cast(vec8, w), qf[s], sc[u]);
+            }
+        uint64_t seen = ~0ull;
+        if (key0 + kChunkTile - 1 > wave_all || held != 15u) {
+            seen = seen_bits(sees, words, sp.len, sp.rows, sp.row0, where.row, key0);
+#pragma unroll
+            for (int run = 0; run < 4; ++run)
+                if (!(held >> run & 1)) seen &= ~(0xffffull << (16 * run));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t bits = (uint32_t)(seen >> (32 * u)) >> (8 * hf);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!(bits >> (16 * (r >> 3) + (r & 7)) & 1)) sc[u][r] = -INFINITY;
+            }
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[u][r]);
+        mx = max_xor32(mx);
+        const float cand = mx * scale;
+        const bool raise = cand > m_i;
+        const float m_new = raise ? cand : m_i;
+        const float base = m_new == -INFINITY ? 0.f : m_new;  // a row may have seen no slot yet
+        if (__builtin_amdgcn_ballot_w64(raise)) {
+            const float corr = raise ? __builtin_amdgcn_exp2f(m_i - base) : 1.0f;
+            l_i *= corr;
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[tt][r] *= corr;
+        }
+        m_i = m_new;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][r], scale, -base));
+                sc[u][r] = p;
+                l_i += p;
+            }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int u = s >> 1, b = 8 * (s & 1);
+            const vec8 pf = __builtin_bit_cast(vec8, u32x4{T::pack(sc[u][b], sc[u][b + 1]), T::pack(sc[u][b + 2], sc[u][b + 3]), T::pack(sc[u][b + 4], sc[u][b + 5]),
+                                                           T::pack(sc[u][b + 6], sc[u][b + 7])});
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt) {
+                u32x4 w;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int slot = 16 * s + 8 * hf + 4 * h + vr, chunk = 4 * tt + 2 * vg + (vx >> 1);
+                    const uint32_t at = v_at(tile) + slot * RB + ((chunk ^ swap(slot)) << 4) + (vx & 1) * 8;
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at));
+                    w[2 * h] = x.x, w[2 * h + 1] = x.y;
+                }
+                o[tt] = T::mfma32(__builtin_bit_cast(vec8, w), pf, o[tt]);
+            }
+        }
+        if (part) {
+            const u32x4 f = *((const lds_u32x4 *)(uintptr_t)flags_at(tile));
+            if (f.x | f.y | f.z | f.w)  // register r of tile tt is channel 32 tt + r % 4 + 8 (r / 4) + 4 hf
+                for (int j = 0; j < kChunkTile && key0 + j < n_keys; ++j) {
+                    const int page = page_of(pages, view.n_pages, (key0 + j) >> view.shift);
+                    if (page < 0 || !(seen >> j & 1)) continue;
+                    const uint16_t *src = view.v + ((((size_t)page * nkv + kvh) << view.shift) + ((key0 + j) & mask)) * D + 4 * hf;
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                        for (int r = 0; r < 16; r += 2) {
+                            const uint32_t w = *reinterpret_cast<const uint32_t *>(src + 32 * tt + (r & 3) + 8 * (r >> 2)), b = not_finite<T>(w);
+                            if (b & 0x8000u) o[tt][r] += T::lo(w);
+                            if (b >> 31) o[tt][r + 1] += T::hi(w);
+                        }
+                }
+        }
+    };
+    if (t_begin < t_end) {
+        int at = look_up(t_begin), next = look_up(min(t_begin + 1, t_end - 1));
+        load(t_begin, at);
+        for (int i = t_begin; i < t_end; ++i) {
+            const uint32_t held = held_runs(at);
+            const bool part = is_part(i, held);
+            wait_for_loads();
+            if (part) look_through(i);
+            __syncthreads();  // tile i is whole, and tile i - 1 has been read by every wave
+            if (i + 1 < t_end) {
+                load(i + 1, next);
+                at = next;
+                next = look_up(min(i + 2, t_end - 1));
+            }
+            if (active && i * kChunkTile <= wave_last) compute(i, held, part);
+        }
+    }
+    l_i = sum_xor32(l_i);
+    if (!active || c0 + l32 >= cols) return;
+    if (sp.splits == 1) {
+        const float inv = l_i == 0.f ? 0.f : 1.0f / l_i;
+        uint16_t *dst = out + (int64_t)(sp.row0 + where.row) * out_stride + where.head * D + 4 * hf;
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<u32x2 *>(dst + 32 * tt + 2 * r) = u32x2{T::pack(o[tt][r] * inv, o[tt][r + 1] * inv), T::pack(o[tt][r + 2] * inv, o[tt][r + 3] * inv)};
+    } else {
+        const size_t pr = (size_t)sp.part0 + ((size_t)z * sp.rows + where.row) * view.nq + where.head;
+        float *dst = part_o + pr * D + 4 * hf;
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<float4 *>(dst + 32 * tt + 2 * r) = make_float4(o[tt][r], o[tt][r + 1], o[tt][r + 2], o[tt][r + 3]);
+        if (hf == 0) *reinterpret_cast<float2 *>(part_ml + pr * 2) = make_float2(m_i, l_i);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them are fetched at once; then D / 4
+// lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range of which the row sees nothing has sum 0 and an unused output.
+// ---------------------------------------------------------------------------------------
+template <class T, int D, int WPU, int CAP>
+__global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                                                    uint16_t *__restrict__ out, int64_t out_stride) {
+    constexpr int UPB = 4 / WPU, TPR = D / 4, PAR = 64 * WPU / TPR, kBatch = 8;  // units of a block, lanes of a range, ranges at a time
+    __shared__ float4 red[UPB][(PAR - 1) * TPR];
+    const Kv4Span sp = t.s[blockIdx.y];
+    if (sp.splits == 1 || (int)blockIdx.x * UPB >= sp.rows * nq) return;
+    const int unit = blockIdx.x * UPB + threadIdx.x / (64 * WPU);
+    const bool live = unit < sp.rows * nq;
+    const int lane = threadIdx.x & 63, tid = threadIdx.x & (64 * WPU - 1), e = tid % TPR, g = tid / TPR;
+    const size_t step = (size_t)sp.rows * nq, pr = (size_t)sp.part0 + unit;
+    const float2 ml = live && lane < sp.splits ? reinterpret_cast<const float2 *>(part_ml)[pr + lane * step] : make_float2(-INFINITY, 0.f);
+    const float4 *po = reinterpret_cast<const float4 *>(part_o) + pr * TPR + e;
+    float4 v[kBatch];
+    auto fetch = [&](int z0) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = live && z0 + u * PAR < sp.splits ? po[(z0 + u * PAR) * step * TPR] : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    fetch(g);
+    const float M = wave_max(ml.x);
+    const float w = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float L = wave_sum(ml.y == 0.f ? 0.f : w * ml.y);
+    float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z0 = g; z0 - g < sp.splits; z0 += kBatch * PAR) {
+        if (z0 != g) fetch(z0);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int z = z0 + u * PAR;
+            const float wz = __shfl(w, z & 63, kWave), lz = __shfl(ml.y, z & 63, kWave);
+            if (z < sp.splits && lz != 0.f) A.x = fmaf(wz, v[u].x, A.x), A.y = fmaf(wz, v[u].y, A.y), A.z = fmaf(wz, v[u].z, A.z), A.w = fmaf(wz, v[u].w, A.w);
+        }
+    }
+    if constexpr (PAR > 1) {  // the PAR sums, in order
+        float4 *mine = red[threadIdx.x / (64 * WPU)];
+        if (g) mine[(g - 1) * TPR + e] = A;
+        __syncthreads();
+        if (g == 0)
+#pragma unroll
+            for (int i = 1; i < PAR; ++i) {
+                const float4 x = mine[(i - 1) * TPR + e];
+                A.x += x.x, A.y += x.y, A.z += x.z, A.w += x.w;
+            }
+    }
+    if (!live || g) return;
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const int row = sp.row0 + unit / nq, head = unit % nq;
+    *reinterpret_cast<u32x2 *>(out + (int64_t)row * out_stride + head * D + 4 * e) = u32x2{T::pack(A.x * inv, A.y * inv), T::pack(A.z * inv, A.w * inv)};
+}
+
+// ---------------------------------------------------------------------------------------
+// launcher
+// ---------------------------------------------------------------------------------------
+PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree) {
+    const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv;
+    int64_t most = 0, longest = 0;
+    for (int j = 0; j < t.n; ++j) {
+        if (!t.s[j].rows) continue;
+        most = std::max<int64_t>(most, (int64_t)t.s[j].rows * G);
+        longest = std::max<int64_t>(longest, (int64_t)t.s[j].len + t.s[j].rows);
+    }
+    PagedAttendPlan p{most <= 16 ? 16 : most <= 32 ? 32 : kChunkCols, 0, 0};
+    const bool few = p.cols < kChunkCols;
+    const int tile = few ? kFewTile : kChunkTile, step = few ? kFewWaves : 1;
+    auto groups = [&](const Kv4Span &s) { return (int64_t)nkv * (((int64_t)s.rows * G + p.cols - 1) / p.cols); };
+    auto tiles = [&](const Kv4Span &s) { return ((int64_t)s.len + s.rows + tile - 1) / tile; };
+    int64_t work = 0;
+    for (int j = 0; j < t.n; ++j)
+        if (t.s[j].rows) work += groups(t.s[j]) * tiles(t.s[j]);
+    // Ranges of one length for all spans: the call's work in kPagedBlocks parts, so that long spans are cut however many short ones stand beside them
+    int64_t per = std::max((work + kPagedBlocks - 1) / kPagedBlocks, ((longest + tile - 1) / tile + kPagedRanges - 1) / kPagedRanges);
+    if (few && longest <= 512) per = std::max<int64_t>(per, 512 / tile);
+    per = std::max<int64_t>((per + step - 1) / step * step, 1);
+    int64_t part = 0;
+    for (int j = 0; j < t.n; ++j) {
+        Kv4Span &s = t.s[j];
+        s.blk0 = (int32_t)std::min<int64_t>(p.blocks, INT32_MAX);
+        s.per = (int32_t)per, s.splits = 1, s.part0 = (int32_t)part;
+        if (!s.rows) continue;
+        s.splits = (int32_t)((tiles(s) + per - 1) / per);
+        p.blocks += groups(s) * s.splits;
+        if (s.splits > 1) {
+            part += (int64_t)s.splits * s.rows * k.c.n_q_heads;
+            p.join = std::max(p.join, s.rows);
+        }
+    }
+    return p;
+}
+
+// More LDS than a kernel has without asking: allowed once per kernel and GPU
+template <class T, int D, int CAP>
+static hipError_t allow_chunk_lds() {
+    if (kChunkLds<D> <= 65536) return hipSuccess;
+    static std::atomic<uint64_t> allowed{0};  // a bit per GPU; those past 64 are asked every time
+    int gpu = 0;
+    hipError_t e = hipGetDevice(&gpu);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = gpu >= 0 && gpu < 64 ? 1ull << gpu : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_chunk<T, D, CAP>), hipFuncAttributeMaxDynamicSharedMemorySize, kChunkLds<D>);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
+template <class T, int D>
+static hipError_t attend_in(const Paged &k, int layer, const Kv4Table &t, const PagedAttendPlan &p, const uint64_t *sees, int words, const uint16_t *q,
+                            int64_t q_stride, uint16_t *out, int64_t out_stride) {
+    hipError_t e = hipSuccess;
+    with_table(t, [&](auto tab) {
+        constexpr int CAP = sizeof(tab.s) / sizeof(Kv4Span);
+        const dim3 grid(p.blocks);
+        const PagedView view = k.view(layer);
+        if (p.cols == 16)
+            hipLaunchKernelGGL((k_paged_few<T, D, 1, CAP>), grid, dim3(256), 0, k.stream, tab, view, sees, words, q, q_stride, out, out_stride, k.part_o, k.part_ml);
+        else if (p.cols == 32)
+            hipLaunchKernelGGL((k_paged_few<T, D, 2, CAP>), grid, dim3(256), 0, k.stream, tab, view, sees, words, q, q_stride, out, out_stride, k.part_o, k.part_ml);
+        else {
+            e = allow_chunk_lds<T, D, CAP>();
+            if (e != hipSuccess) return;
+            hipLaunchKernelGGL((k_paged_chunk<T, D, CAP>), grid, dim3(256), kChunkLds<D>, k.stream, tab, view, sees, words, q, q_stride, out, out_stride, k.part_o,
+                               k.part_ml);
+        }
+        if (p.join) {
+            // four waves a unit while there are fewer units than would fill the chip with one each
+            const int64_t units = (int64_t)p.join * k.c.n_q_heads;
+            const bool wide = units * t.n < 1024;
+            auto *kern = wide ? k_paged_join<T, D, 4, CAP> : k_paged_join<T, D, 1, CAP>;
+            hipLaunchKernelGGL(kern, dim3(wide ? units : (units + 3) / 4, t.n), dim3(256), 0, k.stream, tab, k.c.n_q_heads, k.part_o, k.part_ml, out, out_stride);
+        }
+        e = hipGetLastError();
+    });
+    return e;
+}
+
+int launch_paged_attend(const Paged &k, int layer, Kv4Table &t, const uint64_t *sees, int words, const uint16_t *q, int64_t q_stride, uint16_t *out,
+                        int64_t out_stride) {
+    const PagedAttendPlan p = plan_paged_attend(k, t, sees != nullptr);
+    // a launch has at most 2^32 - 1 threads a direction (asked before anything is launched)
+    if (p.blocks >= 1 << 24) return fail(ST_ERANGE, "%lld blocks of work, 2^24 or more", (long long)p.blocks);
+    const bool f16 = k.c.dtype == ST_F16;
+    const hipError_t e = k.c.head_dim == 128 ? (f16 ? attend_in<Fp16, 128>(k, layer, t, p, sees, words, q, q_stride, out, out_stride)
+                                                    : attend_in<Bf16, 128>(k, layer, t, p, sees, words, q, q_stride, out, out_stride))
+                                             : (f16 ? attend_in<Fp16, 64>(k, layer, t, p, sees, words, q, q_stride, out, out_stride)
+                                                    : attend_in<Bf16, 64>(k, layer, t, p, sees, words, q, q_stride, out, out_stride));
+    return launched("st_paged_attend", e);
+}
+
+}  // namespace st
