@@ -117,22 +117,32 @@ __global__ __launch_bounds__(256) void k_paged_keep(const Kv4Spans<CAP> t, Paged
     };
     int before = 0;
     for (int i0 = 0; i0 < n; i0 += kKeepBatch) {
-        u32x4 v[kKeepBatch];
-        int into[kKeepBatch], from[kKeepBatch];
+        // (all of a batch's numbers are asked for before any is looked at: rows past the end are read as the last, and their table entries as the first row's)
+        int r[kKeepBatch], from[kKeepBatch], into[kKeepBatch];
+#pragma unroll
+        for (int e = 0; e < kKeepBatch; ++e) r[e] = rows[min(i0 + e, n - 1)];
         bool whole = true;
 #pragma unroll
         for (int e = 0; e < kKeepBatch; ++e) {
-            const int r = i0 + e < n ? rows[i0 + e] : 0;
-            whole = whole && r > before && r < sp.rows;
-            before = whole ? r : before;
-            from[e] = whole ? page_of(pages, view.n_pages, (sp.len + r) >> view.shift) : -1;
-            into[e] = whole && r != i0 + e + 1 ? page_of(pages, view.n_pages, (sp.len + 1 + i0 + e) >> view.shift) : -1;
-            if (from[e] < 0) into[e] = -1;
-            if (into[e] >= 0) v[e] = *place(from[e], sp.len + r);
+            whole = whole && i0 + e < n && r[e] > before && r[e] < sp.rows;
+            before = whole ? r[e] : before;
+            r[e] = whole ? r[e] : 0;  // (0: nothing moves)
+        }
+#pragma unroll
+        for (int e = 0; e < kKeepBatch; ++e) {
+            from[e] = pages[(sp.len + r[e]) >> view.shift];
+            into[e] = pages[(sp.len + (r[e] ? 1 + i0 + e : 0)) >> view.shift];
+        }
+        u32x4 v[kKeepBatch];
+        bool moves[kKeepBatch];
+#pragma unroll
+        for (int e = 0; e < kKeepBatch; ++e) {
+            moves[e] = r[e] > 1 + i0 + e && (uint32_t)from[e] < (uint32_t)view.n_pages && (uint32_t)into[e] < (uint32_t)view.n_pages;
+            if (moves[e]) v[e] = *place(from[e], sp.len + r[e]);
         }
 #pragma unroll
         for (int e = 0; e < kKeepBatch; ++e)
-            if (into[e] >= 0) *place(into[e], sp.len + 1 + i0 + e) = v[e];
+            if (moves[e]) *place(into[e], sp.len + 1 + i0 + e) = v[e];
         if (!whole) return;
     }
 }

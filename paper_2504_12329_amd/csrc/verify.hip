@@ -5,14 +5,14 @@
 // (where p_k is positive, p_k - q = (p - (a_k + b_k) q) / b_k, and elsewhere both are cut), so that a failure costs one look at p and q and nothing is stored.  A draft
 // with token t stays if u q(t) b_k < max(p(t) - a_k q(t), 0).  Without draft logits p_k is p without the failed tokens and b_k what they leave of its sum.
 //
-// All of it is in 64 bits: a verdict compares two numbers, and the token that follows is looked for among 150000 sums that lie 1e-5 apart.  Vector instructions of 64 bits
-// run at the rate of plain 32-bit ones here, and the exponential is 15 of them.
+// All of it is in 64 bits: a verdict compares two numbers, and the token that follows is looked for among 150000 sums that lie 1e-5 apart.
 //
-//   k_verify_sums     largest logit and sum of exponentials of every part of every row            (the whole chip, all logits once)
-//   k_verify_left     b_k of the rows whose first k drafts have failed, k = 1 .. width - 1          (drafts with logits and trees only)
-//   k_verify_walk     the verdicts of all rows at once, then the walk through them; a block a sequence
-//   k_verify_weights  sums of the parts of the row that the next token is drawn from
-//   k_verify_pick     the part, and in it the token; a block a sequence
+//   k_verify_sums   largest logit and sum of exponentials of every part of every row          (the whole chip, all logits once)
+//   k_verify_rows   the verdict after every row, a wave each; with draft logits, of its first draft
+//   k_verify_left   b_k of the rows whose first k drafts have failed, k = 1 .. width - 1        (draft logits and trees only)
+//   k_verify_close  the verdicts that wait for them                                            (draft logits and trees only)
+//   k_verify_draw   the walk through the rows that stay, by every block alike, and the sum of one part of the row that the next token is drawn from
+//   k_verify_pick   the part, and in it the token; a block a sequence
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -22,9 +22,10 @@
 
 namespace st {
 
-constexpr int kVerifyPart = 8192;      // logits of a part
-constexpr int kVerifyRows = 1024;      // most rows of a sequence
-constexpr int kVerifyWidth = 64;       // most rows that follow one (a lane each)
+constexpr int kSumPart = 8192, kSumPartSmall = 2048;  // logits of a part of k_verify_sums
+constexpr int kDrawPart = 4096;                       // of k_verify_draw and k_verify_left
+constexpr int kVerifyRows = 1024;                     // most rows of a sequence
+constexpr int kVerifyWidth = 64;                      // most rows that follow one (a lane each)
 constexpr int kVerifySpans = ST_KV4_MAX_SPANS;
 
 // Sequences of a call, by value: no copy to the device precedes the kernels, and a captured launch keeps them
@@ -33,39 +34,51 @@ struct VerifySpans {
     int32_t first[kVerifySpans + 1];  // their first rows among the call's
     float heat[kVerifySpans];
 };
-// A part of a row: its largest logit, where it is, and the sum of exp((x - top) / T); NaN where some logit is, or (T > 0) is +infinity
+// A part of a row: its largest logit and where it is (greedy sequences), or the sum of 2^((x c - base) / 64), c = 64 / (T ln 2), base the whole number nearest to the largest
+// x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/64).  sum: NaN where some logit is, or (T > 0) is +infinity
 struct VerifyPart {
+    double base, sum;
     float top;
     int32_t at;
-    double sum;
 };
-// The row that a sequence's next token is drawn from
-struct VerifyEnd {
-    int32_t row;     // among the call's rows, -1: there is no token
-    int32_t failed;  // drafts after it that failed, their tokens (without draft logits)
-    double a;        // p's weights are max(p - a q, 0)
-    double p_top, p_sum, q_top, q_sum;
-    int32_t tokens[kVerifyWidth];
+// A row: its distribution p(x) = 2^((x c - p_base) / 64) / p_sum, q alike, and the verdict over the rows that follow it
+struct VerifyRow {
+    double p_base, p_sum, q_base, q_sum;
+    double a;        // p's weights are max(p - a q, 0) once all drafts have failed
+    int32_t stays;   // row of the sequence, -1: none, kOpen: not known yet
+    int32_t drafts;  // that follow it, of which as many as may be tried; without draft logits those that failed
+    int32_t best;    // greedy: the largest logit's token
+    int32_t good;    // it is a distribution
+};
+constexpr int kOpen = -2;
+// A draft after a row
+struct VerifyDraft {
+    double u, p, q;  // its random number, its probabilities
+    int32_t row, token;
 };
 struct VerifyArgs {
     const int32_t *parent, *tokens;
     const void *target, *draft;
     int64_t target_stride, draft_stride;
     const double *accept, *sample;
-    int32_t vocab, parts, rows, width;
-    VerifyPart *part;  // [target | draft][rows][parts]
-    double *left;      // [width - 1][rows][parts]
-    double *weight;    // [sequence][parts]
-    VerifyEnd *end;    // [sequence]
+    int32_t vocab, sum_parts, draw_parts, rows, width;
+    VerifyPart *part;     // [target | draft][rows][sum_parts]
+    VerifyRow *row;       // [rows]
+    VerifyDraft *drafts;  // [rows][width]
+    double *left;         // [width - 1][rows][draw_parts]
+    double *weight;       // [sequence][draw_parts]
+    int32_t *end;         // [sequence]: the row that the next token is drawn from, -1: none is drawn
     int32_t *path, *accepted, *next;
     int32_t path_stride;
 };
 struct Verify {
     st_verify_config c;
-    int32_t parts;
+    int32_t draw_parts;
     VerifyPart *part;
+    VerifyRow *row;
+    VerifyDraft *drafts;
     double *left, *weight;
-    VerifyEnd *end;
+    int32_t *end;
     hipStream_t stream;
 };
 
@@ -120,37 +133,107 @@ __device__ __forceinline__ double exp2_64(double t) {
     p = fma(p, x, 1.0);
     return ldexp(p, (int)n);
 }
-__device__ __forceinline__ double per_log2(float heat) { return 1.4426950408889634074 / (double)heat; }  // (x - top) / T as a power of 2
+__device__ __forceinline__ double units_of(float heat) { return 64 * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/64 of a power of 2
+__device__ __forceinline__ double power_of(float x, double c, double base) { return exp2_64(fma((double)x, c, -base) * (1.0 / 64)); }
+
+// The same for many numbers, off by less than 3e-14 (the table's own error), in nine instructions of 64 bits: powers of 2^(1/64) from a table in LDS times a fourth-degree
+// polynomial (the series of e^x, |x| <= r = ln 2 / 128, with x^5 replaced by 5/4 r^2 x^3 - 5/16 r^4 x, which it is nearest to), the exponent added to the number's upper half.  (A
+// sum of 1.5 * 2^52 and a number has the rounded number in its low bits.)
+struct Exp2Table {
+    const double *two;  // 2^(i / 64)
+    double c, base, shift;
+    __device__ __forceinline__ Exp2Table(const double *table, double units, double b) : two(table), c(units), base(b), shift(6755399441055744.0 - b) {}
+    // y and g with y * g = 2^((x c - base) / 64); x c - base is above -64000 and not above 1
+    __device__ __forceinline__ double power(float x, double &g) const {
+        constexpr double l = 0.69314718055994530942 / 64, r = l / 2;
+        const double v = (double)x, k = fma(v, c, shift), f = fma(v, c, -(k - shift));
+        const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, k);
+        double p = l * l * l * l / 24;
+        p = fma(p, f, l * l * l * (1.0 / 6 + r * r / 96));
+        p = fma(p, f, l * l / 2);
+        p = fma(p, f, l * (1 - r * r * r * r / 384));
+        g = fma(p, f, 1.0);
+        const uint2 half = reinterpret_cast<const uint2 *>(two)[n & 63];
+        const uint32_t upper = half.y + ((uint32_t)(n >> 6) << 20);
+        return __builtin_bit_cast(double, (uint64_t)upper << 32 | half.x);
+    }
+    __device__ __forceinline__ bool small(float x) const { return !(fma((double)x, c, -base) > -64000.0); }
+    __device__ __forceinline__ double any(float x) const { return small(x) ? 0.0 : power_of(x, c, base); }  // of any x; 0 below 2^-1000
+    __device__ __forceinline__ bool exact() const { return fabs(base) < 0x1p50; }  // (a larger base, of temperatures near 0, would not leave the table's sums exact)
+};
+constexpr int kTable = 64;
+__device__ __forceinline__ void fill_table(double *two) {  // followed by a barrier
+    if (threadIdx.x < kTable) two[threadIdx.x] = exp2_64((int)threadIdx.x / 64.0 - 1.0) * 2.0;
+}
+
+// Sums over a wave by lane moves without LDS (see wave_sum)
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double dpp_move64(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROW_MASK, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROW_MASK, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, kWave);
-    return v;
+    v += dpp_move64<0xB1, 0xf>(v);
+    v += dpp_move64<0x4E, 0xf>(v);
+    v += dpp_move64<0x141, 0xf>(v);
+    v += dpp_move64<0x140, 0xf>(v);
+    v += dpp_move64<0x142, 0xa>(v);
+    v += dpp_move64<0x143, 0xc>(v);
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = __builtin_amdgcn_readlane((int)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ double wave_max64(double v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = fmax(v, __shfl_xor(v, d, kWave));
     return v;
 }
+__device__ __forceinline__ double wave_prefix64(double v) {  // inclusive
+    v += dpp_move64<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8: within rows of 16
+    v += dpp_move64<0x112, 0xf>(v);
+    v += dpp_move64<0x114, 0xf>(v);
+    v += dpp_move64<0x118, 0xf>(v);
+    v += dpp_move64<0x142, 0xa>(v);  // the last lane of row 0 (2) to row 1 (3), of row 1 to rows 2 and 3
+    v += dpp_move64<0x143, 0xc>(v);
+    return v;
+}
+__device__ __forceinline__ double lane64(double v, int lane) {  // of a wave-uniform lane
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int wave_min_int(int v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d, kWave));
+    return v;
+}
+__device__ __forceinline__ double block_sum64(double v, double *sums) {  // 256 threads; sums: 4 numbers of LDS
+    v = wave_sum64(v);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
 __device__ __forceinline__ int span_of_row(const VerifySpans &t, int row) {
     const int lane = threadIdx.x & 63;
     return __builtin_amdgcn_readfirstlane(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < t.n && t.first[lane] <= row)) - 1);
 }
 
-// A part of a row of logits in registers: thread i has vectors i, i + 256, ... of 16 bytes.  Rows may start anywhere: parts are cut at multiples of 16 bytes of the
+// A part of a row of logits in the registers of 256 threads: vectors i, i + 256, ... of 16 bytes.  Rows may start anywhere: parts are cut at multiples of 16 bytes of the
 // address, and vectors that are not wholly in the row are read number by number.
-template <class L>
+template <class L, int PART>
 struct PartOf {
-    static constexpr int E = L::kPer16, N = kVerifyPart / E / 256;
+    static constexpr int E = L::kPer16, N = PART / E / 256;
     const typename L::type *p;
     int mis, x0, vocab;  // numbers between the last multiple of 16 bytes and the row; the part's first number (may lie before the row)
     __device__ __forceinline__ PartOf(const void *logits, int64_t stride, int row, int part, int v) {
         p = static_cast<const typename L::type *>(logits) + row * stride;
         mis = (int)(((uintptr_t)p & 15) / sizeof(typename L::type));
-        x0 = part * kVerifyPart - mis, vocab = v;
+        x0 = part * PART - mis, vocab = v;
     }
     __device__ __forceinline__ int first(int i) const { return x0 + (i * 256 + (int)threadIdx.x) * E; }
     __device__ __forceinline__ void load(float (&x)[N][E]) const {  // what is not in the row: -infinity
-        if (x0 >= 0 && x0 + kVerifyPart <= vocab) {
+        if (x0 >= 0 && x0 + PART <= vocab) {
             u32x4 w[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const u32x4 *>(p + first(i));
@@ -169,18 +252,6 @@ struct PartOf {
             }
         }
     }
-    // the same numbers of another row (the draft's): its rows may start elsewhere within 16 bytes
-    __device__ __forceinline__ void load_of(const void *logits, int64_t stride, int row, int part, float (&x)[N][E]) const {
-        const PartOf other(logits, stride, row, part, vocab);
-        if (other.mis == mis) return other.load(x);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int at = first(i) + e;
-                x[i][e] = at >= 0 && at < vocab ? L::get(other.p[at]) : -INFINITY;
-            }
-    }
 };
 
 // Whether a row follows another: lanes of a wave look together
@@ -198,386 +269,451 @@ __device__ __forceinline__ bool has_followers(const int32_t *parent, int first, 
 // Sums.  A block is one part of one row; the part stays in registers between its largest number and its sum.  Draft rows that nothing follows, and those of greedy
 // sequences, are not read.
 // ---------------------------------------------------------------------------------------
-template <class L>
-__global__ __launch_bounds__(256) void k_verify_sums(const VerifySpans t, const VerifyArgs a) {
+template <class L, int PART>
+__global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, const VerifyArgs a) {
     const bool is_draft = (int)blockIdx.y >= a.rows;
     const int row = blockIdx.y - (is_draft ? a.rows : 0), part = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
     const int j = span_of_row(t, row);
     const float heat = t.heat[j];
     if (is_draft && (heat == 0.f || !has_followers(a.parent, t.first[j], t.first[j + 1] - t.first[j], row - t.first[j]))) return;
-    typedef PartOf<L> P;
+    __shared__ float tops[4];
+    __shared__ double sums[4], two[kTable];
+    __shared__ int lowest[4];
+    typedef PartOf<L, PART> P;
     const P at = is_draft ? P(a.draft, a.draft_stride, row, part, a.vocab) : P(a.target, a.target_stride, row, part, a.vocab);
     float x[P::N][P::E];
     at.load(x);
+    fill_table(two);
     float top = -INFINITY;
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < P::N; ++i)
 #pragma unroll
         for (int e = 0; e < P::E; ++e) top = fmaxf(top, x[i][e]), nan |= x[i][e] != x[i][e];
-    __shared__ float tops[4];
-    __shared__ double sums[4];
-    __shared__ int lowest[4];
     top = wave_max(top);
     if ((tid & 63) == 0) tops[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     double sum = nan ? (double)NAN : 0.0;
     int low = INT32_MAX;
+    double base = -1e300;  // of a part without numbers
     if (heat > 0.f) {
-        const double c = per_log2(heat), base = top == -INFINITY ? 0.0 : (double)top;
+        const double c = units_of(heat);
+        if (top == INFINITY) {
+            sum = (double)NAN;
+        } else if (top > -INFINITY) {
+            base = rint((double)top * c);
+            const Exp2Table ex(two, c, base);
+            float low = top;
 #pragma unroll
-        for (int i = 0; i < P::N; ++i)
+            for (int i = 0; i < P::N; ++i)
 #pragma unroll
-            for (int e = 0; e < P::E; ++e) sum += exp2_64(((double)x[i][e] - base) * c);
-        if (top == INFINITY) sum = (double)NAN;
+                for (int e = 0; e < P::E; ++e) low = fminf(low, x[i][e]);
+            if (!ex.exact()) {
+                for (int i = 0; i < P::N; ++i)
+                    for (int e = 0; e < P::E; ++e) {
+                        const int n = at.first(i) + e;
+                        if (n >= 0 && n < a.vocab) sum += ex.any(L::get(at.p[n]));
+                    }
+            } else if (__builtin_amdgcn_ballot_w64(ex.small(low)) == 0) {
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) {
+                        double g;
+                        const double y = ex.power(x[i][e], g);
+                        sum = fma(y, g, sum);
+                    }
+            } else {  // some are masked, or not in the row
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) {
+                        double g;
+                        const bool none = ex.small(x[i][e]);
+                        const double y = ex.power(none ? top : x[i][e], g);
+                        sum = fma(y, none ? 0.0 : g, sum);
+                    }
+            }
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < P::N; ++i)
 #pragma unroll
             for (int e = 0; e < P::E; ++e)
                 if (x[i][e] == top) low = min(low, at.first(i) + e);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) low = min(low, __shfl_xor(low, d, kWave));
+        low = wave_min_int(low);
+        if ((tid & 63) == 0) lowest[wave] = low;
     }
-    sum = wave_sum64(sum);
-    if ((tid & 63) == 0) sums[wave] = sum, lowest[wave] = low;
-    __syncthreads();
+    sum = block_sum64(sum, sums);
     if (tid == 0)
-        a.part[(size_t)blockIdx.y * a.parts + part] =
-            VerifyPart{top, min(min(lowest[0], lowest[1]), min(lowest[2], lowest[3])), (sums[0] + sums[1]) + (sums[2] + sums[3])};
+        a.part[(size_t)blockIdx.y * a.sum_parts + part] =
+            VerifyPart{base, sum, top, heat > 0.f ? 0 : min(min(lowest[0], lowest[1]), min(lowest[2], lowest[3]))};
 }
 
-// A row from its parts, by one wave: largest logit, where, sum of exponentials below it
+// A row from its parts, by one wave
 struct RowSum {
-    double top, sum;
-    int at;
-    bool good;  // it is a distribution (heat 0: it has a largest number)
+    double base, sum;
+    int at;     // greedy: the largest number's token
+    bool good;  // it is a distribution (greedy: it has a largest number)
 };
 __device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int parts, float heat) {
     const int lane = threadIdx.x & 63;
-    float top = -INFINITY;
-    for (int i = lane; i < parts; i += 64) top = fmaxf(top, part[i].top);
-    top = wave_max(top);
-    const double c = heat > 0.f ? per_log2(heat) : 0.0;
+    constexpr VerifyPart none{-1e300, 0.0, -INFINITY, INT32_MAX};
+    const VerifyPart p0 = lane < parts ? part[lane] : none, p1 = lane + 64 < parts ? part[lane + 64] : none;
+    float top = fmaxf(p0.top, p1.top);
     double sum = 0.0;
-    int at = INT32_MAX;
-    for (int i = lane; i < parts; i += 64) {
-        const VerifyPart p = part[i];
-        if (p.top == top) at = min(at, p.at);
-        if (heat > 0.f) sum += p.top == -INFINITY ? p.sum : p.sum * exp2_64(((double)p.top - (double)top) * c);
-        else sum += p.sum;  // 0, or NaN
+    if (heat == 0.f) {
+        for (int i = lane + 128; i < parts; i += 64) top = fmaxf(top, part[i].top);
+        top = wave_max(top);
+        int at = INT32_MAX;
+        auto add = [&](const VerifyPart &p) {
+            if (p.top == top) at = min(at, p.at);
+            sum += p.sum;  // 0, or NaN
+        };
+        add(p0), add(p1);
+        for (int i = lane + 128; i < parts; i += 64) add(part[i]);
+        sum = wave_sum64(sum);
+        return RowSum{0.0, sum, wave_min_int(at), sum == sum && top > -INFINITY};
     }
+    double base = fmax(p0.base, p1.base);
+    for (int i = lane + 128; i < parts; i += 64) base = fmax(base, part[i].base);
+    base = wave_max64(base);
+    auto add = [&](const VerifyPart &p) { sum += p.sum * exp2_64((p.base - base) * (1.0 / 64)); };
+    add(p0), add(p1);
+    for (int i = lane + 128; i < parts; i += 64) add(part[i]);
     sum = wave_sum64(sum);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) at = min(at, __shfl_xor(at, d, kWave));
-    return RowSum{(double)top, sum, at, sum == sum && top > -INFINITY};
+    return RowSum{base, sum, 0, sum == sum && base > -1e299};
 }
 
-// The verdicts after one row, by one wave.  With draft logits only the first `known` drafts can be judged (b_1 .. b_known-1 have been summed).
-struct Verdict {
-    int stays;       // the row that stays (of the sequence), -1: none
-    int next;        // drafts judged; where it is `known`, there are more
-    bool more, good;
-    double a;
-    int failed, token;  // without draft logits: tokens that failed, lane i the i-th
-    RowSum p, q;
-};
+// ---------------------------------------------------------------------------------------
+// Rows.  A wave is one row: its distribution from the parts, the rows that follow it (a lane each, 64 rows at a time) with their tokens' probabilities, and the verdict -- with
+// draft logits, of the first of them.
+// ---------------------------------------------------------------------------------------
 template <class L>
-__device__ __forceinline__ Verdict judge(const VerifyArgs &a, int first, int rows, int local, float heat, int known) {
+__global__ __launch_bounds__(64) void k_verify_rows(const VerifySpans t, const VerifyArgs a) {
     typedef typename L::type X;
-    const int lane = threadIdx.x & 63, row = first + local;
-    Verdict v{-1, 0, false, true, 0.0, 0, -1, {}, {}};
-    v.p = row_sum(a.part + (size_t)row * a.parts, a.parts, heat);
-    v.good = v.p.good;
-    const bool with_q = a.draft && heat > 0.f;
+    const int row = blockIdx.x, lane = threadIdx.x, j = span_of_row(t, row);
+    const int first = t.first[j], rows = t.first[j + 1] - first, local = row - first;
+    const float heat = t.heat[j];
+    const bool draws = a.draft && heat > 0.f;
+    // the first 64 rows behind it, which is where what follows it mostly is: asked for beside the parts
     const X *pr = static_cast<const X *>(a.target) + row * a.target_stride, *qr = static_cast<const X *>(a.draft) + row * a.draft_stride;
-    const double c = heat > 0.f ? per_log2(heat) : 0.0;
-    bool have_q = false;
-    double b = 1.0, rest = v.p.sum;  // rest: what the failed tokens leave of the sum, without draft logits
-    for (int c0 = local + 1; c0 < rows; c0 += 64) {
+    struct Near {
+        int token;
+        double u;
+        float x, y;
+        uint64_t follow;
+    };
+    auto look = [&](int c0) {
         const int child = c0 + lane;
+        Near n{-1, 0.0, -INFINITY, -INFINITY, 0};
         const bool follows = child < rows && (a.parent ? a.parent[first + child] == local : child == local + 1);
-        uint64_t bits = __builtin_amdgcn_ballot_w64(follows);
-        if (!bits) {
+        n.follow = __builtin_amdgcn_ballot_w64(follows);
+        if (follows) {
+            n.token = a.tokens[first + child], n.u = a.accept[first + child];
+            if (n.token >= 0 && n.token < a.vocab) {
+                n.x = L::get(pr[n.token]);
+                if (draws) n.y = L::get(qr[n.token]);
+            }
+        }
+        return n;
+    };
+    Near near = look(local + 1);
+    const RowSum p = row_sum(a.part + (size_t)row * a.sum_parts, a.sum_parts, heat);
+    RowSum q{0.0, 1.0, 0, true};
+    const double c = heat > 0.f ? units_of(heat) : 0.0;
+    int stays = -1, drafts = 0, failed_token = -1;  // lane i: token of draft i that failed
+    bool good = p.good, have_q = false;
+    double rest = p.sum;  // what the failed tokens leave of the sum, without draft logits
+    for (int c0 = local + 1; c0 < rows && good && stays < 0 && drafts < a.width; c0 += 64) {
+        if (c0 != local + 1) near = look(c0);
+        if (!near.follow) {
             if (!a.parent) break;
             continue;
         }
-        if (with_q && !have_q) {
-            v.q = row_sum(a.part + (size_t)(a.rows + row) * a.parts, a.parts, heat);
-            v.good = v.good && v.q.good, have_q = true;
+        if (draws && !have_q) {
+            q = row_sum(a.part + (size_t)(a.rows + row) * a.sum_parts, a.sum_parts, heat);
+            good = q.good, have_q = true;
+            if (!good) break;
         }
-        if (!v.good) return v;
-        int t = -1;
-        double u = 0.0, pt = 0.0, qt = 0.0;
-        if (follows) {
-            t = a.tokens[first + child], u = a.accept[first + child];
-            if (t >= 0 && t < a.vocab) {
-                const double x = (double)L::get(pr[t]);
-                pt = heat > 0.f ? exp2_64((x - v.p.top) * c) : 0.0;
-                if (with_q) pt /= v.p.sum, qt = exp2_64(((double)L::get(qr[t]) - v.q.top) * c) / v.q.sum;
-            }
-        }
-        while (bits) {
-            const int l = __builtin_ctzll(bits);
-            bits &= bits - 1;
-            if (v.next >= a.width) return v;
-            if (v.next >= known) {
-                v.more = true;
-                return v;
-            }
-            if (with_q && v.next > 0) {  // the sum of what is left
-                const double *part = a.left + ((size_t)(v.next - 1) * a.rows + row) * a.parts;
-                b = 0.0;
-                for (int i = lane; i < a.parts; i += 64) b += part[i];
-                b = wave_sum64(b);
-            }
-            ++v.next;
-            const int token = __shfl(t, l, kWave);
-            const double ul = __shfl(u, l, kWave), pl = __shfl(pt, l, kWave), ql = __shfl(qt, l, kWave);
-            bool stays;
-            if (token < 0 || token >= a.vocab) {
-                stays = false;
-            } else if (heat == 0.f) {
-                stays = token == v.p.at;
-            } else if (with_q) {
-                stays = ul * ql * b < fmax(pl - v.a * ql, 0.0);
+        const bool known = near.token >= 0 && near.token < a.vocab;
+        double pt = known && heat > 0.f ? power_of(near.x, c, p.base) : 0.0;
+        const double qt = known && draws ? power_of(near.y, c, q.base) / q.sum : 0.0;
+        if (draws) pt /= p.sum;
+        for (uint64_t bits = near.follow; bits && drafts < a.width && stays < 0; bits &= bits - 1) {
+            const int l = __builtin_ctzll(bits), token = __builtin_amdgcn_readlane(near.token, l);
+            const bool in = token >= 0 && token < a.vocab;
+            if (heat == 0.f) {
+                if (in && token == p.at) stays = c0 + l;
+            } else if (draws) {
+                if (drafts == 0 && in && lane64(near.u, l) * lane64(qt, l) < lane64(pt, l)) stays = c0 + l;
+                if (a.width > 1 && lane == l) a.drafts[(size_t)row * a.width + drafts] = VerifyDraft{near.u, pt, qt, c0 + l, near.token};
             } else {
-                const bool again = __builtin_amdgcn_ballot_w64(lane < v.failed && v.token == token) != 0;
-                stays = !again && ul * rest < pl;
-                if (!stays && !again) rest -= pl;
-                if (!stays && lane == v.failed) v.token = token;
-                v.failed += !stays;
+                const bool again = __builtin_amdgcn_ballot_w64(lane < drafts && failed_token == token) != 0;
+                const double pl = lane64(pt, l);
+                if (in && !again && lane64(near.u, l) * rest < pl) {
+                    stays = c0 + l;
+                } else {
+                    if (lane == drafts) failed_token = token;
+                    if (in && !again) rest -= pl;
+                    if (rest < p.sum * 0x1p-10) {  // little is left of a difference: summed up instead (once in a thousand failures)
+                        rest = 0.0;
+                        for (int x = lane; x < a.vocab; x += 64) {
+                            bool out = false;
+                            for (int f = 0; f <= drafts; ++f) out |= __builtin_amdgcn_readlane(failed_token, f) == x;
+                            if (!out) rest += power_of(L::get(pr[x]), c, p.base);
+                        }
+                        rest = wave_sum64(rest);
+                    }
+                }
             }
-            if (stays) {
-                v.stays = c0 + l;
-                return v;
-            }
-            if (with_q) v.a += b;
+            drafts += stays < 0 || draws;
         }
     }
-    return v;
+    if (!draws && heat > 0.f && lane < drafts) a.drafts[(size_t)row * a.width + lane].token = failed_token;
+    if (lane == 0) {
+        VerifyRow r;
+        r.p_base = p.base, r.p_sum = p.sum, r.q_base = q.base, r.q_sum = q.sum;
+        r.a = draws && drafts > 0 && stays < 0 ? 1.0 : 0.0;
+        r.stays = stays < 0 && good && draws && drafts > 1 ? kOpen : stays;
+        r.drafts = drafts, r.best = p.at, r.good = good;
+        a.row[row] = r;
+    }
 }
+
+// The verdict over drafts 1 .. known - 1 of an open row, whose b_k have been summed; by one wave.  a: as they leave it
+__device__ __forceinline__ int judge_on(const VerifyArgs &args, int row, int known, double &a) {
+    const int lane = threadIdx.x & 63;
+    for (int k = 1; k < known; ++k) {
+        const VerifyDraft d = args.drafts[(size_t)row * args.width + k];
+        const double *part = args.left + ((size_t)(k - 1) * args.rows + row) * args.draw_parts;
+        double b = 0.0;
+        for (int i = lane; i < args.draw_parts; i += 64) b += part[i];
+        b = wave_sum64(b);
+        if (d.token >= 0 && d.token < args.vocab && d.u * d.q * b < fmax(d.p - a * d.q, 0.0)) return d.row;
+        a += b;
+    }
+    return -1;
+}
+
+// The weights of a row: p, or p without tokens that have failed, or max(p - a q, 0); parts of kDrawPart of them, kOwn neighbouring ones to each of 256 threads
+constexpr int kOwn = kDrawPart / 256;
+template <class L>
+struct Weights {
+    typedef typename L::type X;
+    const X *p, *q;
+    const double *two;
+    double c, p_base, p_of, q_base, q_of;  // q_of 0: without q
+    const VerifyDraft *failed;
+    int n_failed, vocab;
+    __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const double *table, float heat, double by, bool plain) {
+        p = static_cast<const X *>(a.target) + row * a.target_stride, q = static_cast<const X *>(a.draft) + row * a.draft_stride;
+        two = table, c = units_of(heat), p_base = r.p_base, p_of = 1.0 / r.p_sum, q_base = r.q_base, q_of = plain ? 0.0 : by / r.q_sum;
+        failed = a.drafts + (size_t)row * a.width, n_failed = plain || a.draft ? 0 : r.drafts, vocab = a.vocab;
+    }
+    __device__ __forceinline__ int first(int part) const { return part * kDrawPart + (int)threadIdx.x * kOwn; }  // of this thread
+    __device__ __forceinline__ double one(int x) const {  // of any token
+        if (x >= vocab) return 0.0;
+        for (int f = 0; f < n_failed; ++f)
+            if (failed[f].token == x) return 0.0;
+        double w = Exp2Table(two, c, p_base).any(L::get(p[x])) * p_of;
+        if (q_of > 0.0) w = fmax(w - Exp2Table(two, c, q_base).any(L::get(q[x])) * q_of, 0.0);
+        return w;
+    }
+    static constexpr int E = L::kPer16, N = kOwn / E;
+    static __device__ __forceinline__ void load(const X *at, float (&x)[N][E]) {
+        if ((uintptr_t)at & 15) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[i][e] = L::get(at[i * E + e]);
+        } else {
+            u32x4 v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const u32x4 *>(at + i * E);
+#pragma unroll
+            for (int i = 0; i < N; ++i) L::spread(v[i], x[i]);
+        }
+    }
+    // the sum of this thread's
+    __device__ __forceinline__ double own(int part) const {
+        const int x0 = first(part);
+        const Exp2Table ep(two, c, p_base), eq(two, c, q_base);
+        bool plain = x0 + kOwn <= vocab && ep.exact() && eq.exact();
+        for (int f = 0; f < n_failed; ++f) plain &= failed[f].token < x0 || failed[f].token >= x0 + kOwn;
+        double sum = 0.0;
+        if (plain) {
+            float x[N][E], y[N][E], low = INFINITY, low_q = INFINITY;
+            load(p + x0, x);
+            if (q_of > 0.0) load(q + x0, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) low = fminf(low, x[i][e]), low_q = q_of > 0.0 ? fminf(low_q, y[i][e]) : 0.f;
+            plain = !ep.small(low) && !(q_of > 0.0 && eq.small(low_q));
+            if (plain && q_of > 0.0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        double g, h;
+                        const double u = ep.power(x[i][e], g), z = eq.power(y[i][e], h);
+                        sum += fmax(u * g * p_of - z * h * q_of, 0.0);
+                    }
+            } else if (plain) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        double g;
+                        const double u = ep.power(x[i][e], g);
+                        sum = fma(u * p_of, g, sum);
+                    }
+            }
+        }
+        if (!plain)
+            for (int i = 0; i < kOwn; ++i) sum += one(x0 + i);
+        return sum;
+    }
+};
 
 // ---------------------------------------------------------------------------------------
 // Left: b_k of one part of one row.  Rows whose verdict is known, or that have no more drafts, return.
 // ---------------------------------------------------------------------------------------
 template <class L>
 __global__ __launch_bounds__(256) void k_verify_left(const VerifySpans t, const VerifyArgs a, int k) {
-    const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, j = span_of_row(t, row);
-    const float heat = t.heat[j];
-    if (heat == 0.f) return;
-    const int first = t.first[j], rows = t.first[j + 1] - first;
-    if (!has_followers(a.parent, first, rows, row - first)) return;
-    const Verdict v = judge<L>(a, first, rows, row - first, heat, k);  // (every wave on its own, with the same result)
-    if (!v.more) return;
-    typedef PartOf<L> P;
-    const P at(a.target, a.target_stride, row, part, a.vocab);
-    const double c = per_log2(heat), p_of = 1.0 / v.p.sum, q_of = v.a / v.q.sum;
-    double sum = 0.0;
-    float x[P::N][P::E], y[P::N][P::E];
-    at.load(x);
-    at.load_of(a.draft, a.draft_stride, row, part, y);
-#pragma unroll
-    for (int i = 0; i < P::N; ++i)
-#pragma unroll
-        for (int e = 0; e < P::E; ++e)
-            sum += fmax(exp2_64(((double)x[i][e] - v.p.top) * c) * p_of - exp2_64(((double)y[i][e] - v.q.top) * c) * q_of, 0.0);
-    __shared__ double sums[4];
-    sum = wave_sum64(sum);
-    if ((tid & 63) == 0) sums[tid >> 6] = sum;
+    const int row = blockIdx.y, part = blockIdx.x;
+    const VerifyRow r = a.row[row];
+    if (r.stays != kOpen || r.drafts <= k) return;
+    __shared__ double sums[4], two[kTable];
+    fill_table(two);
+    double by = r.a;
+    if (judge_on(a, row, k, by) >= 0) return;  // (every wave on its own, with the same result)
     __syncthreads();
-    if (tid == 0) a.left[((size_t)(k - 1) * a.rows + row) * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    const double sum = block_sum64(Weights<L>(a, row, r, two, t.heat[span_of_row(t, row)], by, false).own(part), sums);
+    if (threadIdx.x == 0) a.left[((size_t)(k - 1) * a.rows + row) * a.draw_parts + part] = sum;
+}
+
+__global__ __launch_bounds__(64) void k_verify_close(const VerifyArgs a) {
+    VerifyRow &r = a.row[blockIdx.x];
+    if (r.stays != kOpen) return;
+    double by = r.a;
+    const int stays = judge_on(a, blockIdx.x, r.drafts, by);
+    if (threadIdx.x == 0) r.stays = stays, r.a = by;
 }
 
 // ---------------------------------------------------------------------------------------
-// Walk: a wave judges every sixteenth row of a sequence, then one thread follows the rows that stay.
+// Draw.  Every block of a sequence walks through the rows that stay (one load, then steps in LDS), and sums up one part of the weights at the end of the walk; the first
+// one writes the path.
 // ---------------------------------------------------------------------------------------
 template <class L>
-__global__ __launch_bounds__(1024) void k_verify_walk(const VerifySpans t, const VerifyArgs a) {
-    const int j = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+__global__ __launch_bounds__(256) void k_verify_draw(const VerifySpans t, const VerifyArgs a) {
+    const int j = blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
     const int first = t.first[j], rows = t.first[j + 1] - first;
-    const float heat = t.heat[j];
-    __shared__ int stays[kVerifyRows];
-    __shared__ int end, count;
-    for (int r = wave; r < rows; r += 16) {
-        const Verdict v = judge<L>(a, first, rows, r, heat, kVerifyWidth);
-        if (lane == 0) stays[r] = v.stays;
-    }
+    __shared__ int stays[kVerifyRows], path[kVerifyRows];
+    __shared__ int end_of, count_of;
+    __shared__ double sums[4], two[kTable];
+    for (int i = tid; i < rows; i += 256) stays[i] = a.row[first + i].stays;
+    fill_table(two);
     __syncthreads();
-    int32_t *path = a.path + (int64_t)j * a.path_stride;
     if (tid == 0) {
         int at = 0, n = 0;
-        while (stays[at] >= 0) at = stays[at], path[n++] = at;  // (a row that stays lies behind the row it follows)
-        end = at, count = n;
-        a.accepted[j] = n;
+        for (int next = stays[0]; next >= 0; next = stays[at]) path[n++] = at = next;  // (a row that stays lies behind the row it follows)
+        end_of = at, count_of = n;
     }
     __syncthreads();
-    for (int i = count + tid; i < a.path_stride; i += 1024) path[i] = -1;
-    if (wave) return;
-    const Verdict v = judge<L>(a, first, rows, end, heat, kVerifyWidth);  // once more for what it leaves
-    if (heat == 0.f || !v.good) {
-        if (lane == 0) a.end[j].row = -1, a.next[j] = v.good ? v.p.at : -1;
-        return;
+    const int end = first + end_of, count = count_of;
+    const VerifyRow r = a.row[end];
+    const float heat = t.heat[j];
+    const bool drawn = heat > 0.f && r.good;
+    if (part == 0) {
+        for (int i = tid; i < a.path_stride; i += 256) a.path[(int64_t)j * a.path_stride + i] = i < count ? path[i] : -1;
+        if (tid == 0) {
+            a.accepted[j] = count, a.end[j] = drawn ? end : -1;
+            if (!drawn) a.next[j] = r.good ? r.best : -1;
+        }
     }
-    a.end[j].tokens[lane] = v.token;
-    if (lane == 0) {
-        VerifyEnd &e = a.end[j];
-        e.row = first + end, e.failed = v.failed, e.a = v.a;
-        e.p_top = v.p.top, e.p_sum = v.p.sum, e.q_top = v.q.top, e.q_sum = v.q.sum;
-    }
-}
-
-// The weights of one part of a sequence's last row, from which its next token is drawn.  plain: p itself, whatever failed.
-template <class L>
-__device__ __forceinline__ void end_weights(const VerifyArgs &a, const VerifyEnd &e, float heat, bool plain, const PartOf<L> &at, int part,
-                                            double (&w)[PartOf<L>::N][PartOf<L>::E]) {
-    typedef PartOf<L> P;
-    const double c = per_log2(heat), p_top = e.p_top, p_of = 1.0 / e.p_sum;
-    float x[P::N][P::E];
-    at.load(x);
-    for (int f = 0; f < e.failed && !plain; ++f) {
-        const int token = e.tokens[f];
-        if (token < at.x0 || token >= at.x0 + kVerifyPart) continue;
-#pragma unroll
-        for (int i = 0; i < P::N; ++i)
-#pragma unroll
-            for (int k = 0; k < P::E; ++k)
-                if (at.first(i) + k == token) x[i][k] = -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < P::N; ++i)
-#pragma unroll
-        for (int k = 0; k < P::E; ++k) w[i][k] = exp2_64(((double)x[i][k] - p_top) * c) * p_of;
-    if (plain || !(e.a > 0.0)) return;
-    const double q_top = e.q_top, q_of = e.a / e.q_sum;
-    at.load_of(a.draft, a.draft_stride, e.row, part, x);
-#pragma unroll
-    for (int i = 0; i < P::N; ++i)
-#pragma unroll
-        for (int k = 0; k < P::E; ++k) w[i][k] = fmax(w[i][k] - exp2_64(((double)x[i][k] - q_top) * c) * q_of, 0.0);
+    if (!drawn) return;
+    const double sum = block_sum64(Weights<L>(a, end, r, two, heat, r.a, false).own(part), sums);
+    if (tid == 0) a.weight[(size_t)j * a.draw_parts + part] = sum;
 }
 
 // ---------------------------------------------------------------------------------------
-// Weights: the sum of one part
+// Pick: the first token at which the running sum of the weights passes sample * their sum.  The part first, by every wave alike; in it a thread has neighbouring
+// tokens, so that the sums run from thread to thread; and of the thread that passes, its tokens, a lane each.  Where rounding lets none pass, the last with a weight.
 // ---------------------------------------------------------------------------------------
-template <class L>
-__global__ __launch_bounds__(256) void k_verify_weights(const VerifySpans t, const VerifyArgs a) {
-    typedef PartOf<L> P;
-    const int j = blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
-    const VerifyEnd &e = a.end[j];
-    if (e.row < 0) return;
-    const P at(a.target, a.target_stride, e.row, part, a.vocab);
-    double w[P::N][P::E], sum = 0.0;
-    end_weights<L>(a, e, t.heat[j], false, at, part, w);
-#pragma unroll
-    for (int i = 0; i < P::N; ++i)
-#pragma unroll
-        for (int k = 0; k < P::E; ++k) sum += w[i][k];
-    __shared__ double sums[4];
-    sum = wave_sum64(sum);
-    if ((tid & 63) == 0) sums[tid >> 6] = sum;
-    __syncthreads();
-    if (tid == 0) a.weight[(size_t)j * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-}
-
-// ---------------------------------------------------------------------------------------
-// Pick: the first token at which the running sum of the weights passes sample * their sum.  Parts first, by every wave alike; in the part the sums of 64 vectors
-// (a wave's share of one load), and of those the one that passes, number by number.  Where rounding lets none pass, the last token with a weight.
-// ---------------------------------------------------------------------------------------
-__device__ __forceinline__ double wave_prefix64(double v) {  // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double x = __shfl_up(v, d, kWave);
-        if (lane >= d) v += x;
-    }
-    return v;
+// The first of 64 lanes at which the running sum of v passes the goal, or the last with a v; -1: there is none.  before: in the sum before the lanes, out before that one
+__device__ __forceinline__ int passing_lane(double v, double goal, double &before, bool &passes) {
+    const double sum = before + wave_prefix64(v);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(v > 0.0), over = __builtin_amdgcn_ballot_w64(sum > goal && v > 0.0);
+    passes = over != 0;
+    const int l = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : -1;
+    before = lane64(sum - v, l < 0 ? 63 : l);
+    return l;
 }
 
 template <class L>
 __global__ __launch_bounds__(256) void k_verify_pick(const VerifySpans t, const VerifyArgs a) {
-    typedef PartOf<L> P;
-    const int j = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const VerifyEnd &e = a.end[j];
-    if (e.row < 0) return;
-    const float heat = t.heat[j];
-    const double c = per_log2(heat);
+    const int j = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, end = a.end[j];
+    if (end < 0) return;
+    double *weights = a.weight + (size_t)j * a.draw_parts;
+    __shared__ double sums[4], two[kTable], before_of;
+    __shared__ int thread_of[4];
+    fill_table(two);
+    __syncthreads();
+    const VerifyRow r = a.row[end];
     double total = 0.0;
-    for (int i = lane; i < a.parts; i += 64) total += a.weight[(size_t)j * a.parts + i];
+    for (int i = lane; i < a.draw_parts; i += 64) total += weights[i];
     total = wave_sum64(total);
-    const bool plain = !(total > 0.0);  // rounding has left nothing: p itself
-    auto part_weight = [&](int i) {
-        if (i >= a.parts) return 0.0;
-        if (!plain) return a.weight[(size_t)j * a.parts + i];
-        const VerifyPart p = a.part[(size_t)e.row * a.parts + i];
-        return p.top == -INFINITY ? 0.0 : p.sum * exp2_64(((double)p.top - e.p_top) * c) / e.p_sum;
-    };
+    const bool plain = !(total > 0.0);  // rounding has left nothing: p itself (rare)
+    const Weights<L> w(a, end, r, two, t.heat[j], r.a, plain);
     if (plain) {
-        total = 0.0;
-        for (int i = lane; i < a.parts; i += 64) total += part_weight(i);
-        total = wave_sum64(total);
+        for (int i = 0; i < a.draw_parts; ++i) {
+            const double s = block_sum64(w.own(i), sums);
+            if (tid == 0) __hip_atomic_store(weights + i, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            total += s;
+            __syncthreads();
+        }
     }
-    double goal = a.sample[j] * total, before = 0.0;
-    int part = -1, full = -1;  // the part that passes the goal; the last one with a weight, and the sum before it
-    double before_full = 0.0;
-    for (int i0 = 0; i0 < a.parts && part < 0; i0 += 64) {
-        const double v = part_weight(i0 + lane), sum = before + wave_prefix64(v);
-        const uint64_t passes = __builtin_amdgcn_ballot_w64(sum > goal && v > 0.0), some = __builtin_amdgcn_ballot_w64(v > 0.0);
-        const int l = passes ? __builtin_ctzll(passes) : some ? 63 - __builtin_clzll(some) : 0;
-        const double at_l = __shfl(sum - v, l, kWave);
-        if (passes) part = i0 + l, before_full = at_l;
-        else if (some) full = i0 + l, before_full = at_l;
-        before = __shfl(sum, 63, kWave);
+    auto weight = [&](int i) {
+        if (i >= a.draw_parts) return 0.0;
+        return plain ? __hip_atomic_load(weights + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : weights[i];
+    };
+    const double goal = a.sample[j] * total;
+    double before = 0.0, before_it = 0.0;
+    int part = -1;  // the part that passes the goal, or the last one with a weight; and the sum before it
+    bool passes = false;
+    for (int i0 = 0; i0 < a.draw_parts && !passes; i0 += 64) {
+        const double v = weight(i0 + lane), all = before + wave_sum64(v);
+        const int l = passing_lane(v, goal, before, passes);
+        if (l >= 0) part = i0 + l, before_it = before;
+        before = all;
     }
-    if (part < 0) part = full;
     if (part < 0) {  // no weight anywhere: not a distribution after all
         if (tid == 0) a.next[j] = -1;
         return;
     }
-    goal -= before_full;
-    const P at(a.target, a.target_stride, e.row, part, a.vocab);
-    double w[P::N][P::E], own[P::N];
-    end_weights<L>(a, e, heat, plain, at, part, w);
-    __shared__ double sums[P::N][4];
-    __shared__ int chosen[4], final_one[4];
-#pragma unroll
-    for (int i = 0; i < P::N; ++i) {
-        own[i] = 0.0;
-#pragma unroll
-        for (int k = 0; k < P::E; ++k) own[i] += w[i][k];
-        const double s = wave_sum64(own[i]);
-        if (lane == 0) sums[i][wave] = s;
-    }
+    const double own = w.own(part), wave_all = wave_sum64(own);
     __syncthreads();
-    double run = 0.0;
-    int first = INT32_MAX, latest = -1;
-#pragma unroll
-    for (int i = 0; i < P::N; ++i)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const double s = sums[i][v];
-            if (v == wave && s > 0.0) {
-                double x = run + (wave_prefix64(own[i]) - own[i]);
-#pragma unroll
-                for (int k = 0; k < P::E; ++k) {
-                    x += w[i][k];
-                    if (w[i][k] > 0.0) {
-                        latest = max(latest, at.first(i) + k);
-                        if (x > goal) first = min(first, at.first(i) + k);
-                    }
-                }
-            }
-            run += s;
-        }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) first = min(first, __shfl_xor(first, d, kWave)), latest = max(latest, __shfl_xor(latest, d, kWave));
-    if (lane == 0) chosen[wave] = first, final_one[wave] = latest;
+    if (lane == 0) sums[wave] = wave_all;
     __syncthreads();
-    if (tid) return;
-    first = min(min(chosen[0], chosen[1]), min(chosen[2], chosen[3]));
-    latest = max(max(final_one[0], final_one[1]), max(final_one[2], final_one[3]));
-    a.next[j] = first != INT32_MAX ? first : latest;
+    before = before_it;
+    for (int v = 0; v < wave; ++v) before += sums[v];
+    const int l = passing_lane(own, goal, before, passes);
+    if (lane == 0) thread_of[wave] = l < 0 ? -1 : (passes ? 256 : 0) + wave * 64 + l;  // (256 on: it passes)
+    __syncthreads();
+    int best = -1;
+    for (int v = 3; v >= 0; --v)  // the first wave that passes, else the last one with a weight
+        if (thread_of[v] >= 256 || (best < 0 && thread_of[v] >= 0)) best = thread_of[v];
+    if (best < 0) best = 0;
+    if ((best & 255) == tid) before_of = lane64(before, 0);
+    __syncthreads();
+    if (wave) return;
+    before = before_of;
+    const int first = part * kDrawPart + (best & 255) * kOwn;
+    const int at = passing_lane(lane < kOwn ? w.one(first + lane) : 0.0, goal, before, passes);
+    if (lane == 0) a.next[j] = first + (at < 0 ? 0 : at);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -591,6 +727,9 @@ static int check_config(const st_verify_config *c) {
     if (c->max_width <= 0 || c->max_width > kVerifyWidth) return fail(ST_EINVAL, "max_width must be from 1 to %d", kVerifyWidth);
     return ST_OK;
 }
+// (a row's first part may start up to 7 numbers before it)
+static int parts_of(int vocab, int part) { return (vocab + 7 + part - 1) / part; }
+
 static void carve(const st_verify_config &c, char *ws, Verify *v, size_t *bytes) {
     size_t off = 0;
     auto take = [&](size_t n) {
@@ -599,24 +738,33 @@ static void carve(const st_verify_config &c, char *ws, Verify *v, size_t *bytes)
         return p;
     };
     v->c = c;
-    v->parts = (c.vocab + 7 + kVerifyPart - 1) / kVerifyPart;  // (a row's first part may start up to 7 numbers before it)
-    const size_t row = (size_t)c.max_rows * v->parts;
-    v->part = reinterpret_cast<VerifyPart *>(take(sizeof(VerifyPart) * 2 * row));
-    v->left = reinterpret_cast<double *>(take(sizeof(double) * (c.max_width - 1) * row));
-    v->weight = reinterpret_cast<double *>(take(sizeof(double) * kVerifySpans * v->parts));
-    v->end = reinterpret_cast<VerifyEnd *>(take(sizeof(VerifyEnd) * kVerifySpans));
+    v->draw_parts = (c.vocab + kDrawPart - 1) / kDrawPart;
+    const size_t rows = c.max_rows;
+    v->part = reinterpret_cast<VerifyPart *>(take(sizeof(VerifyPart) * 2 * rows * parts_of(c.vocab, kSumPartSmall)));
+    v->row = reinterpret_cast<VerifyRow *>(take(sizeof(VerifyRow) * rows));
+    v->drafts = reinterpret_cast<VerifyDraft *>(take(sizeof(VerifyDraft) * rows * c.max_width));
+    v->left = reinterpret_cast<double *>(take(sizeof(double) * (c.max_width - 1) * rows * v->draw_parts));
+    v->weight = reinterpret_cast<double *>(take(sizeof(double) * kVerifySpans * v->draw_parts));
+    v->end = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * kVerifySpans));
     *bytes = off;
 }
 
 template <class L>
-static void launch_verify(const Verify &v, const VerifySpans &t, const VerifyArgs &a, bool all_greedy) {
-    const bool draft = a.draft && !all_greedy;
-    hipLaunchKernelGGL(k_verify_sums<L>, dim3(a.parts, draft ? 2 * a.rows : a.rows), dim3(256), 0, v.stream, t, a);
-    for (int k = 1; draft && k < a.width; ++k) hipLaunchKernelGGL(k_verify_left<L>, dim3(a.parts, a.rows), dim3(256), 0, v.stream, t, a, k);
-    hipLaunchKernelGGL(k_verify_walk<L>, dim3(t.n), dim3(1024), 0, v.stream, t, a);
-    if (all_greedy) return;
-    hipLaunchKernelGGL(k_verify_weights<L>, dim3(a.parts, t.n), dim3(256), 0, v.stream, t, a);
-    hipLaunchKernelGGL(k_verify_pick<L>, dim3(t.n), dim3(256), 0, v.stream, t, a);
+static void launch_verify(const Verify &v, const VerifySpans &t, VerifyArgs a, bool all_greedy) {
+    const bool draws = a.draft && !all_greedy;
+    const int planes = draws ? 2 * a.rows : a.rows, large = parts_of(a.vocab, kSumPart);
+    // Smaller parts while larger ones would leave compute units without a block
+    const bool small = (int64_t)planes * large < 1024;
+    a.sum_parts = small ? parts_of(a.vocab, kSumPartSmall) : large;
+    auto *sums = small ? k_verify_sums<L, kSumPartSmall> : k_verify_sums<L, kSumPart>;
+    hipLaunchKernelGGL(sums, dim3(a.sum_parts, planes), dim3(256), 0, v.stream, t, a);
+    hipLaunchKernelGGL(k_verify_rows<L>, dim3(a.rows), dim3(64), 0, v.stream, t, a);
+    if (draws && a.width > 1) {
+        for (int k = 1; k < a.width; ++k) hipLaunchKernelGGL(k_verify_left<L>, dim3(a.draw_parts, a.rows), dim3(256), 0, v.stream, t, a, k);
+        hipLaunchKernelGGL(k_verify_close, dim3(a.rows), dim3(64), 0, v.stream, a);
+    }
+    hipLaunchKernelGGL(k_verify_draw<L>, dim3(all_greedy ? 1 : a.draw_parts, t.n), dim3(256), 0, v.stream, t, a);
+    if (!all_greedy) hipLaunchKernelGGL(k_verify_pick<L>, dim3(t.n), dim3(256), 0, v.stream, t, a);
 }
 
 }  // namespace st
@@ -688,8 +836,8 @@ int st_verify_drafts(st_verify *h, const int32_t *rows, int32_t n, const st_draf
     if (((uintptr_t)accept | (uintptr_t)sample) & 7) return fail(ST_EINVAL, "accept or sample is not aligned to 8 bytes");
     if (((uintptr_t)target | (uintptr_t)draft) & (size - 1)) return fail(ST_EINVAL, "target or draft is not aligned to its numbers");
     if (target_stride < v->c.vocab || (draft && draft_stride < v->c.vocab)) return fail(ST_EINVAL, "a row stride is less than vocab %d", v->c.vocab);
-    const VerifyArgs a{tree ? tree->parent : nullptr, tokens, target, draft, target_stride, draft_stride, accept, sample, v->c.vocab, v->parts, (int32_t)total,
-                       tree ? tree->width : 1, v->part, v->left, v->weight, v->end, path, accepted, next, path_stride};
+    const VerifyArgs a{tree ? tree->parent : nullptr, tokens, target, draft, target_stride, draft_stride, accept, sample, v->c.vocab, 0, v->draw_parts,
+                       (int32_t)total, tree ? tree->width : 1, v->part, v->row, v->drafts, v->left, v->weight, v->end, path, accepted, next, path_stride};
     if (v->c.dtype == ST_F32) launch_verify<LogitF32>(*v, t, a, all_greedy);
     else if (v->c.dtype == ST_BF16) launch_verify<LogitBf16>(*v, t, a, all_greedy);
     else launch_verify<LogitF16>(*v, t, a, all_greedy);
