@@ -792,9 +792,9 @@ class DraftSpans(Kv4Spans):
             at += len(ps)
         if width > 64:
             raise StError(ST_ERANGE, f"{width} rows follow one row, at most 64 are supported")
-        bits = torch.from_numpy(np.concatenate([sees.reshape(-1).view(np.int64), np.concatenate([parent, depth]).view(np.int64)])).to(device)
-        cut = self.rows * words
-        self._take(bits[cut:].view(torch.int32)[:self.rows], bits[cut:].view(torch.int32)[self.rows:], bits[:cut].view(self.rows, words), width)
+        n = self.rows
+        bits = torch.from_numpy(np.concatenate([sees.reshape(-1).view(np.int32), parent, depth])).to(device)     # (one copy)
+        self._take(bits[2 * n * words:2 * n * words + n], bits[2 * n * words + n:], bits[:2 * n * words].view(torch.int64).view(n, words) if n else bits.new_empty((0, words), dtype=torch.int64), width)
 
     @classmethod
     def of_tensors(cls, spans, parent=None, depth=None, sees=None, width=1):

@@ -676,11 +676,15 @@ PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree) {
     int64_t want = kPagedBlocks, per = parts_of(want);
     if (!few && per < 8) want = kPagedBlocks / 2, per = parts_of(want);
     if (few && longest <= 512) per = std::max<int64_t>(per, 512 / tile);
-    for (int64_t more = per; more <= 2 * per; more = up(more + 1))
-        if (blocks_of(more) <= want) {
-            per = more;
-            break;
+    if (blocks_of(per) > want && blocks_of(2 * per) <= want) {  // (longer ranges are never more blocks: the shortest ones that are few enough, by halving)
+        int64_t low = per, high = 2 * per;  // too many blocks, few enough
+        while (high - low > step) {
+            const int64_t middle = up((low + high) / 2);
+            if (middle == high) break;
+            (blocks_of(middle) <= want ? high : low) = middle;
         }
+        per = high;
+    }
     int64_t part = 0;
     for (int j = 0; j < t.n; ++j) {
         Kv4Span &s = t.s[j];
