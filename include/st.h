@@ -531,7 +531,7 @@ int st_paged_append(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_
 
 /* Attention over the cache, scores scaled by head_dim^-1/2.  Without `tree` row i of a span attends to slots [0, len + i]; with it to slots [0, len) and
  * to those of the span's rows that tree->sees names (only sees and words are read), itself only if it is named.  A row that sees nothing gets zeros.  What is in
- * slots that a row does not see, infinities and NaN too, does not reach it.  q, out: n_q_heads * head_dim a row; they share no memory.
+ * slots that a row does not see, infinities and NaN too, does not reach it.  q, out: n_q_heads * head_dim a row, aligned as there; they share no memory.
  * ST_ERANGE: a span outside the table, too many rows, more rows of a span than `sees` has bits, more than 2^24 blocks of work. */
 int st_paged_attend(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_t n, const st_draft_tree *tree, const void *q, int64_t q_stride,
                     void *out, int64_t out_stride);

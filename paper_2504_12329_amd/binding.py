@@ -925,7 +925,7 @@ class PagedCache(_OnStream):
         if not (shape == (rows, heads * d) and stride[1] == 1 or
                 shape == (rows, heads, d) and stride[2] == 1 and (stride[1] == d or heads == 1)):
             raise StError(ST_EINVAL, f"{name} has shape {tuple(shape)} and strides {stride}, needs {rows} rows of {heads} x {d}")
-        return x.data_ptr(), stride[0] if rows > 1 else max(stride[0], heads * d)
+        return x.data_ptr(), stride[0] if rows > 1 else heads * d
 
     def _norm(self, name, w):
         if w is None:
@@ -1014,7 +1014,7 @@ class DraftVerifier(_OnStream):
     def _logits(self, name, x, rows):
         if x.dtype is not self.dtype or x.get_device() != self._index or x.shape != (rows, self.vocab) or (x.stride(1) != 1 and self.vocab > 1):
             raise StError(ST_EINVAL, f"{name} is {self.dtype} [{rows}][{self.vocab}] on {self._dev}, got {x.dtype} {tuple(x.shape)} {x.stride()} on {x.device}")
-        return x.data_ptr(), x.stride(0) if rows > 1 else max(x.stride(0), self.vocab)
+        return x.data_ptr(), x.stride(0) if rows > 1 else self.vocab
 
     def _numbers(self, name, x, n, dtype):
         if x.dtype is not dtype or x.get_device() != self._index or x.shape != (n,) or not x.is_contiguous():
@@ -1030,7 +1030,7 @@ class DraftVerifier(_OnStream):
                 return self.verify(spans, tokens, target, temperature, accept, sample, draft)
         n, rows = spans.n, spans.rows
         counts = [s[3] for s in spans.spans]
-        heat = [float(temperature)] * n if isinstance(temperature, (int, float)) else [float(x) for x in temperature]
+        heat = [float(x) for x in temperature] if hasattr(temperature, "__len__") else [float(temperature)] * n
         if len(heat) != n:
             raise StError(ST_EINVAL, f"{len(heat)} temperatures for {n} sequences")
         pt, st = self._logits("target", target, rows)
