@@ -1038,8 +1038,10 @@ class DraftVerifier(_OnStream):
         pk = self._numbers("tokens", tokens, rows, torch.int32)
         pa, ps = self._numbers("accept", accept, rows, torch.float64), self._numbers("sample", sample, n, torch.float64)
         most = max(counts, default=0)
-        path, accepted, after = self._empty((n, most), torch.int32), self._empty((n,), torch.int32), self._empty((n,), torch.int32)
+        out = self._empty((n * (most + 2),), torch.int32)       # (one allocation)
         if n:
+            at = out.data_ptr()
             _check(self._drafts(self._h, (C.c_int32 * n)(*counts), n, self._tree_of(spans), pk, pt, st, pd, sd, (C.c_float * n)(*heat), pa, ps,
-                                path.data_ptr(), most, accepted.data_ptr(), after.data_ptr()))
-        return path, accepted, after
+                                at, most, at + 4 * n * most, at + 4 * n * (most + 1)))
+        path, accepted, after = out.split_with_sizes((n * most, n, n))
+        return path.view(n, most), accepted, after

@@ -171,7 +171,8 @@ static int verify() {
                                                    (int32_t *)p, rows, (int32_t *)p, (int32_t *)p) == ST_OK);
                             const bool all = greedy == 1 || (greedy == 2 && n == 1);
                             const size_t left = (k & 2) && !all && (k & 1) && t.width > 1 ? t.width : 0;  // width - 1 looks, and the verdicts after them
-                            CHECK(!refused && launches.size() == 3 + left + (all ? 0 : 1));
+                            const bool fused = !left && rows <= 8 && ((int64_t)c.vocab + 4095) / 4096 * n <= 256;  // (the verdicts in the launch that draws)
+                            CHECK(!refused && launches.size() == 3 + left + (all ? 0 : 1) - fused);
                         }
                     }
                 }
