@@ -587,26 +587,26 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
 }
 
 // ---------------------------------------------------------------------------------------
-// Joins the key ranges of one row and head (a unit): WPU waves.  A lane takes the (max, sum) of one range, so that all of them are fetched at once; then D / 4
-// lanes add a range's output, four channels each, 64 WPU / (D / 4) ranges at a time.  A range of which the row sees nothing has sum 0 and an unused output.
+// Joins the key ranges of one row and head (a unit).  A range of which the row sees nothing has sum 0 and an unused output.
+// Few units: four waves each.  A lane takes the (max, sum) of one range, so that all of them are fetched at once; then D / 4 lanes add a range's output, four channels each,
+// 1024 / D ranges at a time.
 // ---------------------------------------------------------------------------------------
-template <class T, int D, int WPU, int CAP>
-__global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                                                    uint16_t *__restrict__ out, int64_t out_stride) {
-    constexpr int UPB = 4 / WPU, TPR = D / 4, PAR = 64 * WPU / TPR, kBatch = 8;  // units of a block, lanes of a range, ranges at a time
-    __shared__ float4 red[UPB][(PAR - 1) * TPR];
+template <class T, int D, int CAP>
+__global__ __launch_bounds__(256) void k_paged_join_wide(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                                                         uint16_t *__restrict__ out, int64_t out_stride) {
+    constexpr int TPR = D / 4, PAR = 256 / TPR, kBatch = 8;  // lanes of a range, ranges at a time
+    __shared__ float4 red[(PAR - 1) * TPR];
     const Kv4Span sp = t.s[blockIdx.y];
-    if (sp.splits == 1 || (int)blockIdx.x * UPB >= sp.rows * nq) return;
-    const int unit = blockIdx.x * UPB + threadIdx.x / (64 * WPU);
-    const bool live = unit < sp.rows * nq;
-    const int lane = threadIdx.x & 63, tid = threadIdx.x & (64 * WPU - 1), e = tid % TPR, g = tid / TPR;
+    const int unit = blockIdx.x;
+    if (sp.splits == 1 || unit >= sp.rows * nq) return;
+    const int tid = threadIdx.x, lane = tid & 63, e = tid % TPR, g = tid / TPR;
     const size_t step = (size_t)sp.rows * nq, pr = (size_t)sp.part0 + unit;
-    const float2 ml = live && lane < sp.splits ? reinterpret_cast<const float2 *>(part_ml)[pr + lane * step] : make_float2(-INFINITY, 0.f);
+    const float2 ml = lane < sp.splits ? reinterpret_cast<const float2 *>(part_ml)[pr + lane * step] : make_float2(-INFINITY, 0.f);
     const float4 *po = reinterpret_cast<const float4 *>(part_o) + pr * TPR + e;
     float4 v[kBatch];
     auto fetch = [&](int z0) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u] = live && z0 + u * PAR < sp.splits ? po[(z0 + u * PAR) * step * TPR] : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int u = 0; u < kBatch; ++u) v[u] = z0 + u * PAR < sp.splits ? po[(z0 + u * PAR) * step * TPR] : make_float4(0.f, 0.f, 0.f, 0.f);
     };
     fetch(g);
     const float M = wave_max(ml.x);
@@ -622,21 +622,55 @@ __global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int n
             if (z < sp.splits && lz != 0.f) A.x = fmaf(wz, v[u].x, A.x), A.y = fmaf(wz, v[u].y, A.y), A.z = fmaf(wz, v[u].z, A.z), A.w = fmaf(wz, v[u].w, A.w);
         }
     }
-    if constexpr (PAR > 1) {  // the PAR sums, in order
-        float4 *mine = red[threadIdx.x / (64 * WPU)];
-        if (g) mine[(g - 1) * TPR + e] = A;
-        __syncthreads();
-        if (g == 0)
+    if (g) red[(g - 1) * TPR + e] = A;  // the PAR sums, in order
+    __syncthreads();
+    if (g) return;
 #pragma unroll
-            for (int i = 1; i < PAR; ++i) {
-                const float4 x = mine[(i - 1) * TPR + e];
-                A.x += x.x, A.y += x.y, A.z += x.z, A.w += x.w;
+    for (int i = 1; i < PAR; ++i) {
+        const float4 x = red[(i - 1) * TPR + e];
+        A.x += x.x, A.y += x.y, A.z += x.z, A.w += x.w;
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    *reinterpret_cast<u32x2 *>(out + (int64_t)(sp.row0 + unit / nq) * out_stride + unit % nq * D + 4 * e) = u32x2{T::pack(A.x * inv, A.y * inv), T::pack(A.z * inv, A.w * inv)};
+}
+// Many units: D / 4 lanes each, four channels a lane, which reads every (max, sum) itself; nothing passes between lanes.
+template <class T, int D, int CAP>
+__global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                                                    uint16_t *__restrict__ out, int64_t out_stride) {
+    constexpr int TPU = D / 4, UPB = 256 / TPU, kBatch = 8;
+    const Kv4Span sp = t.s[blockIdx.y];
+    if (sp.splits == 1) return;
+    const int unit = blockIdx.x * UPB + threadIdx.x / TPU, e = threadIdx.x % TPU;
+    if (unit >= sp.rows * nq) return;
+    const size_t step = (size_t)sp.rows * nq, pr = (size_t)sp.part0 + unit;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + pr;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o) + pr * TPU + e;
+    float M = -INFINITY, L = 0.f;
+    float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z0 = 0; z0 < sp.splits; z0 += kBatch) {
+        float2 m[kBatch];
+        float4 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const bool there = z0 + u < sp.splits;
+            m[u] = there ? ml[(z0 + u) * step] : make_float2(-INFINITY, 0.f);
+            v[u] = there ? po[(z0 + u) * step * TPU] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) top = fmaxf(top, m[u].x);
+        const float corr = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);  // (0 where there is nothing yet: A and L are 0)
+        L *= corr, A.x *= corr, A.y *= corr, A.z *= corr, A.w *= corr;
+        M = top;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (m[u].y != 0.f) {
+                const float w = __builtin_amdgcn_exp2f(m[u].x - M);
+                L = fmaf(w, m[u].y, L), A.x = fmaf(w, v[u].x, A.x), A.y = fmaf(w, v[u].y, A.y), A.z = fmaf(w, v[u].z, A.z), A.w = fmaf(w, v[u].w, A.w);
             }
     }
-    if (!live || g) return;
     const float inv = L == 0.f ? 0.f : 1.0f / L;
-    const int row = sp.row0 + unit / nq, head = unit % nq;
-    *reinterpret_cast<u32x2 *>(out + (int64_t)row * out_stride + head * D + 4 * e) = u32x2{T::pack(A.x * inv, A.y * inv), T::pack(A.z * inv, A.w * inv)};
+    *reinterpret_cast<u32x2 *>(out + (int64_t)(sp.row0 + unit / nq) * out_stride + unit % nq * D + 4 * e) = u32x2{T::pack(A.x * inv, A.y * inv), T::pack(A.z * inv, A.w * inv)};
 }
 
 // ---------------------------------------------------------------------------------------
@@ -735,11 +769,12 @@ static hipError_t attend_in(const Paged &k, int layer, const Kv4Table &t, const 
                                k.part_ml);
         }
         if (p.join) {
-            // four waves a unit while there are fewer units than would fill the chip with one each
+            // four waves a unit while there are fewer units than would fill the chip otherwise
             const int64_t units = (int64_t)p.join * k.c.n_q_heads;
             const bool wide = units * t.n < 1024;
-            auto *kern = wide ? k_paged_join<T, D, 4, CAP> : k_paged_join<T, D, 1, CAP>;
-            hipLaunchKernelGGL(kern, dim3(wide ? units : (units + 3) / 4, t.n), dim3(256), 0, k.stream, tab, k.c.n_q_heads, k.part_o, k.part_ml, out, out_stride);
+            auto *kern = wide ? k_paged_join_wide<T, D, CAP> : k_paged_join<T, D, CAP>;
+            constexpr int per_block = 1024 / D;
+            hipLaunchKernelGGL(kern, dim3(wide ? units : (units + per_block - 1) / per_block, t.n), dim3(256), 0, k.stream, tab, k.c.n_q_heads, k.part_o, k.part_ml, out, out_stride);
         }
         e = hipGetLastError();
     });
