@@ -765,8 +765,8 @@ class Kv4Cache:
 
 class DraftSpans(Kv4Spans):
     """Spans whose rows are the last decided token and drafts after it: parents[j][i] is the row of span j that its row i follows, before it
-    (parents[j][0] is not read).  Made once for all layers of a step; a branch's rows see each other and the context, and a row's position is
-    the span's pos and the number of rows before it in its branch."""
+    (parents[j][0] is not read).  Made once for all layers of a step, and moved to the next one's places by at(); a branch's rows see each other and
+    the context, and a row's position is the span's pos and the number of rows before it in its branch."""
 
     def __init__(self, spans, parents, device="cuda"):
         super().__init__(spans)
@@ -776,25 +776,37 @@ class DraftSpans(Kv4Spans):
         if most > 1024:
             raise StError(ST_ERANGE, f"{most} rows of a span, trees have at most 1024")
         words = max(1, -(-most // 64))
-        parent, depth = np.full(self.rows, -1, dtype=np.int32), np.zeros(self.rows, dtype=np.int32)
-        sees, at, width = np.zeros((self.rows, words), dtype=np.uint64), 0, 1
+        parent, depth, masks, width = [], [], [], 1
         for ps in parents:
-            after = [0] * len(ps)
+            ps = [-1, *map(int, ps[1:])][:len(ps)]
+            d, m, after = [0] * len(ps), [1] * len(ps), [0] * len(ps)
             for i, p in enumerate(ps):
                 if i:
-                    p = int(p)
                     if not 0 <= p < i:
                         raise StError(ST_EINVAL, f"row {i} follows row {p}: not a row before it")
-                    parent[at + i], depth[at + i], sees[at + i] = p, depth[at + p] + 1, sees[at + p]
+                    d[i], m[i] = d[p] + 1, m[p] | 1 << i
                     after[p] += 1
-                sees[at + i, i // 64] |= np.uint64(1 << (i % 64))
+            parent += ps
+            depth += d
+            masks += m
             width = max(width, *after, 1)
-            at += len(ps)
         if width > 64:
             raise StError(ST_ERANGE, f"{width} rows follow one row, at most 64 are supported")
+        if words > 1:
+            masks = [m >> 64 * w & 2 ** 64 - 1 for m in masks for w in range(words)]
+        parent, depth, sees = np.array(parent, dtype=np.int32), np.array(depth, dtype=np.int32), np.array(masks, dtype=np.uint64)
         n = self.rows
-        bits = torch.from_numpy(np.concatenate([sees.reshape(-1).view(np.int32), parent, depth])).to(device)     # (one copy)
+        bits = torch.from_numpy(np.concatenate([sees.view(np.int32), parent, depth])).to(device)     # (one copy)
         self._take(bits[2 * n * words:2 * n * words + n], bits[2 * n * words + n:], bits[:2 * n * words].view(torch.int64).view(n, words) if n else bits.new_empty((0, words), dtype=torch.int64), width)
+
+    def at(self, spans):
+        """The same trees at other places: spans of as many rows each, as a step later."""
+        other = DraftSpans.__new__(DraftSpans)
+        Kv4Spans.__init__(other, spans)
+        if [s[3] for s in other.spans] != [s[3] for s in self.spans]:
+            raise StError(ST_EINVAL, "the spans have other numbers of rows than the trees")
+        other._take(self.parent, self.depth, self.sees, self.width)
+        return other
 
     @classmethod
     def of_tensors(cls, spans, parent=None, depth=None, sees=None, width=1):

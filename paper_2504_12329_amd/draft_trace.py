@@ -84,12 +84,15 @@ class Drafting:
         n = len(texts)
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
         self.verifier = B.DraftVerifier(large.cfg["vocab"], n * self.rows, max_width=max([1, *widths]))
-        self.widths = widths
+        self.widths, self.trees = widths, {}                  # trees: of the first levels, by their rows
         small.read(self.texts, [len(t) - 1 for t in texts])
         large.read(self.texts, [len(t) - 1 for t in texts])
 
     def _spans(self, model, rows):
-        return B.DraftSpans([(s, n, n, rows) for s, n in enumerate(model.len)], [self.parents[:rows]] * len(self.texts))
+        spans = [(s, n, n, rows) for s, n in enumerate(model.len)]
+        if rows not in self.trees:
+            self.trees[rows] = B.DraftSpans(spans, [self.parents[:rows]] * len(self.texts))
+        return self.trees[rows].at(spans)
 
     def draft(self):
         """Tokens of the trees [sequences][rows], and the small model's logits after every row but the last level's (zeros there)."""

@@ -261,6 +261,17 @@ def test_draft_spans():
     assert B.DraftSpans([], [], device="cpu").rows == 0
 
 
+def test_the_same_trees_at_other_places():
+    s = B.DraftSpans([(0, 9, 9, 3), (1, 0, 5, 1)], [[-1, 0, 0], [-1]], device="cpu")
+    t = s.at([(4, 20, 25, 3), (2, 7, 7, 1)])
+    assert t.spans == [(4, 20, 25, 3), (2, 7, 7, 1)] and t.rows == 4 and t.width == 2 and t.parent is s.parent and t.sees is s.sees and t.depth is s.depth
+    assert s.spans == [(0, 9, 9, 3), (1, 0, 5, 1)]
+    for bad in ([(0, 9, 9, 3)], [(0, 9, 9, 1), (1, 0, 5, 3)]):
+        with pytest.raises(B.StError) as e:
+            s.at(bad)
+        assert e.value.code == B.ST_EINVAL
+
+
 @pytest.mark.parametrize("parents", [[[-1, 0]], [[-1, 0, 0], [-1]], [[-1, 0, 2]], [[-1, 0, -1]], [[-1, 1, 0]]])
 def test_bad_parents(parents):
     with pytest.raises(B.StError) as e:
