@@ -536,7 +536,7 @@ int st_paged_append(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_
 int st_paged_attend(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_t n, const st_draft_tree *tree, const void *q, int64_t q_stride,
                     void *out, int64_t out_stride);
 
-/* Host only: how such a call of st_paged_attend is dealt out; see st_kv4_attend_plan. */
+/* Host only: how such a call of st_paged_attend is dealt out; see st_kv4_attend_plan.  with_tree: spans of more than 1024 rows are refused, as no tree has them. */
 int st_paged_attend_plan(const st_paged_config *cfg, const st_kv4_span *spans, int32_t n, int32_t with_tree, int32_t *columns, int32_t *blocks,
                          int32_t *ranges);
 

@@ -8,6 +8,7 @@ namespace st {
 
 // Attention: blocks that a call is cut into where it has the slots for them, and most key ranges of a span (a lane each in the join)
 constexpr int kPagedBlocks = 512, kPagedRanges = 64, kPagedColumns = 128;
+constexpr int kTreeWords = 16;  // most words of a row's bits
 
 // One layer of the cache, and where its sequences' pages are
 struct PagedView {
@@ -37,7 +38,7 @@ struct PagedAttendPlan {
     int join;        // rows of the longest span in several ranges, 0 without one
 };
 // Fills in blk0, splits, per and part0 of the spans
-PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree);
+PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t);
 
 // All enqueue only; the arguments have been checked.
 void launch_paged_append(const Paged &k, int layer, const Kv4Table &t, int rows, const int32_t *depth, const uint16_t *qkv, int64_t qkv_stride,

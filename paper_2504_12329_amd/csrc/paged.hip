@@ -19,6 +19,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // Append.  D / 8 threads per head; a thread owns two groups of four neighbouring channels.  Where pairs are halves of the rotating part the groups lie half of
 // it apart, else side by side, and either way the thread has its four pairs whole: pairs 4 l .. 4 l + 3 of the table.  Channels behind the rotating part
 // are passed on.  The norm's sum is an exchange over the head's 8 or 16 lanes.
+//
+// Memory bounds it: every number is read and written once, 8 bytes an instruction and lane so that a thread has whole pairs of either order without exchanges.  4096
+// rows of 40 / 8 heads of 128 with norms and rotation take 21.1 us, 119 MB at 5.6 TB/s (a copy of 2 GiB reaches 4.9; the rotation table comes from L2); a single row 2.1 us.
 // ---------------------------------------------------------------------------------------
 template <class T, int D, int CAP>
 __global__ __launch_bounds__(256) void k_paged_append(const Kv4Spans<CAP> t, const PagedView view, const int32_t *__restrict__ depth,
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(256) void k_paged_append(const Kv4Spans<CAP> t, con
 // ---------------------------------------------------------------------------------------
 // Keep.  A thread owns 16 bytes of a slot in one layer, plane and kv head, and moves them down the branch: every source lies behind its destination and behind all
 // destinations before, so sources that are read before their batch's first write are as they were.  A chain of four dependent loads (count, path, table, row) and
-// a batch of rows in flight: latency.
+// a batch of rows in flight: latency.  8 sequences of 21 rows in 64 layers of 8 heads of 128 take 7.3 us, one sequence in 28 layers of 2 heads 4.2 us.
 // ---------------------------------------------------------------------------------------
 constexpr int kKeepBatch = 8;
 
@@ -313,7 +316,7 @@ int st_paged_append(st_paged *h, int32_t layer, const st_kv4_span *spans, int32_
 static int check_sees(const st_draft_tree *tree, const st_kv4_span *spans, int n) {
     if (!tree->sees) return fail(ST_EINVAL, "tree: sees is NULL");
     if ((uintptr_t)tree->sees & 7) return fail(ST_EINVAL, "tree: sees is not aligned to 8 bytes");
-    if (tree->words < 1 || tree->words > 16) return fail(ST_EINVAL, "tree: %d words, 1 to 16 are supported", tree->words);
+    if (tree->words < 1 || tree->words > kTreeWords) return fail(ST_EINVAL, "tree: %d words, 1 to %d are supported", tree->words, kTreeWords);
     for (int j = 0; j < n; ++j)
         if (spans[j].rows > 64 * tree->words) return fail(ST_ERANGE, "span %d: %d rows, sees has bits for %d", j, spans[j].rows, 64 * tree->words);
     return ST_OK;
@@ -346,7 +349,9 @@ int st_paged_attend_plan(const st_paged_config *cfg, const st_kv4_span *spans, i
     int rows;
     carve(*cfg, nullptr, nullptr, &k, &cb, &wb);
     if (int rc = take_spans(k, spans, n, false, false, &t, &rows)) return rc;
-    const PagedAttendPlan p = plan_paged_attend(k, t, with_tree != 0);
+    for (int j = 0; with_tree && j < n; ++j)
+        if (spans[j].rows > 64 * kTreeWords) return fail(ST_ERANGE, "span %d: %d rows, trees have at most %d", j, spans[j].rows, 64 * kTreeWords);
+    const PagedAttendPlan p = plan_paged_attend(k, t);
     if (columns) *columns = rows ? p.cols : 0;
     if (blocks) *blocks = rows ? (int32_t)std::min<int64_t>(p.blocks, INT32_MAX) : 0;
     for (int j = 0; ranges && j < n; ++j) ranges[j] = t.s[j].rows ? t.s[j].splits : 0;

@@ -57,6 +57,10 @@ __device__ __forceinline__ PagedColumn paged_column(int col, int G, int kvh) { r
 // product wants them, 64 bytes of 16 slots an instruction; of eight slots of values a lane reads the D / 16 channels that make its row m of D / 16 products, whole
 // slots an instruction, and puts the slots of a channel together by byte permutes.  The next tile's loads are issued before this tile's work, its pages' numbers (wave-uniform, in
 // scalar registers) one tile before that.  A block's four waves take every fourth tile of its range and are joined through LDS; ranges are joined by k_paged_join.
+//
+// One row of 12 / 2 heads of 128 on 4608 slots: 5.6 us for 4.7 MB in 72 blocks of a tile a wave, which is the latency of queries, page numbers, tiles and the join of the
+// waves one after the other.  16 sequences of 4 rows of 40 / 8 heads on 3000 slots: 41 us for 197 MB, 4.8 TB/s, memory.  Columns by 32 are 16 to 30 % longer than
+// blocks of 128 once a call has more than 32 of them (see the plan), since every group of columns reads the cache again.
 // ---------------------------------------------------------------------------------------
 constexpr int kFewTile = 32, kFewWaves = 4;
 
@@ -315,6 +319,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_few(const Kv4Spa
 // directly (a wave loads 16 slots of a tile, which lie in one page), a tile ahead, 16-byte chunks swapped by the slot so that neither the reads of S^T
 // fragments nor the transposing reads of V^T meet in a bank.  S^T rows: fragment row m of 32 slots is slot m with bits 2 and 3 exchanged: registers 0-7 and
 // 8-15 of a lane are then eight consecutive slots each, as the second product wants them.
+//
+// Matrix and vector pipe bound it, one after the other: with 2048 rows of 40 / 8 heads behind 2048 slots (129 GFLOP, 0.72 PFLOP/s, 180 us) the matrix pipe is busy for 33 %
+// of the cycles and the vector pipe for 43 %, and 640 blocks on 512 places leave a sixth of the chip without work at the end.  A tile costs a block 2.2 us beside
+// another block on its compute unit, the call some 10 us beside its tiles.  Two blocks of four waves a compute unit are what 256 registers a lane and 66 KB of LDS allow.
+// Measured against it: products and softmax of 32-slot steps interleaved in one wave 220 us, eight waves in halves that take turns 196, fragments read 6 and 8
+// ahead 0, three blocks a compute unit not possible without spilling 40 registers.  16 sequences of 21 rows on 500 to 6000 slots: 53.7 us in 488 blocks.
 // ---------------------------------------------------------------------------------------
 constexpr int kChunkTile = 64, kChunkCols = kPagedColumns;
 template <int D>
@@ -439,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
     };
     // S^T: lane i of a 32-slot fragment reads slot swap23(i);  V^T: lane 4 r + x of a group of 16 reads four channels of slot r.  Fragment n of a product is read while
     // fragment n - kAhead is multiplied; what differs between fragments is an exclusive or of the lane's address, or a constant added to it.
-        constexpr int kAhead = 4, NS = 2 * ST, NV = 4 * TT;
+    constexpr int kAhead = 4, NS = 2 * ST, NV = 4 * TT;
     const int krow = (l32 & 19) | ((l32 & 4) << 1) | ((l32 & 8) >> 1), vr = (lane & 15) >> 2, vx = lane & 3, vg = (lane >> 4) & 1;
     const uint32_t k_lane = krow * RB + ((hf ^ swap(krow)) << 4);                                           // chunk 2 s + hf: ^ (s << 5)
     const uint32_t v_lane = (8 * hf + vr) * RB + (((2 * vg + (vx >> 1)) ^ swap(8 * hf + vr)) << 4) + (vx & 1) * 8;  // chunk 4 tt + ..: ^ (tt << 6); four slots on: ^ swap(4)
@@ -589,7 +599,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
 // ---------------------------------------------------------------------------------------
 // Joins the key ranges of one row and head (a unit).  A range of which the row sees nothing has sum 0 and an unused output.
 // Few units: four waves each.  A lane takes the (max, sum) of one range, so that all of them are fetched at once; then D / 4 lanes add a range's output, four channels each,
-// 1024 / D ranges at a time.
+// 1024 / D ranges at a time.  3.7 us with 12 units of 36 ranges: the launch and two dependent reads.
 // ---------------------------------------------------------------------------------------
 template <class T, int D, int CAP>
 __global__ __launch_bounds__(256) void k_paged_join_wide(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
@@ -633,7 +643,8 @@ __global__ __launch_bounds__(256) void k_paged_join_wide(const Kv4Spans<CAP> t, 
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     *reinterpret_cast<u32x2 *>(out + (int64_t)(sp.row0 + unit / nq) * out_stride + unit % nq * D + 4 * e) = u32x2{T::pack(A.x * inv, A.y * inv), T::pack(A.z * inv, A.w * inv)};
 }
-// Many units: D / 4 lanes each, four channels a lane, which reads every (max, sum) itself; nothing passes between lanes.
+// Many units: D / 4 lanes each, four channels a lane, which reads every (max, sum) itself; nothing passes between lanes.  2560 units of 21 ranges: 6.6 us for 27 MB that the
+// blocks before have just written, 4.1 TB/s.
 template <class T, int D, int CAP>
 __global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int nq, const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                     uint16_t *__restrict__ out, int64_t out_stride) {
@@ -676,7 +687,7 @@ __global__ __launch_bounds__(256) void k_paged_join(const Kv4Spans<CAP> t, int n
 // ---------------------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------------------
-PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree) {
+PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t) {
     const int nkv = k.c.n_kv_heads, G = k.c.n_q_heads / nkv;
     int64_t most = 0, longest = 0;
     for (int j = 0; j < t.n; ++j) {
@@ -684,7 +695,7 @@ PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree) {
         most = std::max<int64_t>(most, (int64_t)t.s[j].rows * G);
         longest = std::max<int64_t>(longest, (int64_t)t.s[j].len + t.s[j].rows);
     }
-        // us with columns by 32 : by 128, 40 / 8 heads, one sequence of 8 rows on 1000 slots 12.0 : 11.9, on 4000 18.1 : 13.1, of 64 rows on 4000 34.5 : 26.2; 16 of 8 rows on
+    // us with columns by 32 : by 128, 40 / 8 heads, one sequence of 8 rows on 1000 slots 12.0 : 11.9, on 4000 18.1 : 13.1, of 64 rows on 4000 34.5 : 26.2; 16 of 8 rows on
     // 3000 slots 51.1 : 44.2; 12 / 2 heads, 16 rows on 2000 slots 11.3 : 11.2, 40 rows 13.0 : 14.1
     PagedAttendPlan p{most <= 16 ? 16 : most <= 32 ? 32 : kChunkCols, 0, 0};
     const bool few = p.cols < kChunkCols;
@@ -703,12 +714,13 @@ PagedAttendPlan plan_paged_attend(const Paged &k, Kv4Table &t, bool tree) {
             if (t.s[j].rows) blocks += groups(t.s[j]) * ((tiles(t.s[j]) + x - 1) / x);
         return blocks;
     };
-        auto parts_of = [&](int64_t want) { return up(std::max((work + want - 1) / want, ((longest + tile - 1) / tile + kPagedRanges - 1) / kPagedRanges)); };
+    auto parts_of = [&](int64_t want) { return up(std::max((work + want - 1) / want, ((longest + tile - 1) / tile + kPagedRanges - 1) / kPagedRanges)); };
     // Ranges of less than eight tiles of 64 slots are made twice as long, for one block a compute unit: what such a block saves at its tiles costs as much again in
     // partial results.  us with 512 : 256 blocks, 40 / 8 heads, 64 rows on 1000 slots 24.4 : 19.1, on 4000 28.8 : 26.3, on 16000 44.8 : 50.1; 16 rows on 4000 20.7 : 16.4;
     // 16 sequences of 21 rows on 500 to 6000 67.0 : 77.6; 12 of 10 to 60 rows on 128 to 1500, 28 / 4 heads, 27.8 : 26.9.
     int64_t want = kPagedBlocks, per = parts_of(want);
     if (!few && per < 8) want = kPagedBlocks / 2, per = parts_of(want);
+    // up to 512 slots in one range, without a join: 12 / 2 heads, one row, 300 slots 7.4 us : 9.1 in ranges, 500 slots 8.6 : 9.2; 4 of 300 slots with 40 / 8 heads 7.6 : 9.2
     if (few && longest <= 512) per = std::max<int64_t>(per, 512 / tile);
     if (blocks_of(per) > want && blocks_of(2 * per) <= want) {  // (longer ranges are never more blocks: the shortest ones that are few enough, by halving)
         int64_t low = per, high = 2 * per;  // too many blocks, few enough
@@ -769,7 +781,8 @@ static hipError_t attend_in(const Paged &k, int layer, const Kv4Table &t, const 
                                k.part_ml);
         }
         if (p.join) {
-            // four waves a unit while there are fewer units than would fill the chip otherwise
+            // Four waves a unit while there are fewer units than would fill the chip otherwise.  us with four waves : without, 40 / 8 heads, one sequence, 1 row on 4000
+            // slots 9.3 : 11.4, on 2000 8 rows 12.0 : 14.3, 22 rows 18.2 : 19.7, 30 rows 17.6 : 17.6, 64 rows 22.6 : 21.3; 16 of 8 rows on 3000 slots 43.2 : 39.1
             const int64_t units = (int64_t)p.join * k.c.n_q_heads;
             const bool wide = units * t.n < 1024;
             auto *kern = wide ? k_paged_join_wide<T, D, CAP> : k_paged_join<T, D, CAP>;
@@ -783,7 +796,7 @@ static hipError_t attend_in(const Paged &k, int layer, const Kv4Table &t, const 
 
 int launch_paged_attend(const Paged &k, int layer, Kv4Table &t, const uint64_t *sees, int words, const uint16_t *q, int64_t q_stride, uint16_t *out,
                         int64_t out_stride) {
-    const PagedAttendPlan p = plan_paged_attend(k, t, sees != nullptr);
+    const PagedAttendPlan p = plan_paged_attend(k, t);
     // a launch has at most 2^32 - 1 threads a direction (asked before anything is launched)
     if (p.blocks >= 1 << 24) return fail(ST_ERANGE, "%lld blocks of work, 2^24 or more", (long long)p.blocks);
     const bool f16 = k.c.dtype == ST_F16;

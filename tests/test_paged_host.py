@@ -174,6 +174,7 @@ def test_attend_plan(L):
     assert max(plan(L, c, *spans((0, 16000, 0, 1), *((j, 200, 0, 1) for j in range(1, 64))))[3]) > 10
     assert L.st_paged_attend_plan(C.byref(c), *spans((0, 5, 0, 1)), 0, None, None, None) == B.ST_OK
     assert plan(L, config(head_dim=96), *spans((0, 0, 0, 1)))[0] == B.ST_EINVAL
+    assert plan(L, c, *spans((0, 5, 0, 1024)), 1)[0] == B.ST_OK and plan(L, c, *spans((0, 5, 0, 1025)), 1)[0] == B.ST_ERANGE and plan(L, c, *spans((0, 5, 0, 1025)))[0] == B.ST_OK
     for bad, code in BAD_SPANS:
         assert plan(L, config(), *spans(*bad))[0] == code
 
