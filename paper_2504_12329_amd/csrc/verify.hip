@@ -34,14 +34,14 @@ struct VerifySpans {
     int32_t first[kVerifySpans + 1];  // their first rows among the call's
     float heat[kVerifySpans];
 };
-// A part of a row: its largest logit and where it is (greedy sequences), or the sum of 2^((x c - base) / 64), c = 64 / (T ln 2), base the whole number nearest to the largest
-// x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/64).  sum: NaN where some logit is, or (T > 0) is +infinity
+// A part of a row: its largest logit and where it is (greedy sequences), or the sum of 2^((x c - base) / 256), c = 256 / (T ln 2), base the whole number nearest to the largest
+// x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/256).  sum: NaN where some logit is, or (T > 0) is +infinity
 struct VerifyPart {
     double base, sum;
     float top;
     int32_t at;
 };
-// A row: its distribution p(x) = 2^((x c - p_base) / 64) / p_sum, q alike, and the verdict over the rows that follow it
+// A row: its distribution p(x) = 2^((x c - p_base) / 256) / p_sum, q alike, and the verdict over the rows that follow it
 struct VerifyRow {
     double p_base, p_sum, q_base, q_sum;
     double a;        // p's weights are max(p - a q, 0) once all drafts have failed
@@ -115,6 +115,8 @@ struct LogitF16 {
     }
 };
 
+constexpr int kTable = 256;  // powers of 2 that are tabulated: 2^(i / kTable)
+
 // 2^t for t <= 0, off by less than 2e-14 of it: 2^n times the series of e^x, |x| <= ln 2 / 2, to its eleventh power
 __device__ __forceinline__ double exp2_64(double t) {
     t = fmax(t, -2000.0);
@@ -133,37 +135,52 @@ __device__ __forceinline__ double exp2_64(double t) {
     p = fma(p, x, 1.0);
     return ldexp(p, (int)n);
 }
-__device__ __forceinline__ double units_of(float heat) { return 64 * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/64 of a power of 2
-__device__ __forceinline__ double power_of(float x, double c, double base) { return exp2_64(fma((double)x, c, -base) * (1.0 / 64)); }
+__device__ __forceinline__ double units_of(float heat) { return kTable * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/256 of a power of 2
+__device__ __forceinline__ double power_of(float x, double c, double base) { return exp2_64(fma((double)x, c, -base) * (1.0 / kTable)); }
 
-// The same for many numbers, off by less than 3e-14 (the table's own error), in nine instructions of 64 bits: powers of 2^(1/64) from a table in LDS times a fourth-degree
-// polynomial (the series of e^x, |x| <= r = ln 2 / 128, with x^5 replaced by 5/4 r^2 x^3 - 5/16 r^4 x, which it is nearest to), the exponent added to the number's upper half.  (A
-// sum of 1.5 * 2^52 and a number has the rounded number in its low bits.)
+// The same for many numbers, off by less than 2e-14 of it, in eight instructions of 64 bits and three others: powers of 2^(1/256) from a table in LDS times a third-degree
+// polynomial (the series of e^x, |x| <= r = ln 2 / 512, with x^4 replaced by r^2 x^2 - r^4 / 8, which it is nearest to: off by r^4 / 192 = 1.8e-14), the exponent added to the
+// number's upper half.  (A sum of 1.5 * 2^52 and a number has the rounded number in its low bits.)  A table of 64 needs the fourth degree and one instruction more for
+// its index, which is no byte.
 struct Exp2Table {
-    const double *two;  // 2^(i / 64)
+    const uint2 *two;  // as fill_table leaves them
     double c, base, shift;
-    __device__ __forceinline__ Exp2Table(const double *table, double units, double b) : two(table), c(units), base(b), shift(6755399441055744.0 - b) {}
-    // y and g with y * g = 2^((x c - base) / 64); x c - base is above -64000 and not above 1
+    __device__ __forceinline__ Exp2Table(const uint2 *table, double units, double b) : two(table), c(units), base(b), shift(6755399441055744.0 - b) {}
+    // y and g with y * g = 2^((x c - base) / 256); x c - base is above -256000 and not above 1
     __device__ __forceinline__ double power(float x, double &g) const {
-        constexpr double l = 0.69314718055994530942 / 64, r = l / 2;
+        constexpr double l = 0.69314718055994530942 / kTable, r = l / 2;
         const double v = (double)x, k = fma(v, c, shift), f = fma(v, c, -(k - shift));
-        const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, k);
-        double p = l * l * l * l / 24;
-        p = fma(p, f, l * l * l * (1.0 / 6 + r * r / 96));
-        p = fma(p, f, l * l / 2);
-        p = fma(p, f, l * (1 - r * r * r * r / 384));
-        g = fma(p, f, 1.0);
-        const uint2 half = reinterpret_cast<const uint2 *>(two)[n & 63];
-        const uint32_t upper = half.y + ((uint32_t)(n >> 6) << 20);
+        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, k);
+        double p = l * l * l / 6;
+        p = fma(p, f, l * l * (0.5 + r * r / 24));
+        p = fma(p, f, l);
+        g = fma(p, f, 1 - r * r * r * r / 192);
+        const uint2 half = two[n & (kTable - 1)];
+        const uint32_t upper = half.y + (n << 12);
         return __builtin_bit_cast(double, (uint64_t)upper << 32 | half.x);
     }
-    __device__ __forceinline__ bool small(float x) const { return !(fma((double)x, c, -base) > -64000.0); }
+    __device__ __forceinline__ bool small(float x) const { return !(fma((double)x, c, -base) > -1000.0 * kTable); }
     __device__ __forceinline__ double any(float x) const { return small(x) ? 0.0 : power_of(x, c, base); }  // of any x; 0 below 2^-1000
     __device__ __forceinline__ bool exact() const { return fabs(base) < 0x1p50; }  // (a larger base, of temperatures near 0, would not leave the table's sums exact)
 };
-constexpr int kTable = 64;
-__device__ __forceinline__ void fill_table(double *two) {  // followed by a barrier
-    if (threadIdx.x < kTable) two[threadIdx.x] = exp2_64((int)threadIdx.x / 64.0 - 1.0) * 2.0;
+// 2^(i / 256) as its halves, the upper one less i << 12: with n << 12 added, n = 256 e + i, it is 2^e times as large
+struct Exp2Powers {
+    uint2 at[kTable];
+};
+constexpr Exp2Powers exp2_powers() {
+    Exp2Powers t{};
+    for (int i = 0; i < kTable; ++i) {
+        const double x = i * (0.69314718055994530942 / kTable);
+        double p = 1.0;
+        for (int k = 24; k; --k) p = 1.0 + p * x / k;  // the series of e^x
+        const uint64_t bits = __builtin_bit_cast(uint64_t, p);
+        t.at[i].x = (uint32_t)bits, t.at[i].y = (uint32_t)(bits >> 32) - ((uint32_t)i << 12);
+    }
+    return t;
+}
+__constant__ constexpr Exp2Powers kPowers = exp2_powers();
+__device__ __forceinline__ void fill_table(uint2 *two) {  // followed by a barrier
+    if (threadIdx.x < kTable) two[threadIdx.x] = kPowers.at[threadIdx.x];
 }
 
 // Sums over a wave by lane moves without LDS (see wave_sum)
@@ -285,7 +302,8 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
     const float heat = t.heat[j];
     if (is_draft && (heat == 0.f || !has_followers(a.parent, t.first[j], t.first[j + 1] - t.first[j], row - t.first[j]))) return;
     __shared__ float tops[4];
-    __shared__ double sums[4], two[kTable];
+    __shared__ double sums[4];
+    __shared__ uint2 two[kTable];
     __shared__ int lowest[4];
     typedef PartOf<L, PART> P;
     const P at = is_draft ? P(a.draft, a.draft_stride, row, part, a.vocab) : P(a.target, a.target_stride, row, part, a.vocab);
@@ -293,11 +311,11 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
     at.load(x);
     fill_table(two);
     float top = -INFINITY;
-    bool nan = false;
 #pragma unroll
     for (int i = 0; i < P::N; ++i)
 #pragma unroll
-        for (int e = 0; e < P::E; ++e) top = fmaxf(top, x[i][e]), nan |= x[i][e] != x[i][e];
+        for (int e = 0; e < P::E; ++e) top = __builtin_elementwise_maximum(top, x[i][e]);  // NaN where one is (wave_max passes it over)
+    const bool nan = top != top;
     top = wave_max(top);
     if ((tid & 63) == 0) tops[wave] = top;
     __syncthreads();
@@ -387,7 +405,7 @@ __device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int parts, flo
     double base = fmax(p0.base, p1.base);
     for (int i = lane + 128; i < parts; i += 64) base = fmax(base, part[i].base);
     base = wave_max64(base);
-    auto add = [&](const VerifyPart &p) { sum += p.sum * exp2_64((p.base - base) * (1.0 / 64)); };
+    auto add = [&](const VerifyPart &p) { sum += p.sum * exp2_64((p.base - base) * (1.0 / kTable)); };
     add(p0), add(p1);
     for (int i = lane + 128; i < parts; i += 64) add(part[i]);
     sum = wave_sum64(sum);
@@ -509,11 +527,11 @@ template <class L>
 struct Weights {
     typedef typename L::type X;
     const X *p, *q;
-    const double *two;
+    const uint2 *two;
     double c, p_base, p_of, q_base, q_of;  // q_of 0: without q
     const VerifyDraft *failed;
     int n_failed, vocab;
-    __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const double *table, float heat, double by, bool plain) {
+    __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const uint2 *table, float heat, double by, bool plain) {
         p = static_cast<const X *>(a.target) + row * a.target_stride, q = static_cast<const X *>(a.draft) + row * a.draft_stride;
         two = table, c = units_of(heat), p_base = r.p_base, p_of = 1.0 / r.p_sum, q_base = r.q_base, q_of = plain ? 0.0 : by / r.q_sum;
         failed = a.drafts + (size_t)row * a.width, n_failed = plain || a.draft ? 0 : r.drafts, vocab = a.vocab;
@@ -593,7 +611,8 @@ __global__ __launch_bounds__(256) void k_verify_left(const VerifySpans t, const 
     const int row = blockIdx.y, part = blockIdx.x;
     const VerifyRow r = a.row[row];
     if (r.stays != kOpen || r.drafts <= k) return;
-    __shared__ double sums[4], two[kTable];
+    __shared__ double sums[4];
+    __shared__ uint2 two[kTable];
     fill_table(two);
     double by = r.a;
     if (judge_on(a, row, k, by) >= 0) return;  // (every wave on its own, with the same result)
@@ -622,7 +641,8 @@ __global__ __launch_bounds__(FUSED ? 64 * kFusedRows : 256) void k_verify_draw(c
     const int first = t.first[j], rows = t.first[j + 1] - first;
     __shared__ int stays[FUSED ? kFusedRows : kVerifyRows], path[FUSED ? kFusedRows : kVerifyRows];
     __shared__ int end_of, count_of;
-    __shared__ double sums[FUSED ? kFusedRows : 4], two[kTable];
+    __shared__ double sums[FUSED ? kFusedRows : 4];
+    __shared__ uint2 two[kTable];
     __shared__ VerifyRow own[FUSED ? kFusedRows : 1];
     if constexpr (FUSED) {
         const int i = tid >> 6;  // a wave a row
@@ -679,7 +699,8 @@ __global__ __launch_bounds__(256) void k_verify_pick(const VerifySpans t, const 
     const int j = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, end = a.end[j];
     if (end < 0) return;
     double *weights = a.weight + (size_t)j * a.draw_parts;
-    __shared__ double sums[4], two[kTable], before_of;
+    __shared__ double sums[4], before_of;
+    __shared__ uint2 two[kTable];
     __shared__ int thread_of[4];
     fill_table(two);
     __syncthreads();
