@@ -138,8 +138,8 @@ __device__ __forceinline__ double exp2_64(double t) {
 __device__ __forceinline__ double units_of(float heat) { return kTable * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/256 of a power of 2
 __device__ __forceinline__ double power_of(float x, double c, double base) { return exp2_64(fma((double)x, c, -base) * (1.0 / kTable)); }
 
-// The same for many numbers, off by less than 2e-14 of it, in eight instructions of 64 bits and three others: powers of 2^(1/256) from a table in LDS times a third-degree
-// polynomial (the series of e^x, |x| <= r = ln 2 / 512, with x^4 replaced by r^2 x^2 - r^4 / 8, which it is nearest to: off by r^4 / 192 = 1.8e-14), the exponent added to the
+// The same for many numbers, off by less than 2.5e-14 of it and not at all at the table's own, in eight instructions of 64 bits and three others: powers of 2^(1/256) from a table in LDS times a third-degree
+// polynomial (the series of e^x, |x| <= r = ln 2 / 512, with x^4 replaced by 2 (sqrt 2 - 1) r^2 x^2, which it is nearest to: off by 0.172 r^4 / 24 = 2.4e-14), the exponent added to the
 // number's upper half.  (A sum of 1.5 * 2^52 and a number has the rounded number in its low bits.)  A table of 64 needs the fourth degree and one instruction more for
 // its index, which is no byte.
 struct Exp2Table {
@@ -152,15 +152,21 @@ struct Exp2Table {
         const double v = (double)x, k = fma(v, c, shift), f = fma(v, c, -(k - shift));
         const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, k);
         double p = l * l * l / 6;
-        p = fma(p, f, l * l * (0.5 + r * r / 24));
+        p = fma(p, f, l * l * (0.5 + 0.82842712474619009760 * r * r / 24));
         p = fma(p, f, l);
-        g = fma(p, f, 1 - r * r * r * r / 192);
+        g = fma(p, f, 1.0);
         const uint2 half = two[n & (kTable - 1)];
         const uint32_t upper = half.y + (n << 12);
         return __builtin_bit_cast(double, (uint64_t)upper << 32 | half.x);
     }
     __device__ __forceinline__ bool small(float x) const { return !(fma((double)x, c, -base) > -1000.0 * kTable); }
-    __device__ __forceinline__ double any(float x) const { return small(x) ? 0.0 : power_of(x, c, base); }  // of any x; 0 below 2^-1000
+    __device__ __forceinline__ double any(float x) const {  // of any x; 0 below 2^-1000
+        if (small(x)) return 0.0;
+        if (!exact()) return power_of(x, c, base);
+        double g;
+        const double y = power(x, g);
+        return y * g;
+    }
     __device__ __forceinline__ bool exact() const { return fabs(base) < 0x1p50; }  // (a larger base, of temperatures near 0, would not leave the table's sums exact)
 };
 // 2^(i / 256) as its halves, the upper one less i << 12: with n << 12 added, n = 256 e + i, it is 2^e times as large
@@ -546,8 +552,14 @@ struct Weights {
         return w;
     }
     static constexpr int E = L::kPer16, N = kOwn / E;
-    static __device__ __forceinline__ void load(const X *at, float (&x)[N][E]) {
-        if ((uintptr_t)at & 15) {
+    template <int N>
+    static __device__ __forceinline__ void load(const X *at, int there, float (&x)[N][E]) {  // what is not there: -infinity
+        if (there < N * E) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[i][e] = i * E + e < there ? L::get(at[i * E + e]) : -INFINITY;
+        } else if ((uintptr_t)at & 15) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -562,21 +574,20 @@ struct Weights {
     }
     // the sum of this thread's
     __device__ __forceinline__ double own(int part) const {
-        const int x0 = first(part);
+        const int x0 = first(part), there = min(vocab - x0, kOwn);
         const Exp2Table ep(two, c, p_base), eq(two, c, q_base);
-        bool plain = x0 + kOwn <= vocab && ep.exact() && eq.exact();
-        for (int f = 0; f < n_failed; ++f) plain &= failed[f].token < x0 || failed[f].token >= x0 + kOwn;
         double sum = 0.0;
-        if (plain) {
+        if (there <= 0) return sum;
+        if (!ep.exact() || !eq.exact()) {
+            for (int i = 0; i < there; ++i) sum += one(x0 + i);
+        } else if (q_of > 0.0) {
             float x[N][E], y[N][E], low = INFINITY, low_q = INFINITY;
-            load(p + x0, x);
-            if (q_of > 0.0) load(q + x0, y);
+            load(p + x0, there, x), load(q + x0, there, y);
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) low = fminf(low, x[i][e]), low_q = q_of > 0.0 ? fminf(low_q, y[i][e]) : 0.f;
-            plain = !ep.small(low) && !(q_of > 0.0 && eq.small(low_q));
-            if (plain && q_of > 0.0) {
+                for (int e = 0; e < E; ++e) low = fminf(low, x[i][e]), low_q = fminf(low_q, y[i][e]);
+            if (!ep.small(low) && !eq.small(low_q)) {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -585,19 +596,36 @@ struct Weights {
                         const double u = ep.power(x[i][e], g), z = eq.power(y[i][e], h);
                         sum += fmax(u * g * p_of - z * h * q_of, 0.0);
                     }
-            } else if (plain) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
+            } else {  // some are masked, or not there: vector by vector, for the registers' sake
+#pragma unroll 1
+                for (int i = 0; i < N; ++i) {
+                    float v[1][E], w[1][E];
+                    load(p + x0 + i * E, there - i * E, v), load(q + x0 + i * E, there - i * E, w);
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        double g;
-                        const double u = ep.power(x[i][e], g);
-                        sum = fma(u * p_of, g, sum);
+                        double g, h;
+                        const double u = ep.power(v[0][e], g), z = eq.power(w[0][e], h);
+                        sum += fmax((ep.small(v[0][e]) ? 0.0 : u * g * p_of) - (eq.small(w[0][e]) ? 0.0 : z * h * q_of), 0.0);
                     }
+                }
             }
+        } else {
+            float x[N][E];
+            load(p + x0, there, x);
+            uint32_t out = 0;  // the thread's tokens that have failed
+            for (int f = 0; f < n_failed; ++f) {
+                const uint32_t d = (uint32_t)(failed[f].token - x0);
+                out |= d < kOwn ? 1u << d : 0u;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    double g;
+                    const double u = ep.power(x[i][e], g);
+                    sum += ep.small(x[i][e]) || (out >> (i * E + e) & 1) ? 0.0 : u * p_of * g;
+                }
         }
-        if (!plain)
-            for (int i = 0; i < kOwn; ++i) sum += one(x0 + i);
         return sum;
     }
 };

@@ -167,6 +167,25 @@ def test_infinities_and_nan(with_draft):
     assert all(token == 8200 for _, token in check(rng, chains([3, 3]), 9000, [1.0, 0.0], with_draft, chain=True, change=one))
 
 
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("vocab,offset", [(9000, 0), (4099, 3), (16, 0)])
+def test_few_tokens_are_allowed(dtype, with_draft, vocab, offset):
+    """Nine tokens of ten forbidden to the target, others to the draft, and drafts that mostly fail, side by side"""
+    rng = np.random.default_rng(vocab)
+
+    def change(tokens, target, draft, accept, sample):
+        for x, part in ((target, 0.9), (draft, 0.5)):
+            out = rng.random(tuple(x.shape)) < part
+            out[:, vocab // 2] = False
+            x.masked_fill_(torch.from_numpy(out).cuda(), -float("inf"))
+        tokens[1::2] = vocab // 2 + np.arange(len(tokens[1::2])) % (vocab - vocab // 2)
+        accept[:] = 1 - (1 - accept) / 16
+    ends = check(rng, [random_tree(rng, n, 5) for n in (40, 25, 12)], vocab, [1.0, 0.6, 1.5], with_draft, dtype, offset=offset, change=change)
+    ends += check(rng, chains([6, 9, 3]), vocab, [1.0, 0.6, 1.5], with_draft, dtype, chain=True, offset=offset, change=change)
+    assert any(len(p) == 0 for p, _ in ends)
+
+
 @pytest.mark.parametrize("with_draft", [False, True])
 def test_random_numbers_at_their_ends(with_draft):
     rng = np.random.default_rng(10)
