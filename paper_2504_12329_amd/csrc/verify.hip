@@ -295,10 +295,10 @@ __device__ __forceinline__ bool has_followers(const int32_t *parent, int first, 
 // Sums.  A block is one part of one row; the part stays in registers between its largest number and its sum.  Draft rows that nothing follows, and those of greedy
 // sequences, are not read.
 //
-// 64-bit arithmetic bounds it: about 100 cycles for 64 exponentials, eight for each instruction of 64 bits.  256 rows of 152064 bf16 logits and as many of a draft, 156 MB:
-// 47.9 us, 3.2 TB/s; 336 and 336 rows of 152064 fp32 logits, of which 303 MB are read: 64.7 us, 4.7 TB/s, where memory counts as much.  Parts of 4096 logits cost nothing, of
-// 2048 20 % (the table is filled in every block); six and eight waves a SIMD spill (+12 and +24 %); a third-degree polynomial is not near enough (a verdict on
-// what is left of a difference goes wrong).
+// The vector pipe bounds it: eight instructions of 64 bits (as fast here as those of 32) and some six others a logit.  256 rows of 152064 bf16 logits and as many of a draft, 156 MB:
+// 42 us, 3.7 TB/s; 336 and 336 rows of 152064 fp32 logits, of which 303 MB are read: 61 us, 4.9 TB/s, what a large copy reaches.  Parts of 4096 logits cost nothing, of
+// 2048 20 % (the table is filled in every block); six and eight waves a SIMD spill (+12 and +24 %); a polynomial off by 4e-11 is not near enough (a verdict on what is left of
+// a difference goes wrong).
 // ---------------------------------------------------------------------------------------
 template <class L, int PART>
 __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, const VerifyArgs a) {
@@ -572,7 +572,8 @@ struct Weights {
             for (int i = 0; i < N; ++i) L::spread(v[i], x[i]);
         }
     }
-    // the sum of this thread's
+    // The sum of this thread's, from its registers: with two logits a token masked ones (and rows' ends) go vector by vector, since both forms side by side take 144 registers
+    // (4 trees of 64 rows 88 us instead of 82); masked they take 108, and 177 token by token.  Parts of 2048 logits: 84 us, 16 trees of 12 rows 62 instead of 64.
     __device__ __forceinline__ double own(int part) const {
         const int x0 = first(part), there = min(vocab - x0, kOwn);
         const Exp2Table ep(two, c, p_base), eq(two, c, q_base);
@@ -631,7 +632,7 @@ struct Weights {
 };
 
 // ---------------------------------------------------------------------------------------
-// Left: b_k of one part of one row.  Rows whose verdict is known, or that have no more drafts, return.  7.4 us for 256 rows of 152064 bf16 logits, of which those still
+// Left: b_k of one part of one row.  Rows whose verdict is known, or that have no more drafts, return.  7.1 us for 256 rows of 152064 bf16 logits, of which those still
 // open are read; one after the other for each k, since a_k is known only when b_k-1 is.
 // ---------------------------------------------------------------------------------------
 template <class L>
@@ -659,7 +660,7 @@ __global__ __launch_bounds__(64) void k_verify_close(const VerifyArgs a) {
 
 // ---------------------------------------------------------------------------------------
 // Draw.  Every block of a sequence walks through the rows that stay (one load, then steps in LDS), and sums up one part of the weights at the end of the walk; the first
-// one writes the path.  8.2 us for 16 sequences of 21 rows of 152064 logits, 8.8 with the verdicts of 5 rows: the walk and one part a block, dependent loads.
+// one writes the path.  7.8 us for 16 sequences of 21 rows of 152064 logits, 8.7 with the verdicts of 5 rows: the walk and one part a block, dependent loads.
 // ---------------------------------------------------------------------------------------
 // FUSED: of few rows the verdicts too, by every block alike, in the place of k_verify_rows.
 constexpr int kFusedRows = 8;
@@ -710,7 +711,7 @@ __global__ __launch_bounds__(FUSED ? 64 * kFusedRows : 256) void k_verify_draw(c
 // ---------------------------------------------------------------------------------------
 // Pick: the first token at which the running sum of the weights passes sample * their sum.  The part first, by every wave alike; in it a thread has neighbouring
 // tokens, so that the sums run from thread to thread; and of the thread that passes, its tokens, a lane each.  Where rounding lets none pass, the last with a weight.
-// 5.5 us for one sequence, 8.8 for 16: three dependent reads and the scans between them.
+// 5.5 us for one sequence, 8.0 for 16: three dependent reads and the scans between them.
 // ---------------------------------------------------------------------------------------
 // The first of 64 lanes at which the running sum of v passes the goal, or the last with a v; -1: there is none.  before: in the sum before the lanes, out before that one
 __device__ __forceinline__ int passing_lane(double v, double goal, double &before, bool &passes) {
