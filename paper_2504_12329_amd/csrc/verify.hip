@@ -35,7 +35,8 @@ struct VerifySpans {
     float heat[kVerifySpans];
 };
 // A part of a row: its largest logit and where it is (greedy sequences), or the sum of 2^((x c - base) / 256), c = 256 / (T ln 2), base the whole number nearest to the largest
-// x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/256).  sum: NaN where some logit is, or (T > 0) is +infinity
+// x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/256).  From 2^50 on (logits of 1e13 temperatures, and masks of a type's lowest number)
+// a base is the rounded product itself; any other logit of the type is 2^26 units away and more, 2^-24 of such a product, and weighs nothing.  sum: NaN where some logit is, or (T > 0) is +infinity
 struct VerifyPart {
     double base, sum;
     float top;
@@ -136,7 +137,12 @@ __device__ __forceinline__ double exp2_64(double t) {
     return ldexp(p, (int)n);
 }
 __device__ __forceinline__ double units_of(float heat) { return kTable * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/256 of a power of 2
-__device__ __forceinline__ double power_of(float x, double c, double base) { return exp2_64(fma((double)x, c, -base) * (1.0 / kTable)); }
+// Whether a base leaves x c - base as it is; else a weight is 1 where the products are the same, and 0 (the difference would be the product's rounding, of any size)
+__device__ __forceinline__ bool is_exact(double base) { return fabs(base) < 0x1p50; }
+__device__ __forceinline__ double weight_from(float x, double c, double base) { return rint((double)x * c) == base ? 1.0 : 0.0; }
+__device__ __forceinline__ double power_of(float x, double c, double base) {
+    return is_exact(base) ? exp2_64(fma((double)x, c, -base) * (1.0 / kTable)) : weight_from(x, c, base);
+}
 
 // The same for many numbers, off by less than 2.5e-14 of it and not at all at the table's own, in eight instructions of 64 bits and three others: powers of 2^(1/256) from a table in LDS times a third-degree
 // polynomial (the series of e^x, |x| <= r = ln 2 / 512, with x^4 replaced by 2 (sqrt 2 - 1) r^2 x^2, which it is nearest to: off by 0.172 r^4 / 24 = 2.4e-14), the exponent added to the
@@ -161,13 +167,13 @@ struct Exp2Table {
     }
     __device__ __forceinline__ bool small(float x) const { return !(fma((double)x, c, -base) > -1000.0 * kTable); }
     __device__ __forceinline__ double any(float x) const {  // of any x; 0 below 2^-1000
+        if (!exact()) return weight_from(x, c, base);
         if (small(x)) return 0.0;
-        if (!exact()) return power_of(x, c, base);
         double g;
         const double y = power(x, g);
         return y * g;
     }
-    __device__ __forceinline__ bool exact() const { return fabs(base) < 0x1p50; }  // (a larger base, of temperatures near 0, would not leave the table's sums exact)
+    __device__ __forceinline__ bool exact() const { return is_exact(base); }
 };
 // 2^(i / 256) as its halves, the upper one less i << 12: with n << 12 added, n = 256 e + i, it is 2^e times as large
 struct Exp2Powers {
@@ -342,11 +348,10 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
 #pragma unroll
                 for (int e = 0; e < P::E; ++e) low = fminf(low, x[i][e]);
             if (!ex.exact()) {
+#pragma unroll
                 for (int i = 0; i < P::N; ++i)
-                    for (int e = 0; e < P::E; ++e) {
-                        const int n = at.first(i) + e;
-                        if (n >= 0 && n < a.vocab) sum += ex.any(L::get(at.p[n]));
-                    }
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) sum += x[i][e] == top ? 1.0 : 0.0;
             } else if (__builtin_amdgcn_ballot_w64(ex.small(low)) == 0) {
 #pragma unroll
                 for (int i = 0; i < P::N; ++i)

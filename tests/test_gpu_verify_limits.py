@@ -1,0 +1,64 @@
+"""The verdict over drafted tokens where its numbers are at their ends, against its definition in 64 bits (paged_ref.verify): rows, numbers and tokens are equal, as in
+test_gpu_verify."""
+import numpy as np
+import pytest
+import torch
+
+from .test_gpu_verify import TYPES, chains, check, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- logits that are large against the temperature ----
+
+@pytest.mark.parametrize("name,value", [("fp32", None), ("fp32", -1e30), ("fp32", -1e20), ("bf16", None), ("bf16", -1e30), ("bf16", -1e20), ("fp16", None)])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_parts_of_a_row_that_are_masked_by_a_finite_number(name, value, with_draft):
+    """value None: the type's lowest"""
+    dtype = TYPES[name]
+    low = torch.finfo(dtype).min if value is None else value
+    rng = np.random.default_rng(1)
+
+    def change(tokens, target, draft, accept, sample):
+        target[:, 8192:24576] = low
+        draft[:, 4096:12288] = low
+        draft[:, ::2] = low
+    for heats in ([1.0, 0.8, 0.7], [0.6, 0.9, 0.3], [0.1, 1.5, 0.0]):
+        check(rng, [random_tree(rng, 7, 2) for _ in heats], 30011, heats, with_draft, dtype, change=change)
+        check(rng, chains([3, 1, 5]), 30011, heats, with_draft, dtype, chain=True, change=change)
+
+
+@pytest.mark.parametrize("top", ["lowest", -1e30, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_rows_whose_largest_logits_are_far_from_zero(top, dtype, with_draft):
+    """Nothing is left but equal numbers, a few or all of a row: they share it"""
+    top = torch.finfo(dtype).min if top == "lowest" else top
+    rng = np.random.default_rng(2)
+
+    def few(tokens, target, draft, accept, sample):
+        target[:] = -float("inf")
+        target[:, 77::2000] = top
+        draft[:, 77::1000] = top
+
+    def every(tokens, target, draft, accept, sample):
+        target[::2], draft[1::2] = top, top
+    for change in (few, every):
+        for heats in ([1.0, 0.8], [0.7, 0.6], [2.5, 0.0]):
+            check(rng, [random_tree(rng, 8, 3), random_tree(rng, 5, 1)], 9001, heats, with_draft, dtype, change=change)
+            check(rng, chains([4, 2]), 9001, heats, with_draft, dtype, chain=True, change=change)
+
+
+@pytest.mark.parametrize("T", [1e-9, 1e-12, 1e-17, 1e-18, 1e-20, 1e-30, 1.5e-45])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_temperatures_near_zero(T, with_draft):
+    rng = np.random.default_rng(3)
+
+    def shared(tokens, target, draft, accept, sample):          # many tokens have the largest logit
+        target.clamp_(max=2.0)
+        draft.clamp_(max=1.0)
+    for change in (None, shared):
+        for vocab in (50, 9000):
+            check(rng, [random_tree(rng, 12, 3) for _ in range(3)], vocab, [T, 1.0, T], with_draft, change=change)
+            check(rng, chains([1, 6]), vocab, [T, T], with_draft, chain=True, change=change)
+            check(rng, chains([12, 6]), vocab, [T, 0.7], with_draft, torch.bfloat16, chain=True, change=change)
