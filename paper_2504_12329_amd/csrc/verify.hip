@@ -517,6 +517,11 @@ __global__ __launch_bounds__(64) void k_verify_rows(const VerifySpans t, const V
     if (threadIdx.x == 0) a.row[row] = r;
 }
 
+// max(p - a q, 0), p and q given by factors.  Powers and sums are off by up to 2.5e-14 each, so that p and q of one distribution may differ by 1e-13 of themselves: as much of p
+// is left out, or what is left of it less itself would be drawn from their rounding.  (Written as the one fused instruction it is, so that every place that asks gets the same number.)
+constexpr double kSure = 1.0 - 0x1p-42;
+__device__ __forceinline__ double left_of(double p, double p_of, double q, double q_of) { return fmax(fma(p, p_of, -(q * q_of)), 0.0); }
+
 // The verdict over drafts 1 .. known - 1 of an open row, whose b_k have been summed; by one wave.  a: as they leave it
 __device__ __forceinline__ int judge_on(const VerifyArgs &args, int row, int known, double &a) {
     const int lane = threadIdx.x & 63;
@@ -526,7 +531,7 @@ __device__ __forceinline__ int judge_on(const VerifyArgs &args, int row, int kno
         double b = 0.0;
         for (int i = lane; i < args.draw_parts; i += 64) b += part[i];
         b = wave_sum64(b);
-        if (d.token >= 0 && d.token < args.vocab && d.u * d.q * b < fmax(d.p - a * d.q, 0.0)) return d.row;
+        if (d.token >= 0 && d.token < args.vocab && d.u * d.q * b < left_of(d.p, kSure, d.q, a)) return d.row;
         a += b;
     }
     return -1;
@@ -544,7 +549,7 @@ struct Weights {
     int n_failed, vocab;
     __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const uint2 *table, float heat, double by, bool plain) {
         p = static_cast<const X *>(a.target) + row * a.target_stride, q = static_cast<const X *>(a.draft) + row * a.draft_stride;
-        two = table, c = units_of(heat), p_base = r.p_base, p_of = 1.0 / r.p_sum, q_base = r.q_base, q_of = plain ? 0.0 : by / r.q_sum;
+        two = table, c = units_of(heat), p_base = r.p_base, q_base = r.q_base, q_of = plain ? 0.0 : by / r.q_sum, p_of = (q_of > 0.0 ? kSure : 1.0) / r.p_sum;
         failed = a.drafts + (size_t)row * a.width, n_failed = plain || a.draft ? 0 : r.drafts, vocab = a.vocab;
     }
     __device__ __forceinline__ int first(int part) const { return part * kDrawPart + (int)threadIdx.x * kOwn; }  // of this thread
@@ -552,9 +557,8 @@ struct Weights {
         if (x >= vocab) return 0.0;
         for (int f = 0; f < n_failed; ++f)
             if (failed[f].token == x) return 0.0;
-        double w = Exp2Table(two, c, p_base).any(L::get(p[x])) * p_of;
-        if (q_of > 0.0) w = fmax(w - Exp2Table(two, c, q_base).any(L::get(q[x])) * q_of, 0.0);
-        return w;
+        const double w = Exp2Table(two, c, p_base).any(L::get(p[x]));
+        return q_of > 0.0 ? left_of(w, p_of, Exp2Table(two, c, q_base).any(L::get(q[x])), q_of) : w * p_of;
     }
     static constexpr int E = L::kPer16, N = kOwn / E;
     template <int N>
@@ -600,7 +604,7 @@ struct Weights {
                     for (int e = 0; e < E; ++e) {
                         double g, h;
                         const double u = ep.power(x[i][e], g), z = eq.power(y[i][e], h);
-                        sum += fmax(u * g * p_of - z * h * q_of, 0.0);
+                        sum += left_of(u * g, p_of, z * h, q_of);
                     }
             } else {  // some are masked, or not there: vector by vector, for the registers' sake
 #pragma unroll 1
@@ -611,7 +615,7 @@ struct Weights {
                     for (int e = 0; e < E; ++e) {
                         double g, h;
                         const double u = ep.power(v[0][e], g), z = eq.power(w[0][e], h);
-                        sum += fmax((ep.small(v[0][e]) ? 0.0 : u * g * p_of) - (eq.small(w[0][e]) ? 0.0 : z * h * q_of), 0.0);
+                        sum += left_of(ep.small(v[0][e]) ? 0.0 : u * g, p_of, eq.small(w[0][e]) ? 0.0 : z * h, q_of);
                     }
                 }
             }

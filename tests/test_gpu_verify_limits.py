@@ -4,6 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2504_12329_amd import binding as B
+
+from . import paged_ref as R
 from .test_gpu_verify import TYPES, chains, check, random_tree
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +65,47 @@ def test_temperatures_near_zero(T, with_draft):
             check(rng, [random_tree(rng, 12, 3) for _ in range(3)], vocab, [T, 1.0, T], with_draft, change=change)
             check(rng, chains([1, 6]), vocab, [T, T], with_draft, chain=True, change=change)
             check(rng, chains([12, 6]), vocab, [T, 0.7], with_draft, torch.bfloat16, chain=True, change=change)
+
+
+# ---- target and draft that agree ----
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("vocab,masked", [(50, False), (9001, False), (9001, True)])
+def test_nothing_is_left_of_a_distribution_less_itself(dtype, vocab, masked):
+    """Drafts that cannot stay (no tokens), then others: what is left of p is empty, no draft after them stays, and the next token is drawn from p itself"""
+    rng = np.random.default_rng(4)
+
+    def change(tokens, target, draft, accept, sample):
+        if masked:
+            target[:, ::3] = -float("inf")
+        draft.copy_(target)
+        tokens[1:] = np.where(rng.random(len(tokens) - 1) < 0.5, -1, rng.integers(0, vocab, len(tokens) - 1))
+        tokens[[1, 2, 3]] = -1
+        accept[4::2] = 0.0
+    for heats in ([1.0, 1.0], [0.5, 2.0]):
+        got = check(rng, [[-1, 0, 0, 0], [-1, 0, 0, 1]], vocab, heats, True, dtype, change=change)
+        assert got[0][0] == []
+        check(rng, [random_tree(rng, 30, 5), random_tree(rng, 20, 4)], vocab, heats, True, dtype, change=change)
+        check(rng, chains([4, 2]), vocab, heats, True, dtype, chain=True, change=change)
+    for _ in range(10):
+        check(rng, chains([4, 2, 12]), vocab, [1.0] * 3, True, dtype, chain=True, change=change)
+
+
+@pytest.mark.parametrize("vocab", [9001, 30011])
+@pytest.mark.parametrize("how", ["place", "shift"])
+def test_the_same_distribution_from_other_numbers(vocab, how):
+    """Rows that are cut into parts at other places, or logits that differ by one constant (multiples of 2^-8 up to 16: exactly)"""
+    rng = np.random.default_rng(5)
+    n = 16
+    target = torch.from_numpy(np.round(rng.standard_normal((2 * n, vocab)) * 768) / 256).clamp_(-15, 15).float().cuda()
+    wide = torch.zeros(2 * n, vocab + 7, device="cuda")
+    draft = wide[:, 3:3 + vocab] if how == "place" else wide[:, :vocab]
+    draft.copy_(target if how == "place" else target + 37.25)
+    tokens, accept, sample = np.tile([0, -1], n), rng.random(2 * n), rng.random(n)
+    v = B.DraftVerifier(vocab, 2 * n)
+    c = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    path, counts, after = v.verify(B.Kv4Spans([(j, 0, 0, 2) for j in range(n)]), c(tokens).int(), target, 0.7, c(accept), c(sample), draft=draft)
+    assert counts.tolist() == [0] * n
+    x = target.double().cpu().numpy()
+    want = [R.verify([-1, 0], tokens[:2], x[2 * j:2 * j + 2], x[2 * j:2 * j + 2], 0.7, accept[2 * j:2 * j + 2], sample[j])[1] for j in range(n)]
+    assert after.tolist() == want
