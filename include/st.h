@@ -573,6 +573,10 @@ void st_verify_destroy(st_verify *v);
 int st_verify_drafts(st_verify *v, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
                      int64_t target_stride, const void *draft, int64_t draft_stride, const float *temperature, const double *accept,
                      const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next);
+/* The same with temperatures of 64 bits, for those that 32 do not hold (0.6 rounded moves a verdict's border by some 1e-8). */
+int st_verify_drafts64(st_verify *v, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
+                       int64_t target_stride, const void *draft, int64_t draft_stride, const double *temperature, const double *accept,
+                       const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next);
 
 const char *st_last_error(void);
 

@@ -27,7 +27,7 @@ EXPORTS = ("st_query_sizes", "st_prefill_plan_check", "st_prefill_plan_forms", "
            "st_generate_batch", "st_kv4_query_sizes", "st_kv4_create", "st_kv4_destroy", "st_kv4_append", "st_kv4_attend",
            "st_kv4_attend_plan", "st_kv4_evict", "st_kv4_read", "st_paged_query_sizes", "st_paged_create", "st_paged_destroy",
            "st_paged_append", "st_paged_attend", "st_paged_attend_plan", "st_paged_keep", "st_verify_query_sizes", "st_verify_create",
-           "st_verify_destroy", "st_verify_drafts", "st_last_error")
+           "st_verify_destroy", "st_verify_drafts", "st_verify_drafts64", "st_last_error")
 
 
 class StError(RuntimeError):
@@ -181,6 +181,7 @@ def lib():
         L.st_verify_destroy.restype = None
         L.st_verify_drafts.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        L.st_verify_drafts64.argtypes = L.st_verify_drafts.argtypes
         _lib = L
     return _lib
 
@@ -1007,7 +1008,7 @@ class PagedCache(_OnStream):
 
 
 class DraftVerifier(_OnStream):
-    """st_verify over a torch-owned workspace: the verdict over drafted tokens (see st_verify_drafts)."""
+    """st_verify over a torch-owned workspace: the verdict over drafted tokens (see st_verify_drafts64)."""
 
     def __init__(self, vocab, max_rows, max_width=1, dtype=torch.float32, device="cuda", stream=None):
         if dtype not in _TYPE_OF:
@@ -1021,7 +1022,7 @@ class DraftVerifier(_OnStream):
         self._ws = self._empty((wb.value,), torch.uint8)
         h = C.c_void_p()
         _check(lib().st_verify_create(C.byref(c), self._ws.data_ptr(), wb.value, self.stream, C.byref(h)))
-        self._h, self._destroy, self._drafts = h, lib().st_verify_destroy, lib().st_verify_drafts
+        self._h, self._destroy, self._drafts = h, lib().st_verify_destroy, lib().st_verify_drafts64
 
     def _logits(self, name, x, rows):
         if x.dtype is not self.dtype or x.get_device() != self._index or x.shape != (rows, self.vocab) or (x.stride(1) != 1 and self.vocab > 1):
@@ -1053,7 +1054,7 @@ class DraftVerifier(_OnStream):
         out = self._empty((n * (most + 2),), torch.int32)       # (one allocation)
         if n:
             at = out.data_ptr()
-            _check(self._drafts(self._h, (C.c_int32 * n)(*counts), n, self._tree_of(spans), pk, pt, st, pd, sd, (C.c_float * n)(*heat), pa, ps,
+            _check(self._drafts(self._h, (C.c_int32 * n)(*counts), n, self._tree_of(spans), pk, pt, st, pd, sd, (C.c_double * n)(*heat), pa, ps,
                                 at, most, at + 4 * n * most, at + 4 * n * (most + 1)))
         path, accepted, after = out.split_with_sizes((n * most, n, n))
         return path.view(n, most), accepted, after

@@ -32,7 +32,7 @@ constexpr int kVerifySpans = ST_KV4_MAX_SPANS;
 struct VerifySpans {
     int32_t n;
     int32_t first[kVerifySpans + 1];  // their first rows among the call's
-    float heat[kVerifySpans];
+    double heat[kVerifySpans];
 };
 // A part of a row: its largest logit and where it is (greedy sequences), or the sum of 2^((x c - base) / 256), c = 256 / (T ln 2), base the whole number nearest to the largest
 // x c: products with c are never rounded, and parts of different bases differ by a power of 2^(1/256).  From 2^50 on (logits of 1e13 temperatures, and masks of a type's lowest number)
@@ -136,7 +136,7 @@ __device__ __forceinline__ double exp2_64(double t) {
     p = fma(p, x, 1.0);
     return ldexp(p, (int)n);
 }
-__device__ __forceinline__ double units_of(float heat) { return kTable * 1.4426950408889634074 / (double)heat; }  // c: logits to 1/256 of a power of 2
+__device__ __forceinline__ double units_of(double heat) { return kTable * 1.4426950408889634074 / heat; }  // c: logits to 1/256 of a power of 2
 // Whether a base leaves x c - base as it is; else a weight is 1 where the products are the same, and 0 (the difference would be the product's rounding, of any size)
 __device__ __forceinline__ bool is_exact(double base) { return fabs(base) < 0x1p50; }
 __device__ __forceinline__ double weight_from(float x, double c, double base) { return rint((double)x * c) == base ? 1.0 : 0.0; }
@@ -311,8 +311,8 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
     const bool is_draft = (int)blockIdx.y >= a.rows;
     const int row = blockIdx.y - (is_draft ? a.rows : 0), part = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
     const int j = span_of_row(t, row);
-    const float heat = t.heat[j];
-    if (is_draft && (heat == 0.f || !has_followers(a.parent, t.first[j], t.first[j + 1] - t.first[j], row - t.first[j]))) return;
+    const double heat = t.heat[j];
+    if (is_draft && (heat == 0.0 || !has_followers(a.parent, t.first[j], t.first[j + 1] - t.first[j], row - t.first[j]))) return;
     __shared__ float tops[4];
     __shared__ double sums[4];
     __shared__ uint2 two[kTable];
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
     double sum = nan ? (double)NAN : 0.0;
     int low = INT32_MAX;
     double base = -1e300;  // of a part without numbers
-    if (heat > 0.f) {
+    if (heat > 0.0) {
         const double c = units_of(heat);
         if (top == INFINITY) {
             sum = (double)NAN;
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(256, 4) void k_verify_sums(const VerifySpans t, con
     sum = block_sum64(sum, sums);
     if (tid == 0)
         a.part[(size_t)blockIdx.y * a.sum_parts + part] =
-            VerifyPart{base, sum, top, heat > 0.f ? 0 : min(min(lowest[0], lowest[1]), min(lowest[2], lowest[3]))};
+            VerifyPart{base, sum, top, heat > 0.0 ? 0 : min(min(lowest[0], lowest[1]), min(lowest[2], lowest[3]))};
 }
 
 // A row from its parts, by one wave
@@ -394,13 +394,13 @@ struct RowSum {
     int at;     // greedy: the largest number's token
     bool good;  // it is a distribution (greedy: it has a largest number)
 };
-__device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int parts, float heat) {
+__device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int parts, double heat) {
     const int lane = threadIdx.x & 63;
     constexpr VerifyPart none{-1e300, 0.0, -INFINITY, INT32_MAX};
     const VerifyPart p0 = lane < parts ? part[lane] : none, p1 = lane + 64 < parts ? part[lane + 64] : none;
     float top = fmaxf(p0.top, p1.top);
     double sum = 0.0;
-    if (heat == 0.f) {
+    if (heat == 0.0) {
         for (int i = lane + 128; i < parts; i += 64) top = fmaxf(top, part[i].top);
         top = wave_max(top);
         int at = INT32_MAX;
@@ -428,10 +428,10 @@ __device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int parts, flo
 // draft logits, of the first of them.  A chain of dependent loads (parts, tokens, their logits): 5.9 us for 336 rows.
 // ---------------------------------------------------------------------------------------
 template <class L>
-__device__ __forceinline__ VerifyRow row_verdict(const VerifyArgs &a, int first, int rows, int local, float heat) {
+__device__ __forceinline__ VerifyRow row_verdict(const VerifyArgs &a, int first, int rows, int local, double heat) {
     typedef typename L::type X;
     const int row = first + local, lane = threadIdx.x & 63;
-    const bool draws = a.draft && heat > 0.f;
+    const bool draws = a.draft && heat > 0.0;
     // the first 64 rows behind it, which is where what follows it mostly is: asked for beside the parts
     const X *pr = static_cast<const X *>(a.target) + row * a.target_stride, *qr = static_cast<const X *>(a.draft) + row * a.draft_stride;
     struct Near {
@@ -457,7 +457,7 @@ __device__ __forceinline__ VerifyRow row_verdict(const VerifyArgs &a, int first,
     Near near = look(local + 1);
     const RowSum p = row_sum(a.part + (size_t)row * a.sum_parts, a.sum_parts, heat);
     RowSum q{0.0, 1.0, 0, true};
-    const double c = heat > 0.f ? units_of(heat) : 0.0;
+    const double c = heat > 0.0 ? units_of(heat) : 0.0;
     int stays = -1, drafts = 0, failed_token = -1;  // lane i: token of draft i that failed
     bool good = p.good, have_q = false;
     double rest = p.sum;  // what the failed tokens leave of the sum, without draft logits
@@ -473,13 +473,13 @@ __device__ __forceinline__ VerifyRow row_verdict(const VerifyArgs &a, int first,
             if (!good) break;
         }
         const bool known = near.token >= 0 && near.token < a.vocab;
-        double pt = known && heat > 0.f ? power_of(near.x, c, p.base) : 0.0;
+        double pt = known && heat > 0.0 ? power_of(near.x, c, p.base) : 0.0;
         const double qt = known && draws ? power_of(near.y, c, q.base) / q.sum : 0.0;
         if (draws) pt /= p.sum;
         for (uint64_t bits = near.follow; bits && drafts < a.width && stays < 0; bits &= bits - 1) {
             const int l = __builtin_ctzll(bits), token = __builtin_amdgcn_readlane(near.token, l);
             const bool in = token >= 0 && token < a.vocab;
-            if (heat == 0.f) {
+            if (heat == 0.0) {
                 if (in && token == p.at) stays = c0 + l;
             } else if (draws) {
                 if (drafts == 0 && in && lane64(near.u, l) * lane64(qt, l) < lane64(pt, l)) stays = c0 + l;
@@ -506,7 +506,7 @@ __device__ __forceinline__ VerifyRow row_verdict(const VerifyArgs &a, int first,
             drafts += stays < 0 || draws;
         }
     }
-    if (!draws && heat > 0.f && lane < drafts) a.drafts[(size_t)row * a.width + lane].token = failed_token;
+    if (!draws && heat > 0.0 && lane < drafts) a.drafts[(size_t)row * a.width + lane].token = failed_token;
     return VerifyRow{p.base, p.sum, q.base, q.sum, draws && drafts > 0 && stays < 0 ? 1.0 : 0.0, stays < 0 && good && draws && drafts > 1 ? kOpen : stays, drafts, p.at, good};
 }
 
@@ -547,7 +547,7 @@ struct Weights {
     double c, p_base, p_of, q_base, q_of;  // q_of 0: without q
     const VerifyDraft *failed;
     int n_failed, vocab;
-    __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const uint2 *table, float heat, double by, bool plain) {
+    __device__ __forceinline__ Weights(const VerifyArgs &a, int row, const VerifyRow &r, const uint2 *table, double heat, double by, bool plain) {
         p = static_cast<const X *>(a.target) + row * a.target_stride, q = static_cast<const X *>(a.draft) + row * a.draft_stride;
         two = table, c = units_of(heat), p_base = r.p_base, q_base = r.q_base, q_of = plain ? 0.0 : by / r.q_sum, p_of = (q_of > 0.0 ? kSure : 1.0) / r.p_sum;
         failed = a.drafts + (size_t)row * a.width, n_failed = plain || a.draft ? 0 : r.drafts, vocab = a.vocab;
@@ -701,8 +701,8 @@ __global__ __launch_bounds__(FUSED ? 64 * kFusedRows : 256) void k_verify_draw(c
     __syncthreads();
     const int end = first + end_of, count = count_of;
     const VerifyRow r = FUSED ? own[end_of] : a.row[end];
-    const float heat = t.heat[j];
-    const bool drawn = heat > 0.f && r.good;
+    const double heat = t.heat[j];
+    const bool drawn = heat > 0.0 && r.good;
     if (part == 0) {
         for (int i = tid; i < a.path_stride; i += 256) a.path[(int64_t)j * a.path_stride + i] = i < count ? path[i] : -1;
         if (tid == 0) {
@@ -891,9 +891,9 @@ int st_verify_create(const st_verify_config *cfg, void *workspace, size_t worksp
 
 void st_verify_destroy(st_verify *h) { delete reinterpret_cast<Verify *>(h); }
 
-int st_verify_drafts(st_verify *h, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
-                     int64_t target_stride, const void *draft, int64_t draft_stride, const float *temperature, const double *accept,
-                     const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next) {
+int st_verify_drafts64(st_verify *h, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
+                       int64_t target_stride, const void *draft, int64_t draft_stride, const double *temperature, const double *accept,
+                       const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next) {
     const Verify *v = reinterpret_cast<const Verify *>(h);
     if (!v) return fail(ST_EINVAL, "verifier is NULL");
     if (n < 0 || n > kVerifySpans) return fail(ST_EINVAL, "%d sequences, 0 to %d are supported", n, kVerifySpans);
@@ -906,10 +906,10 @@ int st_verify_drafts(st_verify *h, const int32_t *rows, int32_t n, const st_draf
     for (int j = 0; j < n; ++j) {
         if (rows[j] < 1 || rows[j] > kVerifyRows) return fail(ST_ERANGE, "sequence %d: %d rows, 1 to %d are supported", j, rows[j], kVerifyRows);
         if (rows[j] > path_stride) return fail(ST_ERANGE, "sequence %d: %d rows, path_stride is %d", j, rows[j], path_stride);
-        if (!(temperature[j] >= 0.f) || std::isinf(temperature[j])) return fail(ST_EINVAL, "sequence %d: bad temperature", j);
+        if (!(temperature[j] >= 0.0) || std::isinf(temperature[j])) return fail(ST_EINVAL, "sequence %d: bad temperature", j);
         t.first[j] = (int32_t)total;
-        t.heat[j] = temperature[j];
-        all_greedy = all_greedy && temperature[j] == 0.f;
+        t.heat[j] = temperature[j] > 0.0 ? std::max(temperature[j], 0x1p-800) : 0.0;  // (products with 1 / T stay finite; any two logits are far apart by then)
+        all_greedy = all_greedy && temperature[j] == 0.0;
         total += rows[j];
         if (total > v->c.max_rows) return fail(ST_ERANGE, "%lld rows or more, max_rows is %d", (long long)total, v->c.max_rows);
     }
@@ -930,6 +930,15 @@ int st_verify_drafts(st_verify *h, const int32_t *rows, int32_t n, const st_draf
     else if (v->c.dtype == ST_BF16) launch_verify<LogitBf16>(*v, t, a, all_greedy);
     else launch_verify<LogitF16>(*v, t, a, all_greedy);
     return launched("st_verify_drafts", hipGetLastError());
+}
+
+int st_verify_drafts(st_verify *h, const int32_t *rows, int32_t n, const st_draft_tree *tree, const int32_t *tokens, const void *target,
+                     int64_t target_stride, const void *draft, int64_t draft_stride, const float *temperature, const double *accept,
+                     const double *sample, int32_t *path, int32_t path_stride, int32_t *accepted, int32_t *next) {
+    double heat[kVerifySpans];
+    for (int j = 0; temperature && j < n && j < kVerifySpans; ++j) heat[j] = temperature[j];
+    return st_verify_drafts64(h, rows, n, tree, tokens, target, target_stride, draft, draft_stride, temperature ? heat : nullptr, accept, sample, path,
+                              path_stride, accepted, next);
 }
 
 }  // extern "C"

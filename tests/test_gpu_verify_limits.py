@@ -109,3 +109,57 @@ def test_the_same_distribution_from_other_numbers(vocab, how):
     x = target.double().cpu().numpy()
     want = [R.verify([-1, 0], tokens[:2], x[2 * j:2 * j + 2], x[2 * j:2 * j + 2], 0.7, accept[2 * j:2 * j + 2], sample[j])[1] for j in range(n)]
     assert after.tolist() == want
+
+
+# ---- the temperature ----
+
+@pytest.mark.parametrize("T", [0.6, 0.7, 0.8, 0.9, 1 / 3, 1e-3])
+def test_the_temperature_is_not_rounded(T):
+    """Random numbers half way between the borders that T and T rounded to 32 bits have: 5e-11 and more from either, at sums that are right to 1e-13"""
+    rng = np.random.default_rng(6)
+    near, vocab, n = float(np.float32(T)), 3000, 24
+    x = np.float32(rng.standard_normal((2 * n, vocab)) * (3.0 if T > 0.1 else 0.01)).astype(np.float64)
+    y = np.float32(x + 0.7 * (1.0 if T > 0.1 else 0.003) * rng.standard_normal(x.shape)).astype(np.float64)
+    tokens, accept, sample = np.zeros(2 * n, dtype=np.int64), np.full(2 * n, 0.999), rng.random(n)
+    for j in range(n):
+        p, q, p32, q32 = (R.softmax(z[2 * j], t) for t in (T, near) for z in (x, y))
+        if j % 3 == 0:                                           # the draft's verdict
+            ratio, ratio32 = p / q, p32 / q32
+            t = int(np.argmax(np.where(np.maximum(ratio, ratio32) < 1, np.abs(ratio - ratio32), 0)))
+            assert abs(ratio[t] - ratio32[t]) > 1e-10
+            tokens[2 * j + 1], accept[2 * j + 1] = t, (ratio[t] + ratio32[t]) / 2
+        else:                                                    # the token after a draft that failed; j % 3 == 1: no token at all
+            tokens[2 * j + 1] = -1
+            left, left32 = (R.left_over(a, b) for a, b in ((p, q), (p32, q32)))
+            sums, sums32 = np.cumsum(left), np.cumsum(left32)
+            t = int(np.argmax(np.abs(sums - sums32)))
+            assert abs(sums[t] - sums32[t]) > 1e-10
+            sample[j] = (sums[t] + sums32[t]) / 2
+    v = B.DraftVerifier(vocab, 2 * n)
+    c = lambda z: torch.from_numpy(z).cuda()  # noqa: E731
+    path, counts, after = v.verify(B.Kv4Spans([(j, 0, 0, 2) for j in range(n)]), c(tokens).int(), c(x).float(), T, c(accept), c(sample), draft=c(y).float())
+    want = [R.verify([-1, 0], tokens[2 * j:2 * j + 2], x[2 * j:2 * j + 2], y[2 * j:2 * j + 2], T, accept[2 * j:2 * j + 2], sample[j]) for j in range(n)]
+    assert [(path[j, :k].tolist(), t) for j, (k, t) in enumerate(zip(counts.tolist(), after.tolist()))] == want
+    for j in range(0, n, 3):                                     # without draft logits, the border of a draft and of a token
+        p, p32 = R.softmax(x[2 * j], T), R.softmax(x[2 * j], near)
+        t = int(np.argmax(np.abs(p - p32)))
+        assert abs(p[t] - p32[t]) > 1e-10
+        tokens[2 * j + 1], accept[2 * j + 1] = t, (p[t] + p32[t]) / 2
+    path, counts, after = v.verify(B.Kv4Spans([(j, 0, 0, 2) for j in range(n)]), c(tokens).int(), c(x).float(), T, c(accept), c(sample))
+    want = [R.verify([-1, 0], tokens[2 * j:2 * j + 2], x[2 * j:2 * j + 2], None, T, accept[2 * j:2 * j + 2], sample[j]) for j in range(n)]
+    assert [(path[j, :k].tolist(), t) for j, (k, t) in enumerate(zip(counts.tolist(), after.tolist()))] == want
+
+
+@pytest.mark.parametrize("T", [5e-324, 1e-300, 1e-100, 1e-45, 1e38, 1e100, 1.7e308])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_temperatures_past_32_bits(T, with_draft):
+    """Below them the largest logits share a row, above them all of its tokens do"""
+    rng = np.random.default_rng(7)
+
+    def change(tokens, target, draft, accept, sample):
+        target[::2].clamp_(max=1.0)
+        draft[1::2].clamp_(max=1.0)
+        target[:, 5:9] = -float("inf")
+    with np.errstate(over="ignore"):
+        check(rng, [random_tree(rng, 12, 3) for _ in range(3)], 9000, [T, 1.0, T], with_draft, change=change)
+        check(rng, chains([5, 2]), 9000, [T, 0.0], with_draft, chain=True, change=change)
