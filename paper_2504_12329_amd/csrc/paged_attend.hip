@@ -43,6 +43,15 @@ __device__ __forceinline__ uint64_t seen_bits(const uint64_t *__restrict__ sees,
     return own & below(rows - j0);
 }
 
+// Weights are 2^(s c - base), c = log2(e) / sqrt(D), base the rounded product of c and the largest score s so far: one multiply-add each.  What rounding base takes away is the same
+// for all weights, and cancels; but from 2^22 on (scores no trained model has) it could be powers of two, from 2^31 on enough for weights of 0 or infinity.  There every
+// product is rounded as base is before base is taken from it, so that the largest score's weight is 1 again, and base is 0 from then on.
+__device__ __forceinline__ bool is_far(float base) { return fabsf(base) >= 0x1p22f; }
+__device__ __forceinline__ float less_far(float s, float scale, float base) {
+#pragma clang fp contract(off)
+    return (s * scale - base) / scale;
+}
+
 // One column's query: row of the span and head
 struct PagedColumn {
     int row, head;
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_few(const Kv4Spa
             const float cand = mx * scale;
             const bool raise = cand > m_i[c];
             const float m_new = raise ? cand : m_i[c];
-            const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
+            float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
             if (__builtin_amdgcn_ballot_w64(raise)) {
                 const float corr = raise ? __builtin_amdgcn_exp2f(m_i[c] - base) : 1.0f;
                 l_i[c] *= corr;
@@ -204,6 +213,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_few(const Kv4Spa
                 for (int d = 0; d < DPL; ++d) o[c][d] *= corr;
             }
             m_i[c] = m_new;
+            const bool far = is_far(base);
+            if (__builtin_amdgcn_ballot_w64(far)) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sc[c][u][r] = far ? less_far(sc[c][u][r], scale, base) : sc[c][u][r];
+                base = far ? 0.f : base;
+            }
             float p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -506,7 +523,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
         const float cand = mx * scale;
         const bool raise = cand > m_i;
         const float m_new = raise ? cand : m_i;
-        const float base = m_new == -INFINITY ? 0.f : m_new;  // a row may have seen no slot yet
+        float base = m_new == -INFINITY ? 0.f : m_new;  // a row may have seen no slot yet
         if (__builtin_amdgcn_ballot_w64(raise)) {
             const float corr = raise ? __builtin_amdgcn_exp2f(m_i - base) : 1.0f;
             l_i *= corr;
@@ -516,6 +533,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
                 for (int r = 0; r < 16; ++r) o[tt][r] *= corr;
         }
         m_i = m_new;
+        const bool far = is_far(base);
+        if (__builtin_amdgcn_ballot_w64(far)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[u][r] = far ? less_far(sc[u][r], scale, base) : sc[u][r];
+            base = far ? 0.f : base;
+        }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 2; ++u)

@@ -1,0 +1,42 @@
+"""Attention over the cache in pages where scores are at their ends, against its definition in 64 bits (paged_ref).  Tolerances as in test_gpu_paged, where nothing else is
+said."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_12329_amd import binding as B
+
+from . import paged_ref as R
+from .test_gpu_paged import HALF, TYPES, check_attend, contents, f64, make, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [1, 3, 9, 40])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attend_scores_far_from_zero(dtype, d, rows, sign):
+    """Scores of 2^16 to 2^33 (fp16), 2^83 (bf16) and more: the largest of them have the weight, those of one size share it.  Keys and queries are a number in all channels, so that every fp32 sum
+    is exact (six bits times a power of two) and scores are equal or at least a 64th apart: nothing but the rounding of
+    weights and outputs is left."""
+    rng = np.random.default_rng(rows + d)
+    kv, table = make(4, 2, d, dtype=dtype, n_pages=200, max_pages=60, n_seq=3)
+    sizes = [2.0 ** e for e in ((7, 12, 15) if dtype is torch.float16 else (7, 12, 20, 40))]
+    for size in sizes:
+        for lens in ((0, 40, 700), (300, 17, 900 - rows)):
+            spans = [(j, n, 0, rows) for j, n in enumerate(lens)]
+            steps = torch.from_numpy(rng.integers(32, 64, (200, 1, 16, 1))).double() / 64    # several slots have the largest
+            kv.cache[0, 0] = (sign * size * steps).expand(200, 2, 16, d).to(dtype).cuda()
+            q = torch.full((rows * 3, 4, d), 2.0 ** 15 if dtype is torch.float16 else size, device="cuda").to(dtype)
+            parents = [random_tree(rng, rows) for _ in spans]
+            for plan, seen_of in ((B.Kv4Spans(spans), lambda j, i: range(i + 1)), (B.DraftSpans(spans, parents), lambda j, i: R.branch(parents[j], i))):
+                got, at = f64(kv.attend(0, plan, q)), 0
+                for j, (seq, length, _, n) in enumerate(spans):
+                    k, v, there = contents(kv, table, seq, length + n)
+                    for i in range(n):
+                        seen = np.array([*range(length), *(length + x for x in seen_of(j, i))])
+                        want, spread, total = R.attention(f64(q[at + i]), k, v, seen)
+                        tol = (HALF[dtype] + 2.0 ** -15) * spread + HALF[dtype] * np.abs(want) + (2.0 ** -25 * (total + 1) if dtype is torch.float16 else 0)
+                        assert (np.abs(got[at + i] - want) <= tol).all(), f"scores of {size * float(q[0, 0, 0]) * d ** 0.5:.3g}, span {j} row {i}"
+                    at += n
