@@ -59,6 +59,7 @@ typedef uint32_t paged_u32x4 __attribute__((ext_vector_type(4)));
 struct Bf16 {
     typedef paged_bf16x8 vec8;
     static constexpr uint32_t kExponent = 0x7f807f80u, kLowBit = 0x00800080u;  // of both halves
+    static constexpr float kRaise = 0.f;
     static __device__ __forceinline__ paged_f32x4 mfma16(vec8 a, vec8 b, paged_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ paged_f32x16 mfma32(vec8 a, vec8 b, paged_f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -71,6 +72,9 @@ struct Bf16 {
 struct Fp16 {
     typedef paged_f16x8 vec8;
     static constexpr uint32_t kExponent = 0x7c007c00u, kLowBit = 0x04000400u;
+    // A column's softmax weights, and their sum, are 2^15 times as large: with the largest at 1 those below 2^-14 would lose bits of the type and those below 2^-25 be 0, while the
+    // sum in 32 bits has them.  Under one slot 17.5 above 450 equal ones the output was 0 instead of 1e-5 of their values.
+    static constexpr float kRaise = 15.f;
     static __device__ __forceinline__ paged_f32x4 mfma16(vec8 a, vec8 b, paged_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ paged_f32x16 mfma32(vec8 a, vec8 b, paged_f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {

@@ -2,7 +2,7 @@
 //
 // The query heads of a kv head are folded into columns: column i * G + h is row i of head h.  With S^T = K Q^T (slots x columns) a lane holds one column, so the
 // softmax is register arithmetic and P^T is the second product's operand as it stands: O^T = V^T P^T.  Scores, maxima, sums and outputs are fp32; the weights
-// enter the second product in 16 bits (rounded just below the running maximum's 1, where that costs least), as the framework's other attention does.
+// enter the second product in 16 bits (the largest so far as 1, in fp16 as 2^15 where numbers 2^-29 of it are still whole), as the framework's other attention does.
 //
 // What a column sees of a tile is a word of bits: all of the context, of the span's own rows the first i + 1 or those that `sees` names, nothing of a hole and
 // nothing past the end.  It is only made where some column does not see all of the tile ("part").  There the values are looked through as well: an infinity or NaN
@@ -43,13 +43,15 @@ __device__ __forceinline__ uint64_t seen_bits(const uint64_t *__restrict__ sees,
     return own & below(rows - j0);
 }
 
-// Weights are 2^(s c - base), c = log2(e) / sqrt(D), base the rounded product of c and the largest score s so far: one multiply-add each.  What rounding base takes away is the same
+// Weights are 2^(s c - base), c = log2(e) / sqrt(D), base the product of c and the largest score s so far (less kRaise), rounded: one multiply-add each.  What rounding base takes away is the same
 // for all weights, and cancels; but from 2^22 on (scores no trained model has) it could be powers of two, from 2^31 on enough for weights of 0 or infinity.  There every
-// product is rounded as base is before base is taken from it, so that the largest score's weight is 1 again, and base is 0 from then on.
+// product is rounded as base is before base is taken from it, so that the largest score's weight is 1 (or 2^kRaise) again, and base is 0 from then on.
 __device__ __forceinline__ bool is_far(float base) { return fabsf(base) >= 0x1p22f; }
+template <class T>
 __device__ __forceinline__ float less_far(float s, float scale, float base) {
 #pragma clang fp contract(off)
-    return (s * scale - base) / scale;
+    const float less = s * scale - base;
+    return (less > T::kRaise ? T::kRaise : less) / scale;  // (the largest one's rounding may add to what it is raised by)
 }
 
 // One column's query: row of the span and head
@@ -202,7 +204,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_few(const Kv4Spa
             float a, b;
             with_xor16(mx, a, b);
             mx = max_xor32(fmaxf(a, b));
-            const float cand = mx * scale;
+            const float cand = fmaf(mx, scale, -T::kRaise);
             const bool raise = cand > m_i[c];
             const float m_new = raise ? cand : m_i[c];
             float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_few(const Kv4Spa
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[c][u][r] = far ? less_far(sc[c][u][r], scale, base) : sc[c][u][r];
+                    for (int r = 0; r < 4; ++r) sc[c][u][r] = far ? less_far<T>(sc[c][u][r], scale, base) : sc[c][u][r];
                 base = far ? 0.f : base;
             }
             float p[8];
@@ -520,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[u][r]);
         mx = max_xor32(mx);
-        const float cand = mx * scale;
+        const float cand = fmaf(mx, scale, -T::kRaise);
         const bool raise = cand > m_i;
         const float m_new = raise ? cand : m_i;
         float base = m_new == -INFINITY ? 0.f : m_new;  // a row may have seen no slot yet
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(const Kv4Spans<CAP> t, c
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sc[u][r] = far ? less_far(sc[u][r], scale, base) : sc[u][r];
+                for (int r = 0; r < 16; ++r) sc[u][r] = far ? less_far<T>(sc[u][r], scale, base) : sc[u][r];
             base = far ? 0.f : base;
         }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};

@@ -40,3 +40,24 @@ def test_attend_scores_far_from_zero(dtype, d, rows, sign):
                         tol = (HALF[dtype] + 2.0 ** -15) * spread + HALF[dtype] * np.abs(want) + (2.0 ** -25 * (total + 1) if dtype is torch.float16 else 0)
                         assert (np.abs(got[at + i] - want) <= tol).all(), f"scores of {size * float(q[0, 0, 0]) * d ** 0.5:.3g}, span {j} row {i}"
                     at += n
+
+
+@pytest.mark.parametrize("nats", [9.0, 14.0, 17.5, 20.0])
+@pytest.mark.parametrize("nq,nkv,d,rows", [(4, 2, 64, 1), (4, 2, 128, 9), (4, 2, 64, 40), (12, 2, 128, 40)])
+@pytest.mark.parametrize("length", [450, 3000])
+def test_attend_one_slot_stands_above_many(nats, nq, nkv, d, rows, length):
+    """fp16: many weights far below the largest one's 1 are together what the output consists of.  They are rounded at 2^-15 of where numbers of the type are (the largest is
+    2^15): h of a weight, and 2^-40 below 2^-29; an output below 2^-14 by 2^-25."""
+    rng = np.random.default_rng(rows)
+    kv, table = make(nq, nkv, d, dtype=torch.float16, n_pages=220, max_pages=200, n_seq=1)
+    kv.cache[0] = 0.0
+    kv.cache[1] = 30 * (1 + kv.cache[1].double() / 8).half()
+    page, slot = R.place(table, 220, 16, 0, 5)
+    kv.cache[0, 0, page, :, slot] = torch.tensor(nats / d ** 0.5).half()
+    kv.cache[1, 0, page, :, slot] = 0.0
+    q = torch.ones(rows, nq, d, device="cuda").half()
+    got, (k, v, _) = f64(kv.attend(0, B.Kv4Spans([(0, length, 0, rows)]), q)), contents(kv, table, 0, length + rows)
+    for i in range(rows):
+        want, size, total = R.attention(f64(q[i]), k, v, np.arange(length + i + 1))
+        tol = (2.0 ** -11 + 2.0 ** -15) * size + 2.0 ** -11 * np.abs(want) + 2.0 ** -40 * total + 2.0 ** -25
+        assert (np.abs(got[i] - want) <= tol).all(), f"row {i}: {(np.abs(got[i] - want) / tol).max()} of the tolerance"
