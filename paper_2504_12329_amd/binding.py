@@ -777,7 +777,7 @@ class DraftSpans(Kv4Spans):
         if most > 1024:
             raise StError(ST_ERANGE, f"{most} rows of a span, trees have at most 1024")
         words = max(1, -(-most // 64))
-        parent, depth, masks, width = [], [], [], 1
+        parent, depth, masks, width, deepest = [], [], [], 1, []
         for ps in parents:
             ps = [-1, *map(int, ps[1:])][:len(ps)]
             d, m, after = [0] * len(ps), [1] * len(ps), [0] * len(ps)
@@ -791,6 +791,7 @@ class DraftSpans(Kv4Spans):
             depth += d
             masks += m
             width = max(width, *after, 1)
+            deepest.append(max(d, default=-1))
         if width > 64:
             raise StError(ST_ERANGE, f"{width} rows follow one row, at most 64 are supported")
         if words > 1:
@@ -798,7 +799,7 @@ class DraftSpans(Kv4Spans):
         parent, depth, sees = np.array(parent, dtype=np.int32), np.array(depth, dtype=np.int32), np.array(masks, dtype=np.uint64)
         n = self.rows
         bits = torch.from_numpy(np.concatenate([sees.view(np.int32), parent, depth])).to(device)     # (one copy)
-        self._take(bits[2 * n * words:2 * n * words + n], bits[2 * n * words + n:], bits[:2 * n * words].view(torch.int64).view(n, words) if n else bits.new_empty((0, words), dtype=torch.int64), width)
+        self._take(bits[2 * n * words:2 * n * words + n], bits[2 * n * words + n:], bits[:2 * n * words].view(torch.int64).view(n, words) if n else bits.new_empty((0, words), dtype=torch.int64), width, deepest)
 
     def at(self, spans):
         """The same trees at other places: spans of as many rows each, as a step later."""
@@ -806,13 +807,13 @@ class DraftSpans(Kv4Spans):
         Kv4Spans.__init__(other, spans)
         if [s[3] for s in other.spans] != [s[3] for s in self.spans]:
             raise StError(ST_EINVAL, "the spans have other numbers of rows than the trees")
-        other._take(self.parent, self.depth, self.sees, self.width)
+        other._take(self.parent, self.depth, self.sees, self.width, self.deepest)
         return other
 
     @classmethod
     def of_tensors(cls, spans, parent=None, depth=None, sees=None, width=1):
         """From tensors on the GPU, for trees that are made there: parent and depth int32 [rows], sees int64 [rows][words] (see st_draft_tree); a call that
-        reads one that is None is refused."""
+        reads one that is None is refused.  Depths past the rotation table are not seen here, and are cut to it (see st_paged_append)."""
         self = cls.__new__(cls)
         Kv4Spans.__init__(self, spans)
         for name, x, t, dims in (("parent", parent, torch.int32, 1), ("depth", depth, torch.int32, 1), ("sees", sees, torch.int64, 2)):
@@ -821,8 +822,9 @@ class DraftSpans(Kv4Spans):
         self._take(parent, depth, sees, int(width))
         return self
 
-    def _take(self, parent, depth, sees, width):
-        self.parent, self.depth, self.sees, self.width = parent, depth, sees, width
+    def _take(self, parent, depth, sees, width, deepest=None):
+        self.parent, self.depth, self.sees, self.width, self.deepest = parent, depth, sees, width, deepest
+        self.positions = 0 if deepest is None else max((s[2] + d + 1 for s, d in zip(self.spans, deepest)), default=0)  # that the rows need of a rotation table
         ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
         self._tree = st_draft_tree(ptr(parent), ptr(depth), ptr(sees), 1 if sees is None else sees.shape[1], width)
         self.tree = C.byref(self._tree)
@@ -926,6 +928,7 @@ class PagedCache(_OnStream):
         self._h, self._destroy = h, L.st_paged_destroy
         self._append, self._attend, self._keep = L.st_paged_append, L.st_paged_attend, L.st_paged_keep
         self._nq, self._nkv, self._d, self._layers = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"], cfg["n_layers"]
+        self._positions = cfg["max_pos"] if cfg["rot_dim"] else 2 ** 31      # of a tree's rows
 
     def _matrix(self, name, x, rows, heads):
         """(pointer, row stride) of [rows][heads][head_dim] or [rows][heads * head_dim]; rows may be strided."""
@@ -962,6 +965,8 @@ class PagedCache(_OnStream):
         out = self._empty((spans.rows, self._nq, self._d), self.dtype)
         if spans.rows:
             self._layer(layer)
+            if isinstance(spans, DraftSpans) and spans.positions > self._positions:
+                raise StError(ST_ERANGE, f"the drafts need {spans.positions} positions, the rotation table has {self._positions}")
             rc = self._append(self._h, layer, spans.c, spans.n, self._tree_of(spans), p, stride, qn, kn, out.data_ptr(), self._nq * self._d)
             if rc:
                 _check(rc)

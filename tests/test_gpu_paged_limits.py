@@ -1,4 +1,4 @@
-"""Attention over the cache in pages where scores are at their ends, against its definition in 64 bits (paged_ref).  Tolerances as in test_gpu_paged, where nothing else is
+"""The cache in pages where scores and positions are at their ends, against its definition in 64 bits (paged_ref).  Tolerances as in test_gpu_paged, where nothing else is
 said."""
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 from paper_2504_12329_amd import binding as B
 
 from . import paged_ref as R
-from .test_gpu_paged import HALF, TYPES, check_attend, contents, f64, make, random_tree
+from .test_gpu_paged import HALF, TYPES, check_append, contents, f64, make, random_tree
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,23 @@ def test_attend_one_slot_stands_above_many(nats, nq, nkv, d, rows, length):
         want, size, total = R.attention(f64(q[i]), k, v, np.arange(length + i + 1))
         tol = (2.0 ** -11 + 2.0 ** -15) * size + 2.0 ** -11 * np.abs(want) + 2.0 ** -40 * total + 2.0 ** -25
         assert (np.abs(got[i] - want) <= tol).all(), f"row {i}: {(np.abs(got[i] - want) / tol).max()} of the tolerance"
+
+
+def test_append_refuses_drafts_past_the_rotation_table():
+    """As it does chains of as many rows; what the trees of a step need is known on the host"""
+    rng = np.random.default_rng(2)
+    kv, table = make(4, 2, 64, max_pos=100, n_seq=2)
+    deep, wide = [-1, 0, 1, 0, 2], [-1, 0, 0]                                 # depths of 3 and 1
+    check_append(kv, table, [(0, 3, 96, 5), (1, 0, 98, 3)], [deep, wide], True, rng)
+    x = torch.randn(8, 8 * 64, device="cuda").bfloat16()
+    was = kv.cache.clone()
+    for spans in ([(0, 3, 97, 5), (1, 0, 98, 3)], [(0, 3, 96, 5), (1, 0, 99, 3)]):
+        for plan in (B.DraftSpans(spans, [deep, wide]), B.DraftSpans([(0, 3, 0, 5), (1, 0, 0, 3)], [deep, wide]).at(spans)):
+            with pytest.raises(B.StError, match="positions") as e:
+                kv.append(0, plan, x)
+            assert e.value.code == B.ST_ERANGE
+    assert torch.equal(kv.cache, was)
+    still, table = make(4, 2, 64, max_pos=100, n_seq=2, rot=0)                # nothing rotates, wherever it is
+    trees = B.DraftSpans([(0, 3, 97, 5), (1, 0, 99, 3)], [deep, wide])
+    q = still.append(0, trees, x)
+    assert torch.equal(q.flatten(1), x[:, :256]) and torch.equal(q, still.append(0, trees.at([(0, 3, 0, 5), (1, 0, 0, 3)]), x))

@@ -23,3 +23,10 @@ def test_temperatures(L, verifier, call, number):  # noqa: F811
     assert code([1.0] * 63 + [-1.0], 64)[1].startswith(b"sequence 63") and code([1.0] * 65, 65)[0] == B.ST_EINVAL and code([], 0)[0] == B.ST_OK
     if number is C.c_double:
         assert code([5e-324, 1.7e308])[1] == b"an array is NULL"
+
+
+def test_positions_that_trees_need():
+    trees = [[-1, 0, 1, 0, 2], [-1, 0, 0], [], [-1]]
+    s = B.DraftSpans([(0, 9, 20, 5), (1, 0, 21, 3), (2, 0, 5, 0), (3, 7, 7, 1)], trees, device="cpu")
+    assert s.positions == 24 and s.at([(0, 9, 5, 5), (1, 0, 8, 3), (2, 0, 30, 0), (4, 0, 3, 1)]).positions == 30
+    assert B.DraftSpans([], [], device="cpu").positions == 0
