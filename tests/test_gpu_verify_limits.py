@@ -163,3 +163,53 @@ def test_temperatures_past_32_bits(T, with_draft):
     with np.errstate(over="ignore"):
         check(rng, [random_tree(rng, 12, 3) for _ in range(3)], 9000, [T, 1.0, T], with_draft, change=change)
         check(rng, chains([5, 2]), 9000, [T, 0.0], with_draft, chain=True, change=change)
+
+
+# ---- many parts of a row ----
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (2, 1), (1, 5)])
+def test_rows_of_several_large_parts(dtype, with_draft, pad, offset):
+    """512 parts of 8192 logits and more: the form of the sums that large calls take; rows of four parts that start and end inside one"""
+    rng = np.random.default_rng(8 + offset)
+
+    def change(tokens, target, draft, accept, sample):
+        target[3, 8000:17000], target[5, 24570] = -float("inf"), float("nan")
+        draft[7, 16380:] = -float("inf")
+    trees = [random_tree(rng, n, 3) for n in ((30, 24, 25) if with_draft else (60, 50, 48))]
+    check(rng, trees, 30011, [1.0, 0.7, 1.3], with_draft, dtype, pad=pad, offset=offset)
+    check(rng, trees, 30011, [0.0, 0.5, 0.0], with_draft, dtype, pad=pad, offset=offset, change=change)
+    if dtype is torch.bfloat16:
+        check(rng, chains([len(p) for p in trees]), 30011, [0.6, 1.0, 0.0], with_draft, dtype, chain=True, pad=pad, offset=offset)
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("vocab,rows", [(300001, (3, 2)), (1100003, (3, 2))])
+def test_rows_of_more_parts_than_a_wave_has_lanes(with_draft, vocab, rows):
+    """The smaller vocabulary: 147 small parts, 74 of the draw; the larger: 135 large parts, 269 of the draw"""
+    rng = np.random.default_rng(vocab)
+    dtype = torch.float32 if vocab < 1 << 20 else torch.bfloat16
+
+    def late(tokens, target, draft, accept, sample):            # all that has a weight lies behind the first 64 parts
+        target[:, :vocab - 20000] = -float("inf")
+    for change in (None, late):
+        for heats in ([1.0, 0.7], [0.0, 1.0]):
+            check(rng, chains(rows), vocab, heats, with_draft, dtype, chain=True, change=change, offset=1)
+            check(rng, [[-1, 0, 0], [-1, 0]], vocab, heats, with_draft, dtype, change=change)
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_a_token_in_each_part(with_draft):
+    """The token is found in whichever part it is, and the parts before it count"""
+    rng = np.random.default_rng(9)
+    vocab, at = 300001, [0, 4095, 4096, 65535, 262143, 262144, 266239, 266240, 300000]
+
+    def change(tokens, target, draft, accept, sample):
+        target.fill_(-float("inf"))
+        target[:, at] = 0.0
+        draft.fill_(0.0)
+        tokens[:] = 1
+        sample[:] = (np.arange(len(sample)) + 0.5) / len(at)
+    got = check(rng, chains([2] * len(at)), vocab, [1.0] * len(at), with_draft, chain=True, change=change)
+    assert [t for _, t in got] == at
