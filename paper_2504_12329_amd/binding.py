@@ -965,9 +965,10 @@ class PagedCache(_OnStream):
         out = self._empty((spans.rows, self._nq, self._d), self.dtype)
         if spans.rows:
             self._layer(layer)
-            if isinstance(spans, DraftSpans) and spans.positions > self._positions:
+            tree = self._tree_of(spans)
+            if tree is not None and spans.positions > self._positions:
                 raise StError(ST_ERANGE, f"the drafts need {spans.positions} positions, the rotation table has {self._positions}")
-            rc = self._append(self._h, layer, spans.c, spans.n, self._tree_of(spans), p, stride, qn, kn, out.data_ptr(), self._nq * self._d)
+            rc = self._append(self._h, layer, spans.c, spans.n, tree, p, stride, qn, kn, out.data_ptr(), self._nq * self._d)
             if rc:
                 _check(rc)
         return out
