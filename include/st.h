@@ -530,8 +530,9 @@ int st_paged_append(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_
                     const void *q_norm, const void *k_norm, void *q_out, int64_t q_stride);
 
 /* Attention over the cache, scores scaled by head_dim^-1/2.  Without `tree` row i of a span attends to slots [0, len + i]; with it to slots [0, len) and
- * to those of the span's rows that tree->sees names (only sees and words are read), itself only if it is named.  A row that sees nothing gets zeros.  What is in
- * slots that a row does not see, infinities and NaN too, does not reach it.  q, out: n_q_heads * head_dim a row, aligned as there; they share no memory.
+ * to those of the span's rows that tree->sees names (only sees and words are read), itself only if it is named.  A row that sees nothing, or only
+ * scores of -infinity, gets zeros.  What is in slots that a row does not see, infinities and NaN too, does not reach it.  q, out: n_q_heads * head_dim a row, aligned
+ * as there; they share no memory.
  * ST_ERANGE: a span outside the table, too many rows, more rows of a span than `sees` has bits, more than 2^24 blocks of work. */
 int st_paged_attend(st_paged *c, int32_t layer, const st_kv4_span *spans, int32_t n, const st_draft_tree *tree, const void *q, int64_t q_stride,
                     void *out, int64_t out_stride);
@@ -566,7 +567,7 @@ void st_verify_destroy(st_verify *v);
  * stays if accept[c] < p(t) / q(t) (accept[c] < p(t) without draft logits); if not, p becomes max(p - q, 0) (p without t), scaled to the sum 1, for the next.  From the
  * row that stays it goes on; where none does, the next token is the least x with p(0) + ... + p(x) > sample[j] (p's own sum in the place of 1).
  * A temperature of 0: the row that has the largest target logit's token (the lowest token among equals) stays, and the next token is that token.
- * A p that rounding leaves empty is taken as it was before the first draft failed.  A row of logits with a NaN, with none above -infinity, or (T > 0) with +infinity has no
+ * A p that rounding leaves empty is taken as it was before the first draft failed (what p and q differ by counts from 2^-42 of p on).  A row of logits with a NaN, with none above -infinity, or (T > 0) with +infinity has no
  * distribution: no row after it stays, and the next token is -1.  Tokens outside the vocabulary do not stay.
  *
  * path (device int32 [n][path_stride], path_stride >= rows[j]): the rows that stay, -1 behind them up to path_stride; accepted: their number; next: the token. */

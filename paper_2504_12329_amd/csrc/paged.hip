@@ -21,7 +21,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // are passed on.  The norm's sum is an exchange over the head's 8 or 16 lanes.
 //
 // Memory bounds it: every number is read and written once, 8 bytes an instruction and lane so that a thread has whole pairs of either order without exchanges.  4096
-// rows of 40 / 8 heads of 128 with norms and rotation take 21.1 us, 119 MB at 5.6 TB/s (a copy of 2 GiB reaches 4.9; the rotation table comes from L2); a single row 2.1 us.
+// rows of 40 / 8 heads of 128 with norms and rotation take 21.0 us, 119 MB at 5.7 TB/s (a copy of 2 GiB reaches 4.9; the rotation table comes from L2); a single row 2.1 us.
 // ---------------------------------------------------------------------------------------
 template <class T, int D, int CAP>
 __global__ __launch_bounds__(256) void k_paged_append(const Kv4Spans<CAP> t, const PagedView view, const int32_t *__restrict__ depth,
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void k_paged_append(const Kv4Spans<CAP> t, con
 // ---------------------------------------------------------------------------------------
 // Keep.  A thread owns 16 bytes of a slot in one layer, plane and kv head, and moves them down the branch: every source lies behind its destination and behind all
 // destinations before, so sources that are read before their batch's first write are as they were.  A chain of four dependent loads (count, path, table, row) and
-// a batch of rows in flight: latency.  8 sequences of 21 rows in 64 layers of 8 heads of 128 take 7.3 us, one sequence in 28 layers of 2 heads 4.2 us.
+// a batch of rows in flight: latency.  8 sequences of 21 rows in 64 layers of 8 heads of 128 take 7.2 us, one sequence in 28 layers of 2 heads 4.0 us.
 // ---------------------------------------------------------------------------------------
 constexpr int kKeepBatch = 8;
 

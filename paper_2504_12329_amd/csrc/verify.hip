@@ -5,7 +5,7 @@
 // (where p_k is positive, p_k - q = (p - (a_k + b_k) q) / b_k, and elsewhere both are cut), so that a failure costs one look at p and q and nothing is stored.  A draft
 // with token t stays if u q(t) b_k < max(p(t) - a_k q(t), 0).  Without draft logits p_k is p without the failed tokens and b_k what they leave of its sum.
 //
-// All of it is in 64 bits: a verdict compares two numbers, and the token that follows is looked for among 150000 sums that lie 1e-5 apart.
+// All of it is in 64 bits, the temperatures too: a verdict compares two numbers, and the token that follows is looked for among 150000 sums that lie 1e-5 apart.
 //
 //   k_verify_sums   largest logit and sum of exponentials of every part of every row          (the whole chip, all logits once)
 //   k_verify_rows   the verdict after every row, a wave each; with draft logits, of its first draft
@@ -301,8 +301,8 @@ __device__ __forceinline__ bool has_followers(const int32_t *parent, int first, 
 // Sums.  A block is one part of one row; the part stays in registers between its largest number and its sum.  Draft rows that nothing follows, and those of greedy
 // sequences, are not read.
 //
-// The vector pipe bounds it: eight instructions of 64 bits (as fast here as those of 32) and some six others a logit.  256 rows of 152064 bf16 logits and as many of a draft, 156 MB:
-// 42 us, 3.7 TB/s; 336 and 336 rows of 152064 fp32 logits, of which 303 MB are read: 61 us, 4.9 TB/s, what a large copy reaches.  Parts of 4096 logits cost nothing, of
+// The vector pipe bounds it: eight instructions of 64 bits (as fast here as those of 32) and some six others a logit.  256 rows of 152064 bf16 logits and 159 of a draft, 126 MB:
+// 42 us, 3.0 TB/s; 336 and 240 rows of 152064 fp32 logits, 350 MB: 61 us, 5.7 TB/s, more than a large copy reaches.  Parts of 4096 logits cost nothing, of
 // 2048 20 % (the table is filled in every block); six and eight waves a SIMD spill (+12 and +24 %); a polynomial off by 4e-11 is not near enough (a verdict on what is left of
 // a difference goes wrong).
 // ---------------------------------------------------------------------------------------
@@ -669,7 +669,7 @@ __global__ __launch_bounds__(64) void k_verify_close(const VerifyArgs a) {
 
 // ---------------------------------------------------------------------------------------
 // Draw.  Every block of a sequence walks through the rows that stay (one load, then steps in LDS), and sums up one part of the weights at the end of the walk; the first
-// one writes the path.  7.8 us for 16 sequences of 21 rows of 152064 logits, 8.7 with the verdicts of 5 rows: the walk and one part a block, dependent loads.
+// one writes the path.  7.8 us for 16 sequences of 21 rows of 152064 logits, 9.1 with the verdicts of 5 rows: the walk and one part a block, dependent loads.
 // ---------------------------------------------------------------------------------------
 // FUSED: of few rows the verdicts too, by every block alike, in the place of k_verify_rows.
 constexpr int kFusedRows = 8;
@@ -720,7 +720,7 @@ __global__ __launch_bounds__(FUSED ? 64 * kFusedRows : 256) void k_verify_draw(c
 // ---------------------------------------------------------------------------------------
 // Pick: the first token at which the running sum of the weights passes sample * their sum.  The part first, by every wave alike; in it a thread has neighbouring
 // tokens, so that the sums run from thread to thread; and of the thread that passes, its tokens, a lane each.  Where rounding lets none pass, the last with a weight.
-// 5.5 us for one sequence, 8.0 for 16: three dependent reads and the scans between them.
+// 5.5 us for one sequence, 7.5 for 16: three dependent reads and the scans between them.
 // ---------------------------------------------------------------------------------------
 // The first of 64 lanes at which the running sum of v passes the goal, or the last with a v; -1: there is none.  before: in the sum before the lanes, out before that one
 __device__ __forceinline__ int passing_lane(double v, double goal, double &before, bool &passes) {
