@@ -81,3 +81,19 @@ def test_append_refuses_drafts_past_the_rotation_table():
     trees = B.DraftSpans([(0, 3, 97, 5), (1, 0, 99, 3)], [deep, wide])
     q = still.append(0, trees, x)
     assert torch.equal(q.flatten(1), x[:, :256]) and torch.equal(q, still.append(0, trees.at([(0, 3, 0, 5), (1, 0, 0, 3)]), x))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("nq,nkv,d,rows,length", [(4, 2, 64, 1, 0), (4, 2, 64, 5, 40), (12, 2, 128, 9, 3000), (12, 2, 128, 40, 300)])
+def test_attend_rows_whose_scores_are_all_minus_infinity(dtype, nq, nkv, d, rows, length):
+    """Zeros, and other heads and rows as they are"""
+    kv, table = make(nq, nkv, d, dtype=dtype, n_pages=220, max_pages=200, n_seq=1)
+    q = torch.randn(rows, nq, d, device="cuda").to(dtype).abs()
+    q[rows // 2] = -q[rows // 2]                                              # its scores are all +infinity: NaN
+    plan = B.Kv4Spans([(0, length, 0, rows)])
+    want = kv.attend(0, plan, q)
+    kv.cache[0, 0, :, 0, :, 3] = -float("inf")                                # of one kv head
+    got = kv.attend(0, plan, q)
+    others = [i for i in range(rows) if i != rows // 2]
+    assert (got[others, :nq // nkv] == 0).all() and torch.equal(got[:, nq // nkv:], want[:, nq // nkv:])
+    assert torch.isnan(got[rows // 2, :nq // nkv]).all() and torch.isfinite(want).all()
